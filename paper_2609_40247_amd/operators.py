@@ -17,8 +17,10 @@ There is no CPU fallback: without the built library or a GPU the calls raise.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
+import struct
 
 import torch
 
@@ -74,23 +76,37 @@ class HerschelDecodeArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("status", _P), ("hip_stream", _P)]
 
 
-_ready = set()
+# The same structures as struct formats: filling one this way takes 0.2 us
+# instead of 1 to 2, and a decode step's calls are as short as their host time.
+_ROPE = struct.Struct("@3P6q2P4q2PqPq6i2P")
+_READ = struct.Struct("@PqPiq2Pi2P")
+_PROMPT = struct.Struct("@3P6q4Pi2q7if2P")
+_DECODE = struct.Struct("@P3q3PqP5ifPN2P")
+
+_ready = {}
 
 
 def load(variant: str | None = None) -> ctypes.CDLL:
     """The library of ``herschel.load`` with the operators' signatures."""
-    lib = H.load(variant)
-    if id(lib) not in _ready:
-        for name, args in (("herschel_rope_write", [HerschelRopeArgs, HerschelCache]),
-                           ("herschel_cache_read", [HerschelReadArgs, HerschelCache]),
-                           ("herschel_attn_prompt", [HerschelPromptArgs]),
-                           ("herschel_attn_decode", [HerschelDecodeArgs, HerschelCache])):
+    lib = _ready.get(variant) if variant else None
+    if lib is None:
+        lib = H.load(variant)
+        for name, n in (("herschel_rope_write", 2), ("herschel_cache_read", 2), ("herschel_attn_prompt", 1),
+                        ("herschel_attn_decode", 2)):
             fn = getattr(lib, name)
-            fn.restype, fn.argtypes = ctypes.c_int, [ctypes.POINTER(a) for a in args]
+            fn.restype, fn.argtypes = ctypes.c_int, [_P] * n
         lib.herschel_attn_decode_workspace.restype = ctypes.c_int
-        lib.herschel_attn_decode_workspace.argtypes = [_I32, _I32, _I32, ctypes.POINTER(HerschelCache),
-                                                       ctypes.POINTER(ctypes.c_size_t)]
-        _ready.add(id(lib))
+        lib.herschel_attn_decode_workspace.argtypes = [_I32, _I32, _I32, _P, ctypes.POINTER(ctypes.c_size_t)]
+        if variant:
+            _ready[variant] = lib
+    return lib
+
+
+def _lib() -> ctypes.CDLL:
+    """The library that $HERSCHEL_LIB named at the first call."""
+    lib = _ready.get(None)
+    if lib is None:
+        lib = _ready[None] = load()
     return lib
 
 
@@ -100,51 +116,58 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _rows(t: torch.Tensor, name: str, dims: int = 3) -> None:
-    """A tensor of rows of heads on a GPU whose heads' elements are contiguous."""
-    _need(t.is_cuda, f"{name} must be on a GPU")
-    _need(t.dim() == dims, f"{name} must have {dims} dimensions")
-    _need(t.dtype in TYPES, f"{name} must be bfloat16 or float16")
-    _need(t.shape[-1] < 2 or t.stride(-1) == 1, f"{name}'s last dimension must be contiguous")
+def _rows(t: torch.Tensor, name: str, dims: int = 3) -> tuple:
+    """The strides of a tensor of rows of heads on a GPU whose heads' elements are contiguous."""
+    st = t.stride()
+    if not (t.is_cuda and len(st) == dims and t.dtype in TYPES and (st[-1] == 1 or t.shape[-1] < 2)):
+        _need(t.is_cuda, f"{name} must be on a GPU")
+        _need(t.dim() == dims, f"{name} must have {dims} dimensions")
+        _need(t.dtype in TYPES, f"{name} must be bfloat16 or float16")
+        _need(False, f"{name}'s last dimension must be contiguous")
+    return st
 
 
-def _ints(t: torch.Tensor, name: str, dtype, shape: tuple, like: torch.Tensor) -> None:
-    _need(t.dtype == dtype, f"{name} must be {dtype}")
-    _need(t.device == like.device, f"{name} must be on {like.device}")
-    _need(tuple(t.shape) == shape, f"{name} must have shape {shape}")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
+def _ints(t: torch.Tensor, name: str, dtype, shape: tuple, device: int) -> int:
+    """The address of a contiguous tensor of this type and shape on a GPU."""
+    if not (t.dtype == dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()):
+        _need(t.dtype == dtype, f"{name} must be {dtype}")
+        _need(t.get_device() == device, f"{name} must be on GPU {device}")
+        _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
+        _need(False, f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _same(a: torch.Tensor, b: torch.Tensor, name: str) -> None:
-    _need(a.dtype == b.dtype and a.device == b.device, f"{name} must have the type and device of the other rows")
+def _like(t: torch.Tensor, first: torch.Tensor, name: str) -> None:
+    if not (t.dtype == first.dtype and t.get_device() == first.get_device()):
+        _need(False, f"{name} must have the type and device of the other rows")
 
 
-def _table(t: torch.Tensor, n_seqs: int, like: torch.Tensor) -> None:
-    _need(t.dtype == torch.int32 and t.dim() == 2 and t.shape[0] == n_seqs, "block_table must be int32 [sequences, entries]")
-    _need(t.device == like.device, f"block_table must be on {like.device}")
-    _need(t.shape[1] < 2 or t.stride(1) == 1, "block_table's rows must be contiguous")
-    _need(t.shape[0] < 2 or t.stride(0) == t.shape[1], "block_table's rows must follow each other")
+def _table(t: torch.Tensor, n_seqs: int, device: int) -> int:
+    if not (t.dtype == torch.int32 and t.dim() == 2 and t.shape[0] == n_seqs and t.get_device() == device and
+            t.is_contiguous()):
+        _need(False, f"block_table must be int32 [{n_seqs}, entries], contiguous, on GPU {device}")
+    return t.data_ptr()
 
 
-def _call(code: int, name: str) -> None:
-    if code == H.EINVAL:
-        raise ValueError(f"{name}: {H.herschel_strerror(code)}")
+def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> None:
+    """Calls an entry point with the tensors' device current."""
+    other = torch.cuda.current_device() != device
+    with torch.cuda.device(device) if other else _NOTHING:
+        code = fn(args) if cache is None else fn(args, cache or None)
     if code != H.OK:
-        raise RuntimeError(f"{name}: {H.herschel_strerror(code)}")
+        raise (ValueError if code == H.EINVAL else RuntimeError)(f"{name}: {H.herschel_strerror(code)}")
 
 
-def _st(t: torch.Tensor) -> _Strides:
-    return _Strides(t.stride(-3), t.stride(-2))
+# The current stream's handle by itself: 0.1 us, the Stream object around it 2.
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
+_NOTHING = contextlib.nullcontext()
 
 
-def _stream(t: torch.Tensor) -> int:
-    return torch.cuda.current_stream(t.device).cuda_stream
-
-
-def _status(status: torch.Tensor | None, like: torch.Tensor) -> int | None:
+def _status(status: torch.Tensor | None, device: int) -> int:
     if status is None:
-        return None
-    _need(status.dtype == torch.int32 and status.numel() == 1 and status.device == like.device,
+        return 0
+    _need(status.dtype == torch.int32 and status.numel() == 1 and status.get_device() == device,
           "status must be one int32 on the tensors' device")
     return status.data_ptr()
 
@@ -176,13 +199,13 @@ class PagedCache:
         for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             _need((s is not None) == self.quantised, f"{name} goes with an 8-bit cache, and with no other")
             if s is not None:
-                _ints(s, name, torch.float32, tuple(k.shape[:3]), k)
+                _ints(s, name, torch.float32, k.shape[:3], k.get_device())
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.n_pages, self.n_heads, self.page_size, self.head_dim = k.shape
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.struct = HerschelCache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
                                     None if v_scale is None else v_scale.data_ptr(), *k.shape, KINDS[k.dtype])
-        self._ref = ctypes.byref(self.struct)
+        self._at, self._status, self._device = ctypes.addressof(self.struct), self.status.data_ptr(), k.get_device()
 
     @classmethod
     def allocate(cls, n_pages: int, n_heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
@@ -199,8 +222,9 @@ class PagedCache:
         raise_faults(self.status)
 
     def _fits(self, t: torch.Tensor) -> None:
-        _need(t.device == self.k.device, "the cache is on another device")
-        _need(self.quantised or t.dtype == self.k.dtype, "a 16-bit cache has the type of the rows")
+        if t.get_device() != self._device or not (self.quantised or t.dtype == self.k.dtype):
+            _need(t.get_device() == self._device, "the cache is on another device")
+            _need(False, "a 16-bit cache has the type of the rows")
 
 
 def rotary_table(n_positions: int, rotary_dim: int, base: float = 10_000.0, stretch: float = 1.0,
@@ -237,41 +261,43 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
     themselves); k's is None unless ``keep_keys`` or ``k_out`` asks for it or there is no cache."""
     _need(q is not None or k is not None, "q or k must be given")
     first = q if q is not None else k
-    T, D = first.shape[0], first.shape[-1]
-    for t, name in ((q, "q"), (k, "k"), (v, "v"), (q_out, "q_out"), (k_out, "k_out")):
-        if t is not None:
-            _rows(t, name)
-            _same(t, first, name)
-            _need(t.shape[0] == T and t.shape[2] == D, f"{name} must have the tokens and head size of the other rows")
+    _rows(first, "q" if q is not None else "k")
+    dev = first.get_device()
+    T, _, D = first.shape
+
+    def rows(t, name, like=None):
+        """(address, row stride, head stride, heads) of rows that go with the first ones."""
+        if t is None:
+            return 0, 0, 0, 0
+        st, shape = _rows(t, name), t.shape
+        _like(t, first, name)
+        if shape[0] != T or shape[2] != D or (like is not None and shape[1] != like):
+            _need(False, f"{name} must have the tokens, heads and head size of the rows it goes with")
+        return t.data_ptr(), st[0], st[1], shape[1]
+
+    qa, ka = rows(q, "q"), rows(k, "k")
+    va = rows(v, "v", ka[3]) if k is not None else rows(v, "v")
     _need(layout in LAYOUTS, "layout must be 'half' or 'interleaved'")
-    _need(table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous() and
-          table.device == first.device, "table must be float32 [positions, pairs, 2], contiguous, on the rows' device")
-    _ints(positions, "positions", torch.int64, (T,), first)
+    if not (table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous() and
+            table.get_device() == dev):
+        _need(False, "table must be float32 [positions, pairs, 2], contiguous, on the rows' device")
+    pos, slot = _ints(positions, "positions", torch.int64, (T,), dev), 0
     if cache is not None:
         _need(k is not None and v is not None and slots is not None, "a cache needs k, v and slots")
-        _need(v.shape == k.shape, "v must have k's shape")
-        _need(k.shape[1] == cache.n_heads and D == cache.head_dim, "the cache has another number of heads or head size")
+        _need(ka[3] == cache.n_heads and D == cache.head_dim, "the cache has another number of heads or head size")
         cache._fits(k)
-        _ints(slots, "slots", torch.int64, (T,), first)
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None and (keep_keys or cache is None):
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    for o, i, name in ((q_out, q, "q_out"), (k_out, k, "k_out")):
-        _need(o is None or (i is not None and o.shape == i.shape), f"{name} must have its input's shape")
-    zero = _Strides(0, 0)
-    args = HerschelRopeArgs(
-        None if q is None else q.data_ptr(), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
-        zero if q is None else _st(q), zero if k is None else _st(k), zero if v is None else _st(v),
-        None if q_out is None else q_out.data_ptr(), None if k_out is None else k_out.data_ptr(),
-        zero if q_out is None else _st(q_out), zero if k_out is None else _st(k_out), positions.data_ptr(),
-        table.data_ptr(), table.shape[0], None if cache is None else slots.data_ptr(), T,
-        0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D, 2 * table.shape[1], LAYOUTS[layout],
-        TYPES[first.dtype], cache.status.data_ptr() if status is None and cache is not None else _status(status, first),
-        _stream(first))
-    lib = lib or load()
-    with torch.cuda.device(first.device):
-        _call(lib.herschel_rope_write(ctypes.byref(args), None if cache is None else cache._ref), "rope_write")
+        slot = _ints(slots, "slots", torch.int64, (T,), dev)
+    if q_out is None and q is not None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if k_out is None and k is not None and (keep_keys or cache is None):
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    _need((q_out is None or q is not None) and (k_out is None or k is not None), "an output needs its input")
+    qo, ko = rows(q_out, "q_out", qa[3]), rows(k_out, "k_out", ka[3])
+    reported = _status(status, dev) if status is not None else cache._status if cache is not None else 0
+    args = _ROPE.pack(qa[0], ka[0], va[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[0], ko[0], qo[1], qo[2], ko[1],
+                      ko[2], pos, table.data_ptr(), table.shape[0], slot, T, qa[3], ka[3], D, 2 * table.shape[1],
+                      LAYOUTS[layout], TYPES[first.dtype], reported, _stream(dev))
+    _call((lib or _lib()).herschel_rope_write, dev, "rope_write", args, 0 if cache is None else cache._at)
     return q_out, k_out
 
 
@@ -284,20 +310,16 @@ def cache_read(cache: PagedCache, block_table: torch.Tensor, cu: torch.Tensor, *
     _need(dtype in TYPES, "dtype must be bfloat16 or float16")
     _need(cache.head_dim % 16 == 0, "cache_read needs a head size that is a multiple of 16")
     _need(cu.dim() == 1 and cu.shape[0] >= 2, "cu must hold a sequence's start and end")
-    _ints(cu, "cu", torch.int32, tuple(cu.shape), cache.k)
-    _table(block_table, cu.shape[0] - 1, cache.k)
+    dev, n = cache._device, cu.shape[0] - 1
+    starts, table = _ints(cu, "cu", torch.int32, cu.shape, dev), _table(block_table, n, dev)
     _need(total >= 0, "total must not be negative")
     shape = (total, cache.n_heads, cache.head_dim)
-    k_out = torch.empty(shape, dtype=dtype, device=cache.k.device) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=dtype, device=cache.k.device) if v_out is None else v_out
-    for o, name in ((k_out, "k_out"), (v_out, "v_out")):
-        _ints(o, name, dtype, shape, cache.k)
-        cache._fits(o)
-    args = HerschelReadArgs(block_table.data_ptr(), block_table.shape[1], cu.data_ptr(), cu.shape[0] - 1, total,
-                            k_out.data_ptr(), v_out.data_ptr(), TYPES[dtype], cache.status.data_ptr(), _stream(cache.k))
-    lib = lib or load()
-    with torch.cuda.device(cache.k.device):
-        _call(lib.herschel_cache_read(ctypes.byref(args), cache._ref), "cache_read")
+    k_out = cache.k.new_empty(shape, dtype=dtype) if k_out is None else k_out
+    v_out = cache.k.new_empty(shape, dtype=dtype) if v_out is None else v_out
+    cache._fits(k_out)
+    args = _READ.pack(table, block_table.shape[1], starts, n, total, _ints(k_out, "k_out", dtype, shape, dev),
+                      _ints(v_out, "v_out", dtype, shape, dev), TYPES[dtype], cache._status, _stream(dev))
+    _call((lib or _lib()).herschel_cache_read, dev, "cache_read", args, cache._at)
     return k_out, v_out
 
 
@@ -310,32 +332,27 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     Query i of nq sees key j of nk iff, causal, j <= i + nk - nq and, with a window, j > i + nk - nq - window.
     ``max_q`` is the longest sequence's number of queries, ``scale`` the scores' (dim ** -0.5 if not given).
     Returns the outputs, with ``return_lse`` also the log of each row's sum of exponentials [queries, heads]."""
-    for t, name in ((q, "q"), (k, "k"), (v, "v")):
-        _rows(t, name)
-        _same(t, q, name)
-    D = q.shape[2]
-    _need(D in (64, 128), "attention needs heads of 64 or 128")
+    sq, sk, sv = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    _like(k, q, "k")
+    _like(v, q, "v")
+    dev, (n_q, heads, D), (n_k, kv_heads, _) = q.get_device(), q.shape, k.shape
+    _need(D == 64 or D == 128, "attention needs heads of 64 or 128")
     _need(k.shape == v.shape and k.shape[2] == D, "k and v must have one shape, and q's head size")
-    _need(k.shape[1] >= 1 and q.shape[1] >= 1 and q.shape[1] % k.shape[1] == 0, "q's heads must be a multiple of k's")
-    cu_k = cu_q if cu_k is None else cu_k
+    _need(kv_heads >= 1 and heads >= 1 and heads % kv_heads == 0, "q's heads must be a multiple of k's")
     _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, "cu_q must hold a sequence's start and end")
-    _ints(cu_q, "cu_q", torch.int32, tuple(cu_q.shape), q)
-    _ints(cu_k, "cu_k", torch.int32, tuple(cu_q.shape), q)
-    _need(0 <= max_q <= q.shape[0], "max_q must be a number of q's rows")
+    from_q = _ints(cu_q, "cu_q", torch.int32, cu_q.shape, dev)
+    from_k = from_q if cu_k is None else _ints(cu_k, "cu_k", torch.int32, cu_q.shape, dev)
+    _need(0 <= max_q <= n_q, "max_q must be a number of q's rows")
     _need(window >= 0, "window must not be negative")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        _ints(out, "out", q.dtype, tuple(q.shape), q)
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    args = HerschelPromptArgs(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), _st(q), _st(k), _st(v), out.data_ptr(),
-        None if lse is None else lse.data_ptr(), cu_q.data_ptr(), cu_k.data_ptr(), cu_q.shape[0] - 1, q.shape[0],
-        k.shape[0], max_q, q.shape[1], k.shape[1], D, TYPES[q.dtype], int(causal), window,
-        D ** -0.5 if scale is None else scale, _status(status, q), _stream(q))
-    lib = lib or load()
-    with torch.cuda.device(q.device):
-        _call(lib.herschel_attn_prompt(ctypes.byref(args)), "attn_prompt")
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    lse = q.new_empty((n_q, heads), dtype=torch.float32) if return_lse else None
+    args = _PROMPT.pack(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
+        _ints(out, "out", q.dtype, q.shape, dev), lse.data_ptr() if return_lse else 0, from_q, from_k,
+        cu_q.shape[0] - 1, n_q, n_k, max_q, heads, kv_heads, D, TYPES[q.dtype], bool(causal), window,
+        D ** -0.5 if scale is None else scale, _status(status, dev), _stream(dev))
+    _call((lib or _lib()).herschel_attn_prompt, dev, "attn_prompt", args)
     return (out, lse) if return_lse else out
 
 
@@ -354,10 +371,10 @@ class DecodeAttention:
         _need(heads >= 1 and heads % cache.n_heads == 0, "heads must be a multiple of the cache's")
         _need(1 <= new_tokens <= 1024, "new_tokens must be 1 to 1024")
         self.cache, self.batch, self.heads, self.new_tokens, self.dtype = cache, batch, heads, new_tokens, dtype
-        self.lib = lib or load()
+        self.lib = lib or _lib()
         size = ctypes.c_size_t(0)
-        _call(self.lib.herschel_attn_decode_workspace(batch, new_tokens, heads, cache._ref, ctypes.byref(size)),
-              "DecodeAttention")
+        code = self.lib.herschel_attn_decode_workspace(batch, new_tokens, heads, cache._at, ctypes.byref(size))
+        _need(code == H.OK, "DecodeAttention: invalid sizes")
         self.workspace_bytes = int(size.value)
         self._workspaces = {}
 
@@ -368,29 +385,25 @@ class DecodeAttention:
         cached tokens, the new ones among them.  Returns [sequences, new tokens, heads, dim], with
         ``return_lse`` also the log of each row's sum of exponentials."""
         c = self.cache
-        _rows(q, "q", 4)
-        B = q.shape[0]
-        _need(q.dtype == self.dtype, f"q must be {self.dtype}")
+        sq, shape, dev = _rows(q, "q", 4), q.shape, q.get_device()
+        B = shape[0]
+        _need(q.dtype == self.dtype, "q must have the type that DecodeAttention was made for")
         c._fits(q)
-        _need(1 <= B <= self.batch and tuple(q.shape[1:]) == (self.new_tokens, self.heads, c.head_dim),
+        _need(1 <= B <= self.batch and shape[1:] == (self.new_tokens, self.heads, c.head_dim),
               "q must have the sizes that the workspace is for")
-        _table(block_table, B, q)
-        _ints(seq_lens, "seq_lens", torch.int32, (B,), q)
+        table, lens = _table(block_table, B, dev), _ints(seq_lens, "seq_lens", torch.int32, (B,), dev)
         _need(window >= 0, "window must not be negative")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            _ints(out, "out", q.dtype, tuple(q.shape), q)
-        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device) if return_lse else None
-        stream = _stream(q)
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        lse = q.new_empty(shape[:3], dtype=torch.float32) if return_lse else None
+        stream = _stream(dev)
         ws = self._workspaces.get(stream)
         if ws is None:
             ws = self._workspaces[stream] = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device)
-        args = HerschelDecodeArgs(
-            q.data_ptr(), q.stride(0), _st(q), out.data_ptr(), None if lse is None else lse.data_ptr(),
-            block_table.data_ptr(), block_table.shape[1], seq_lens.data_ptr(), B, self.new_tokens, self.heads,
+        args = _DECODE.pack(
+            q.data_ptr(), sq[0], sq[1], sq[2], _ints(out, "out", q.dtype, shape, dev),
+            lse.data_ptr() if return_lse else 0, table, block_table.shape[1], lens, B, self.new_tokens, self.heads,
             TYPES[q.dtype], window, c.head_dim ** -0.5 if scale is None else scale, ws.data_ptr(),
-            self.workspace_bytes, c.status.data_ptr(), stream)
-        with torch.cuda.device(q.device):
-            _call(self.lib.herschel_attn_decode(ctypes.byref(args), c._ref), "DecodeAttention")
+            self.workspace_bytes, c._status, stream)
+        _call(self.lib.herschel_attn_decode, dev, "DecodeAttention", args, c._at)
         return (out, lse) if return_lse else out

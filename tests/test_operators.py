@@ -790,6 +790,20 @@ def test_operator_struct_layouts_match_the_header(tmp_path):
             assert int(got[f"{cname}.{f}"]) == getattr(cls, f).offset, f"{cname}.{f}"
 
 
+def test_packed_arguments_match_the_structures():
+    """The formats that calls are packed with lay every field where the ctypes structure has it."""
+    for fmt, cls in ((O._ROPE, O.HerschelRopeArgs), (O._READ, O.HerschelReadArgs), (O._PROMPT, O.HerschelPromptArgs),
+                     (O._DECODE, O.HerschelDecodeArgs)):
+        flat = []
+        for name, kind in cls._fields_:
+            flat += [(name, f) for f, _ in kind._fields_] if hasattr(kind, "_fields_") else [(name, None)]
+        assert fmt.size <= ctypes.sizeof(cls)
+        got = cls.from_buffer_copy(fmt.pack(*range(1, len(flat) + 1)).ljust(ctypes.sizeof(cls), b"\0"))
+        for i, (name, part) in enumerate(flat):
+            x = getattr(got, name)
+            assert (getattr(x, part) if part else x) == i + 1, (cls.__name__, name)
+
+
 def test_tensor_checks_on_the_cpu():
     """The binding refuses tensors that are not on a GPU, or of the wrong kind, before it calls the library."""
     x = torch.zeros(4, 2, 64, dtype=BF)
