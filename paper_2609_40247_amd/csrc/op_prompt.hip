@@ -11,24 +11,22 @@
 //  - A wave has 32 rows and two waves share a SIMD, of different workgroups: one
 //    wave alone issues a VALU instruction every 6 cycles, two every 3, and the
 //    exponentials of one run beside the products of the other.
-//  - Keys lie in LDS by rows, copied there without passing registers; values
-//    transposed, by dimensions, with each 16 keys in the order above, so that
-//    every operand is one 16-byte read.  The chunks of a row are permuted by the
-//    row's number (K) and by the dimension's (V), which spreads a wave's reads
-//    over all banks.  The transposition is a thread's own: it loads 8 dimensions
-//    of 4 keys and rearranges them with byte permutes.
+//  - Keys and values go to LDS by rows without passing registers, the next tile
+//    of values and the next two of keys while this one is worked on.  The chunks
+//    of a row are permuted by the row's number, differently for K and V, which
+//    spreads a wave's reads over all banks.  V's operand has its keys in a lane:
+//    reads that transpose blocks of four keys by 16 dimensions deliver it.
 //  - The reference of a row's exponentials stays as long as a tile's sum shows
 //    that no exponential is large; then the maximum is taken and the
 //    accumulators scaled.  No maximum is computed otherwise.
 //  - Only tiles in which some row does not see some key are masked.  A hidden
-//    key's exponential is 0, which an infinite or NaN value would turn into NaN:
-//    in the tiles that may be masked such values go into LDS as 0, and if there
-//    were any, they are added at the end to the rows that see them.
+//    key's exponential is 0, which an infinite or NaN value turns into NaN: a
+//    wave whose sums are not finite at the end computes its rows again, key by
+//    key, with nothing but the keys that each row sees.
 #include "ops.hpp"
 
 namespace hop {
 
-constexpr int QROWS = 128;  // query rows of a workgroup, 32 a wave
 constexpr int KT = 64;      // keys of a tile
 constexpr float NO_KEY = -3.0e38f;
 constexpr float LARGE = 4096.0f;  // a sum above this moves the reference (half's largest value is 65504)
@@ -42,22 +40,41 @@ struct PromptArgs {
   int spread;  // XCDs that share a key head's workgroups; 0: heads in turn
 };
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 LdsHalves;
+
 // A wave's copy of 64 chunks of 16 bytes from global memory to consecutive LDS.
 __device__ __forceinline__ void copy_to_lds(const void* from, void* to) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
                                    (__attribute__((address_space(3))) void*)to, 16, 0, 0);
 }
 
-template <int TYPE, int D, bool VEC>
-__global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs p) {
+// Orders N products and their READS LDS reads each: AHEAD products' reads
+// first, then one product and the reads of a later one in turn.  Left alone, the
+// compiler waits for each read just before its product: 60 cycles of 32.
+constexpr int AHEAD = 4;
+template <int N, int READS, int GROUP>
+__device__ __forceinline__ void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, GROUP);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, GROUP);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, GROUP);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, GROUP);
+}
+
+template <int TYPE, int D, int WAVES, bool VEC>
+__global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
+  constexpr int QROWS = 32 * WAVES, THREADS = WAVE * WAVES;
   const herschel_prompt_args& a = p.a;
   constexpr int NC = D / 8;    // 16-byte chunks of a K row
   constexpr int DT = D / 32;   // blocks of dimensions
   constexpr int NS = D / 16;   // steps of the first product
   constexpr int KBYTES = KT * D * 2;
-  __shared__ __align__(16) char s_k[2 * KBYTES];
-  __shared__ __align__(16) char s_v[2 * KBYTES];
-  __shared__ int s_odd;  // values that are not finite in tiles that may be masked
+  constexpr int VBUFS = WAVES == 8 ? 3 : 2;
+  __shared__ __align__(16) char s_k[3 * KBYTES];
+  __shared__ __align__(16) char s_v[VBUFS * KBYTES];
 
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), n = lane % 32, g = lane / 32;
   // Longest tiles first (the end of a causal sequence); the heads of a key head
@@ -99,12 +116,13 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs p) {
   const int wg_to = a.causal ? min(nk, max(0, last + shift + 1)) : nk;
   const int wg_from = a.window > 0 ? min(wg_to, max(0, row0 + shift - a.window + 1)) / KT * KT : 0;
   const int tiles = (wg_to - wg_from + KT - 1) / KT;
-  // keys outside these may be hidden from a row of this wave, of the workgroup
+  // keys outside these may be hidden from a row of this wave
   const int first_row = row0 + wave * 32;
   const int all_to = first_row + 32 > nq ? 0 : a.causal ? min(nk, max(0, first_row + shift + 1)) : nk;
   const int all_from = a.window > 0 ? max(0, first_row + 31 + shift - a.window + 1) : 0;
-  const int wg_all_to = row0 + QROWS > nq ? 0 : a.causal ? min(nk, max(0, row0 + shift + 1)) : nk;
-  const int wg_all_from = a.window > 0 ? max(0, row0 + QROWS - 1 + shift - a.window + 1) : 0;
+  // keys outside these are hidden from all rows of the wave
+  const int any_to = a.causal ? min(nk, max(0, first_row + 32 + shift)) : nk;
+  const int any_from = a.window > 0 ? max(0, first_row + shift - a.window + 1) : 0;
 
   // A negative scale goes into Q's signs: what is left is not negative.
   u32x4 q[NS];
@@ -126,83 +144,53 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs p) {
   // not 0, so that a hidden key's minus infinity stays one: scores up to 2^80 then count as 0
   const float to_log2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 0x1p-100f);
 
-  // A thread's share of a tile: chunks of K by rows; of V eight dimensions of
-  // four keys.  Rows past the sequence's end read its last row.
-  constexpr int KL = KT * NC / 256;
-  constexpr int VT = D / 8;  // threads across the dimensions
+  // A thread's share of a tile: chunks of 16 bytes, by rows.  LDS chunk c of a
+  // row holds the row's chunk c ^ f(row): f is the row's number for K; for V a
+  // multiple of four that differs where rows that are read together would meet.
+  constexpr int KL = KT * NC / THREADS;
+  constexpr int ROWS = THREADS / NC;  // rows of one chunk a thread: f repeats after them
   const uint16_t* kbase = (const uint16_t*)a.k + kk0 * a.k_strides.row + kh * a.k_strides.head;
   const uint16_t* vbase = (const uint16_t*)a.v + kk0 * a.v_strides.row + kh * a.v_strides.head;
-  const int vd = tid % VT, vq = tid / VT;  // dimension block, key quad
-  u32x4 vreg[4];
-  // Whole tiles: one 32-bit offset a thread from addresses that are the
-  // workgroup's.  LDS chunk c of a row holds the row's chunk c ^ row.
-  const uint32_t koff = (uint32_t)((tid / NC) * a.k_strides.row + ((tid % NC) ^ (tid / NC & (NC - 1))) * 8) * 2;
-  const uint32_t voff = (uint32_t)(vq * 4 * a.v_strides.row + vd * 8) * 2;
-  auto load_k = [&](int tile, int buf) INLINE {
+  auto fk = [](int r) INLINE { return (D == 128 ? r : r >> 1) & (NC - 1); };
+  auto fv = [](int r) INLINE { return D == 128 ? (r & 3) * 4 : (r >> 1 & 1) * 4; };
+  const int crow = tid / NC, cc = tid % NC;
+  // whole tiles: one 32-bit offset a thread from addresses that are the workgroup's
+  const uint32_t koff = (uint32_t)(crow * a.k_strides.row + (cc ^ fk(crow)) * 8) * 2;
+  const uint32_t voff = (uint32_t)(crow * a.v_strides.row + (cc ^ fv(crow)) * 8) * 2;
+  auto load_rows = [&](const uint16_t* base, int64_t stride, uint32_t off, int swap, char* dst, int tile) INLINE {
     const int k0 = wg_from + tile * KT;
-    char* dst = s_k + buf * KBYTES + wave * WAVE * 16;
+    dst += wave * WAVE * 16;
     if (VEC && k0 + KT <= nk) {
-      const char* src = (const char*)(kbase + (int64_t)k0 * a.k_strides.row);
+      const char* src = (const char*)(base + (int64_t)k0 * stride);
 #pragma unroll
-      for (int i = 0; i < KL; ++i) copy_to_lds(src + (int64_t)(i * (256 / NC)) * a.k_strides.row * 2 + koff, dst + i * 4096);
-    } else {
+      for (int i = 0; i < KL; ++i) copy_to_lds(src + (int64_t)(i * ROWS) * stride * 2 + off, dst + i * (THREADS * 16));
+    } else {  // rows past the sequence's end read its last row
       for (int i = 0; i < KL; ++i) {
-        const int r = tid / NC + i * (256 / NC);
-        const uint16_t* src = kbase + min(k0 + r, nk - 1) * a.k_strides.row + ((tid % NC) ^ (r & (NC - 1))) * 8;
-        *(u32x4*)(dst + i * 4096 + lane * 16) = VEC ? *(const u32x4*)src : load_elements(src);
+        const uint16_t* src = base + min(k0 + crow + i * ROWS, nk - 1) * stride + swap * 8;
+        *(u32x4*)(dst + i * (THREADS * 16) + lane * 16) = VEC ? *(const u32x4*)src : load_elements(src);
       }
     }
   };
-  auto load_v = [&](int tile) INLINE {
-    const int k0 = wg_from + tile * KT;
-    if (D < 128 && vq >= KT / 4) return;
-    if (VEC && k0 + KT <= nk) {
-      const char* src = (const char*)(vbase + (int64_t)k0 * a.v_strides.row);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) vreg[j] = *(const u32x4*)(src + (int64_t)j * a.v_strides.row * 2 + voff);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint16_t* src = vbase + min(k0 + vq * 4 + j, nk - 1) * a.v_strides.row + vd * 8;
-        vreg[j] = VEC ? *(const u32x4*)src : load_elements(src);
-      }
-    }
-  };
-  auto store_v = [&](int tile, int buf) INLINE {
-    if (D >= 128 || vq < KT / 4) {
-      const int k0 = wg_from + tile * KT;
-      if (k0 + KT > wg_all_to || k0 < wg_all_from) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t bad = not_finite2<TYPE>(vreg[j][i]);
-            vreg[j][i] &= ~bad;
-            any |= bad;
-          }
-        if (any) s_odd = 1;
-      }
-      // four keys of dimension 8 vd + e as 8 bytes: keys 8 hi + 4 g + (0..3) of 16 go to half hi of chunk 2 s + g
-      const int s16 = vq / 4, hi = vq / 2 % 2, gg = vq % 2;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-        const u32x2 w = {__builtin_amdgcn_perm(vreg[1][e / 2], vreg[0][e / 2], sel),
-                         __builtin_amdgcn_perm(vreg[3][e / 2], vreg[2][e / 2], sel)};
-        const int d = vd * 8 + e, ch = (2 * s16 + gg) ^ ((d ^ (d >> 3)) & 7);
-        *(u32x2*)(s_v + buf * KBYTES + d * (KT * 2) + ch * 16 + hi * 8) = w;
-      }
-    }
-  };
+  auto load_k = [&](int tile, char* to) INLINE { load_rows(kbase, a.k_strides.row, koff, cc ^ fk(crow), to, tile); };
+  auto load_v = [&](int tile, char* to) INLINE { load_rows(vbase, a.v_strides.row, voff, cc ^ fv(crow), to, tile); };
   // operands: step s of the keys of half h of a tile; dimension block d, step s of the keys of half h
-  auto read_k = [&](int buf, int h, int s) INLINE {
-    const int key = 32 * h + n;
-    return *(const u32x4*)(s_k + buf * KBYTES + key * (D * 2) + (((2 * s + g) ^ (key & (NC - 1))) * 16));
+  auto read_k = [&](const char* k, int h, int s) INLINE {
+    return *(const u32x4*)(k + (32 * h + n) * (D * 2) + (((2 * s + g) ^ fk(n)) * 16));
   };
-  auto read_v = [&](int buf, int h, int d, int s) INLINE {
-    const int dim = 32 * d + n;
-    return *(const u32x4*)(s_v + buf * KBYTES + dim * (KT * 2) + (((4 * h + 2 * s + g) ^ ((dim ^ (dim >> 3)) & 7)) * 16));
+  // Lane l of 16 reads four dimensions of key l / 4 of four; it receives
+  // dimension l of all four keys.
+  const int vrow = 4 * g + lane % 16 / 4, vcol = 2 * (lane / 16 % 2) + lane % 4 / 2;
+  auto read_v = [&](const char* v, int h, int d, int s) INLINE {
+    u32x4 r;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int key = 32 * h + 16 * s + 8 * i + vrow;
+      const char* at = v + key * (D * 2) + ((4 * d + vcol) ^ fv(vrow)) * 16 + lane % 2 * 8;
+      const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves*)at));
+      r[2 * i] = w[0];
+      r[2 * i + 1] = w[1];
+    }
+    return r;
   };
   f32x16 sc[2];
   u32x4 pb[4];
@@ -219,85 +207,170 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs p) {
     return s;
   };
 
-  if (tid == 0) s_odd = 0;
-  __syncthreads();
-  if (tiles > 0) {
-    load_k(0, 0);
-    load_v(0);
-    store_v(0, 0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    for (int t = 0, buf = 0; t < tiles; ++t, buf ^= 1) {
-      const bool more = t + 1 < tiles;
-      if (more) {
-        load_k(t + 1, buf ^ 1);
-        load_v(t + 1);
+  auto hidden = [&](int t) INLINE { return wg_from + t * KT >= any_to || wg_from + (t + 1) * KT <= any_from; };
+  auto masked = [&](int t) INLINE { return wg_from + (t + 1) * KT > all_to || wg_from + t * KT < all_from; };
+  auto scores = [&](const char* kc) INLINE {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      f32x16 zero;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) zero[i] = 0;
+      sc[h] = mfma32<TYPE>(read_k(kc, h, 0), q[0], zero);
+#pragma unroll
+      for (int s = 1; s < NS; ++s) sc[h] = mfma32<TYPE>(read_k(kc, h, s), q[s], sc[h]);
+    }
+    reads_ahead<2 * NS, 1, 0>();
+  };
+  auto softmax = [&](int t) INLINE {
+    if (masked(t)) {
+      const int k0 = wg_from + t * KT, lo = from - k0 - 4 * g, hi = to - k0 - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
+        sc[i / 16][i % 16] = c < hi && c >= lo ? sc[i / 16][i % 16] : -INFINITY;
       }
-      const int k0 = wg_from + t * KT;
+    }
+    float s = exponentials();
+    if (__ballot(!(s <= LARGE))) {
+      float top = sc[0][0];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        f32x16 zero;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) zero[i] = 0;
-        sc[h] = mfma32<TYPE>(read_k(buf, h, 0), q[0], zero);
-#pragma unroll
-        for (int s = 1; s < NS; ++s) sc[h] = mfma32<TYPE>(read_k(buf, h, s), q[s], sc[h]);
-      }
-      if (k0 + KT > all_to || k0 < all_from) {
-        const int lo = from - k0 - 4 * g, hi = to - k0 - 4 * g;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
-          sc[i / 16][i % 16] = c < hi && c >= lo ? sc[i / 16][i % 16] : -INFINITY;
-        }
-      }
-      float s = exponentials();
-      if (__ballot(!(s <= LARGE))) {
-        float top = sc[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(ref, top * to_log2), by = __builtin_amdgcn_exp2f(ref - next);
-        ref = next;
-        sum *= by;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= by;
-        s = exponentials();
-      }
-      sum += s;
+      for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float next = fmaxf(ref, top * to_log2), by = __builtin_amdgcn_exp2f(ref - next);
+      ref = next;
+      sum *= by;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[d] = mfma32<TYPE>(read_v(buf, k / 2, d, k % 2), pb[k], o[d]);
-      if (more) store_v(t + 1, buf ^ 1);
-      __builtin_amdgcn_s_waitcnt(0);
-      __syncthreads();
+        for (int i = 0; i < 16; ++i) o[d][i] *= by;
+      s = exponentials();
     }
-    if (s_odd) {
-      for (int key = wg_from; key < wg_to; ++key) {
-        const int k0 = key / KT * KT;
-        if (k0 + KT <= wg_all_to && k0 >= wg_all_from) continue;  // went through the product as they are
-        const uint16_t* src = vbase + key * a.v_strides.row;
+    sum += s;
+  };
+  auto product = [&](const char* vc) INLINE {
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint16_t w = src[32 * d + 8 * (i / 4) + 4 * g + i % 4];
-            if (not_finite2<TYPE>(w) & 0xffffu) {
-              float x, unused;
-              unpack2<TYPE>(w, x, unused);
-              if (key < to && key >= from) o[d][i] += x;
-            }
-          }
+      for (int k = 0; k < 4; ++k) o[d] = mfma32<TYPE>(read_v(vc, k / 2, d, k % 2), pb[k], o[d]);
+    reads_ahead<4 * DT, 2, 1>();
+  };
+  // The workgroup's waves meet; this wave's copies but the newest `keep` are done.
+  auto meet = [&](int keep) INLINE {
+    asm volatile("" ::: "memory");
+    if (keep == 0) __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt, lgkmcnt 0
+    else if (keep == KL) __builtin_amdgcn_s_waitcnt(0x0070 | KL);
+    else __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  if (tiles > 0) {
+    if constexpr (WAVES == 4) {
+      load_k(0, s_k);
+      load_v(0, s_v);
+      if (tiles > 1) load_k(1, s_k + KBYTES);
+      meet(tiles > 1 ? KL : 0);
+      // Tile t, from kc and vc, while later tiles are copied to kn and vn: the
+      // pointers' restrict is what lets reads pass copies still under way.
+      auto work = [&](int t, const char* __restrict kc, const char* __restrict vc, char* __restrict kn,
+                      char* __restrict vn) INLINE {
+        if (t + 1 < tiles) load_v(t + 1, vn);
+        if (t + 2 < tiles) load_k(t + 2, kn);
+        if (!hidden(t)) {
+          scores(kc);
+          softmax(t);
+          product(vc);
+        }
+      };
+      int kb0 = 0, kb1 = 1, kb2 = 2;  // K's buffers of tiles t, t + 1, t + 2
+      for (int t = 0; t < tiles; ++t) {
+        work(t, s_k + kb0 * KBYTES, s_v + (t & 1) * KBYTES, s_k + kb2 * KBYTES, s_v + (~t & 1) * KBYTES);
+        meet(t + 2 < tiles ? KL : 0);
+        const int x = kb0;
+        kb0 = kb1;
+        kb1 = kb2;
+        kb2 = x;
       }
+    } else {
+      load_k(0, s_k);
+      load_v(0, s_v);
+      if (tiles > 1) load_k(1, s_k + KBYTES), load_v(1, s_v + KBYTES);
+      if (tiles > 2) load_k(2, s_k + 2 * KBYTES);
+      meet(0);
+      if (!hidden(0)) {
+        scores(s_k);
+        softmax(0);
+      }
+      // The first four waves (one a SIMD) and the last four take turns: while one
+      // half runs the products of a step, the other runs the exponentials.
+      const bool second = wave >= 4;
+      if (second) meet(-1);
+      int b0 = 0, b1 = 1, b2 = 2;  // buffers of tiles t, t + 1, t + 2
+      for (int t = 0; t < tiles; ++t) {
+        __builtin_amdgcn_s_setprio(1);
+        if (t + 1 < tiles && !hidden(t + 1)) scores(s_k + b1 * KBYTES);
+        if (!hidden(t)) product(s_v + b0 * KBYTES);
+        __builtin_amdgcn_s_setprio(0);
+        meet(-1);
+        if (t + 3 < tiles) load_k(t + 3, s_k + b0 * KBYTES);
+        if (t + 2 < tiles) load_v(t + 2, s_v + b2 * KBYTES);
+        if (t + 1 < tiles && !hidden(t + 1)) softmax(t + 1);
+        meet(0);
+        const int x = b0;
+        b0 = b1;
+        b1 = b2;
+        b2 = x;
+      }
+      if (!second) meet(-1);
     }
   }
 
   sum += __shfl_xor(sum, 32);
+  float check = sum - sum;  // 0, or NaN if a sum is not finite
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) check += o[d][i] - o[d][i];
+  if (__ballot(!(check == 0))) {
+    // row by row, the wave's lanes across the dimensions
+    const uint16_t* qb = (const uint16_t*)a.q + q0 * a.q_strides.row + qh * a.q_strides.head;
+    const int rows = min(32, nq - first_row);
+    for (int r = 0; r < rows; ++r) {
+      const int lo = __shfl(from, r), hi = __shfl(to, r);
+      float qv[D / WAVE], acc[D / WAVE], top = NO_KEY, den = 0, unused;
+#pragma unroll
+      for (int d = 0; d < D / WAVE; ++d) {
+        unpack2<TYPE>(qb[(first_row + r) * a.q_strides.row + d * WAVE + lane], qv[d], unused);
+        acc[d] = 0;
+      }
+      for (int key = lo; key < hi; ++key) {
+        float x = 0, v[D / WAVE];
+#pragma unroll
+        for (int d = 0; d < D / WAVE; ++d) {
+          float k;
+          unpack2<TYPE>(kbase[key * a.k_strides.row + d * WAVE + lane], k, unused);
+          unpack2<TYPE>(vbase[key * a.v_strides.row + d * WAVE + lane], v[d], unused);
+          x += qv[d] * k;
+        }
+#pragma unroll
+        for (int m = 1; m < WAVE; m *= 2) x += __shfl_xor(x, m);
+        x *= a.scale * 1.44269504088896340736f;
+        const float next = fmaxf(top, x), by = __builtin_amdgcn_exp2f(top - next), e = __builtin_amdgcn_exp2f(x - next);
+        top = next;
+        den = den * by + e;
+#pragma unroll
+        for (int d = 0; d < D / WAVE; ++d) acc[d] = acc[d] * by + e * v[d];
+      }
+      const int64_t at = (q0 + first_row + r) * a.q_heads + qh;
+#pragma unroll
+      for (int d = 0; d < D / WAVE; ++d)
+        ((uint16_t*)a.out)[at * D + d * WAVE + lane] = (uint16_t)pack2<TYPE>(den == 0 ? 0.0f : acc[d] / den, 0.0f);
+      if (a.lse && lane == 0)
+        a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+    }
+    return;
+  }
   if (row >= nq) return;
-  const float inv = sum > 0 ? 1.0f / sum : sum == 0 ? 0.0f : sum;  // no key seen: 0; NaN stays
+  const float inv = sum > 0 ? 1.0f / sum : 0.0f;  // no key seen: 0
   const int64_t at = (q0 + row) * a.q_heads + qh;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -310,17 +383,21 @@ __global__ __launch_bounds__(256, 2) void k_prompt(PromptArgs p) {
   if (a.lse && g == 0) a.lse[at] = sum == 0 ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
-template <int TYPE, int D>
+template <int TYPE, int D, int WAVES>
 static int prompt_launch(PromptArgs& p, bool vec) {
+  p.levels = (p.a.max_q + 32 * WAVES - 1) / (32 * WAVES);
   // XCDs that share a key head: only where key heads and XCDs divide evenly
   const int G = p.a.kv_heads;
   p.spread = G >= 8 ? (G % 8 == 0 ? 1 : 0) : (8 % G == 0 ? 8 / G : 0);
   int64_t blocks = (int64_t)p.levels * p.a.n_seqs * p.a.q_heads;
   if (p.spread) blocks = (blocks / (G < 8 ? G : 8) + p.spread - 1) / p.spread * 8;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
-  return launch(vec ? k_prompt<TYPE, D, true> : k_prompt<TYPE, D, false>, dim3((unsigned)blocks), dim3(256), 0,
-                p.a.hip_stream, p);
+  return launch(vec ? k_prompt<TYPE, D, WAVES, true> : k_prompt<TYPE, D, WAVES, false>, dim3((unsigned)blocks),
+                dim3(WAVES * WAVE), 0, p.a.hip_stream, p);
 }
+#ifndef PW
+#define PW 8
+#endif
 
 }  // namespace hop
 
@@ -337,10 +414,10 @@ extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
       (a.n_k && (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2))))
     return HERSCHEL_EINVAL;
   if (a.n_q == 0 || a.max_q == 0) return HERSCHEL_OK;
-  PromptArgs p{a, a.q_heads / a.kv_heads, (a.max_q + QROWS - 1) / QROWS, 0};
+  PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0};
   // 16-byte loads, and a tile's rows within 31 bits of bytes
   const bool vec = a.k_strides.row < (1 << 23) && a.v_strides.row < (1 << 23) && chunks_aligned(a.q, a.q_strides) && chunks_aligned(a.k, a.k_strides) && chunks_aligned(a.v, a.v_strides);
   const bool bf = a.type == HERSCHEL_BF16;
-  if (a.head_dim == 64) return bf ? prompt_launch<HERSCHEL_BF16, 64>(p, vec) : prompt_launch<HERSCHEL_F16, 64>(p, vec);
-  return bf ? prompt_launch<HERSCHEL_BF16, 128>(p, vec) : prompt_launch<HERSCHEL_F16, 128>(p, vec);
+  if (a.head_dim == 64) return bf ? prompt_launch<HERSCHEL_BF16, 64, PW>(p, vec) : prompt_launch<HERSCHEL_F16, 64, PW>(p, vec);
+  return bf ? prompt_launch<HERSCHEL_BF16, 128, PW>(p, vec) : prompt_launch<HERSCHEL_F16, 128, PW>(p, vec);
 }
