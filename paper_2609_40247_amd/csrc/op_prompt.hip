@@ -8,9 +8,11 @@
 //    only, so a row's sum and scaling factor are the lane's own, and the scores
 //    leave the first product in the lanes where the second wants them if it takes
 //    its keys in the order 8 a + 4 g + i (g = lane / 32).  P never moves.
-//  - A wave has 32 rows and two waves share a SIMD, of different workgroups: one
-//    wave alone issues a VALU instruction every 6 cycles, two every 3, and the
-//    exponentials of one run beside the products of the other.
+//  - A wave has 32 rows and two waves share a SIMD: one wave alone issues a VALU
+//    instruction every 6 cycles, two every 3, and the exponentials of one run
+//    beside the products of the other.  Eight waves in one workgroup take turns,
+//    half of them at the products while the other half is at the exponentials;
+//    with four, two workgroups of a CU drift apart by themselves.
 //  - Keys and values go to LDS by rows without passing registers, the next tile
 //    of values and the next two of keys while this one is worked on.  The chunks
 //    of a row are permuted by the row's number, differently for K and V, which
@@ -395,9 +397,20 @@ static int prompt_launch(PromptArgs& p, bool vec) {
   return launch(vec ? k_prompt<TYPE, D, WAVES, true> : k_prompt<TYPE, D, WAVES, false>, dim3((unsigned)blocks),
                 dim3(WAVES * WAVE), 0, p.a.hip_stream, p);
 }
-#ifndef PW
-#define PW 8
-#endif
+
+// Eight waves (256 rows) or four (128).  Eight in turns are faster where there
+// is enough for every CU twice over: 4096 rows of 32 heads of 128 145 us against
+// 156, 8192 983 against 1080; below, what counts is more and smaller workgroups:
+// 512 rows 23 against 18 us, 8 heads of 4096 95 against 83.  With heads of 64
+// the exponentials take longer than the products and turns lose (4096 rows
+// twice: 186 against 175 us).
+template <int TYPE>
+static int prompt_size(PromptArgs& p, bool vec) {
+  if (p.a.head_dim == 64) return prompt_launch<TYPE, 64, 4>(p, vec);
+  const int64_t rows = p.a.n_q / p.a.n_seqs;
+  if (rows >= 1024 && rows / 256 * p.a.n_seqs * p.a.q_heads >= 512) return prompt_launch<TYPE, 128, 8>(p, vec);
+  return prompt_launch<TYPE, 128, 4>(p, vec);
+}
 
 }  // namespace hop
 
@@ -417,7 +430,5 @@ extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
   PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0};
   // 16-byte loads, and a tile's rows within 31 bits of bytes
   const bool vec = a.k_strides.row < (1 << 23) && a.v_strides.row < (1 << 23) && chunks_aligned(a.q, a.q_strides) && chunks_aligned(a.k, a.k_strides) && chunks_aligned(a.v, a.v_strides);
-  const bool bf = a.type == HERSCHEL_BF16;
-  if (a.head_dim == 64) return bf ? prompt_launch<HERSCHEL_BF16, 64, PW>(p, vec) : prompt_launch<HERSCHEL_F16, 64, PW>(p, vec);
-  return bf ? prompt_launch<HERSCHEL_BF16, 128, PW>(p, vec) : prompt_launch<HERSCHEL_F16, 128, PW>(p, vec);
+  return a.type == HERSCHEL_BF16 ? prompt_size<HERSCHEL_BF16>(p, vec) : prompt_size<HERSCHEL_F16>(p, vec);
 }

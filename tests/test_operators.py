@@ -496,6 +496,46 @@ def test_attn_prompt_hidden_values_have_no_effect(D, dtype):
     run_prompt([40], [150], 2, 1, D, dtype, True, 0, scale=-0.1)
 
 
+LONG_CASES = [  # queries, keys, heads, kv heads, causal, window, values that are not finite
+    ([1500, 1029], None, 64, 8, True, 0, False),
+    ([1024, 1300], [2000, 1300], 64, 4, True, 700, False),
+    ([1100, 1100], [1100, 900], 64, 64, True, 0, True),
+    ([1030, 1026], [1030, 1700], 64, 16, False, 0, False),
+    ([1030, 1026], [1200, 70], 65, 5, False, 90, True),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("case", LONG_CASES, ids=str)
+def test_attn_prompt_long(case, dtype):
+    """Enough rows and heads for the larger workgroups: chosen rows of chosen heads against 64 bits."""
+    nq, nk, hq, hk, causal, window, odd = case
+    nk, D = nk or nq, 128
+    q, k, v = (rand(sum(n), h, D, seed=11 + i, dtype=dtype) for i, (n, h) in enumerate(((nq, hq), (nk, hk), (nk, hk))))
+    if odd:
+        v[700, 0, 3], v[701, 0, 4], k[705, hk - 1] = math.inf, math.nan, math.nan
+    cu = [torch.tensor([0] + list(n)).cumsum(0).int().to(DEV) for n in (nq, nk)]
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = O.attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), *cu, max_q=max(nq), causal=causal, window=window,
+                             return_lse=True, status=status)
+    assert status.item() == 0
+    out, lse = out.cpu(), lse.cpu()
+    heads = sorted({0, hq // hk - 1, hq // 2, hq - 1})
+    at_q = at_k = 0
+    for n, m in zip(nq, nk):
+        for i in sorted({0, 1, 31, 32, 63, 255, 256, 511, 700, 701, 705, n - 65, n - 2, n - 1}):
+            hi = max(0, min(m, i + m - n + 1)) if causal else m  # as the last row of a shorter sequence
+            lo = max(0, i + m - n - window + 1) if window else 0
+            for h in heads:
+                g = h * hk // hq
+                ref = exact_attention(q[at_q + i:at_q + i + 1, h:h + 1], k[at_k + lo:at_k + max(lo, hi), g:g + 1],
+                                      v[at_k + lo:at_k + max(lo, hi), g:g + 1], D ** -0.5, False, 0)
+                check_attention(out[at_q + i:at_q + i + 1, h:h + 1], lse[at_q + i:at_q + i + 1, h:h + 1], ref, dtype,
+                                U[dtype], m, D)
+        at_q, at_k = at_q + n, at_k + m
+
+
 @gpu
 def test_attn_prompt_faults():
     q = rand(40, 2, 64).to(DEV)
