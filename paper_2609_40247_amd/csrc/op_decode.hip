@@ -21,17 +21,23 @@
 //    share of the line, found from the lengths on the device.  Where a share ends
 //    inside a sequence's head the parts are joined by a second small kernel.
 //
-// The reference of a row's exponentials is its maximum when last looked at: a
-// score may exceed it by 2^8 before the accumulators are scaled anew, which is
-// exact up to rounding and is rarely needed after the first tiles.
+//  - The next step's rows are loaded before this one is worked on, and the page
+//    ids of the one after: a wave has 16 KB (8 with codes) under way at any time.
+//
+// The reference of a row's exponentials moves only when a step's sum shows that
+// one of them is large; no maximum is computed otherwise.  Rows of keys beyond
+// the sequence's end, or before all windows, are never read: a hidden key of a
+// step stands at a seen one's row, with the exponential 0.
 #include "ops.hpp"
 
 namespace hop {
 
+#define INLINE __attribute__((always_inline))
+
 constexpr int TILE = 128;         // keys of a workgroup's step: 32 a wave
-constexpr int DECODE_WGS = 768;   // shares of the line: three workgroups a CU
+constexpr int DECODE_WGS = 512;   // shares of the line: two workgroups a CU
 constexpr float FAR_BELOW = -3.0e38f;
-constexpr float LAZY = 8.0f;
+constexpr float LARGE_SUM = 4096.0f;  // half's largest value is 65504
 
 struct DecodeArgs {
   herschel_decode_args a;
@@ -84,13 +90,18 @@ __device__ __forceinline__ void scan_line(const DecodeArgs& p, int* s_pre, int* 
   __syncthreads();
 }
 
+// Factor of sums whose reference moves up; never 0, so that an infinite sum stays one.
+__device__ __forceinline__ float shrink(float from, float to) {
+  return fmaxf(__builtin_amdgcn_exp2f(from - to), 0x1p-126f);
+}
+
 // Share w of a line of U tiles in G shares: [w U / G, (w + 1) U / G).
 __device__ __forceinline__ int64_t share_start(int64_t w, int64_t U, int64_t G) { return w * U / G; }
 // The share that holds tile x (G <= U, so no share is empty).
 __device__ __forceinline__ int64_t share_of(int64_t x, int64_t U, int64_t G) { return ((x + 1) * G - 1) / U; }
 
 template <int TYPE, int KIND, int D, int RB>
-__global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
+__global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
   // With codes the second product runs in bf16, whose range holds exponential
   // times scale for any scale; for half inputs it runs twice, on the rounded
   // value and on what the rounding left, so that the result keeps half's precision.
@@ -99,17 +110,22 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
   constexpr int NS = D / 32;       // steps of the first product
   constexpr int ND = D / 16;       // blocks of dimensions of the second; dimensions of a lane's chunk
   constexpr int CB = code_bytes(KIND);
+  // two steps' rows fit in registers beside the sums, but for 32 rows of 16-bit heads of 128
+  constexpr bool AHEAD = quantised(KIND) || D == 64 || RB == 1;
+  constexpr int VW = ND / 2 * CB / 2;  // words of a lane's chunk of V
   extern __shared__ char smem[];
   int* s_pre = (int*)smem;
   float* s_o = (float*)(smem + ((p.a.n_seqs + 1 + 3) & ~3) * 4);  // [4][16][D + 2]
   __shared__ int s_wave[4];
 
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE, m = lane % 16, g = lane / 16;
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), m = lane % 16, g = lane / 16;
   scan_line(p, s_pre, s_wave, blockIdx.x == 0);
   const int64_t U = (int64_t)s_pre[p.a.n_seqs] * p.units, G = U < gridDim.x ? U : gridDim.x;
   if (blockIdx.x >= G) return;
   const int64_t begin = share_start(blockIdx.x, U, G), end = share_start(blockIdx.x + 1, U, G);
-  const float to_log2 = p.a.scale * 1.44269504088896340736f;
+  // a negative scale goes into Q's signs
+  const float to_log2 = fabsf(p.a.scale) * 1.44269504088896340736f;
+  const uint32_t sign = p.a.scale < 0 ? 0x80008000u : 0u;
 
   for (int64_t pos = begin; pos < end;) {
     // the sequence, unit and tile at this place of the line
@@ -144,7 +160,7 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const int d = CB == 2 ? 32 * s + 8 * g : 64 * (s / 2) + 16 * g + 8 * (s & 1);
-        q[rb][s] = ((uintptr_t)src & 15) == 0 ? *(const u32x4*)(src + d) : load_elements(src + d);
+        q[rb][s] = (((uintptr_t)src & 15) == 0 ? *(const u32x4*)(src + d) : load_elements(src + d)) ^ sign;
       }
     }
     f32x4 o[RB][ND];
@@ -157,54 +173,63 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
       for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
     }
     const int key_begin = (first_tile(p, len) + tile) * TILE, key_end = min(len, key_begin + n_tiles * TILE);
-    // keys that every row sees need no mask
+    // keys that every row sees need no mask; those that some row sees are read
     const int all_to = len - p.a.new_tokens + 1, all_from = p.a.window > 0 ? len - p.a.window : 0;
+    const int any_from = max(0, p.a.window > 0 ? len - p.a.new_tokens - p.a.window + 1 : 0);
 
-    for (int k0 = key_begin + wave * 32; k0 < key_end; k0 += TILE) {
-      // two runs of 16 keys, each within a page; a run past the end reads page 0 unseen
-      int64_t run[2];
-      bool live[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int k = k0 + 16 * t;
-        int page = k < len ? table[k >> p.page_shift] : 0;
-        live[t] = k < len && page >= 0 && page < p.c.n_pages;
-        if (k < len && !live[t] && lane == 0) flag(p.a.status, HERSCHEL_OP_BAD_PAGE);
-        if (!live[t]) page = 0;
-        run[t] = (((int64_t)page * p.c.n_heads + head) << p.page_shift) + (live[t] ? k & (p.c.page_size - 1) : 0);
-      }
-      // loads: keys, then values, then scales
-      u32x4 kf[2][CB == 2 ? NS : NS / 2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const char* kp = (const char*)p.c.k + (run[t] + m) * (D * CB) + 16 * g;
-#pragma unroll
-        for (int s = 0; s < (CB == 2 ? NS : NS / 2); ++s) kf[t][s] = *(const u32x4*)(kp + 64 * s);
-      }
-      uint32_t vf[8][ND / 2 * CB / 2];  // eight keys, ND dimensions each
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const char* vp = (const char*)p.c.v + (run[j / 4] + 4 * g + j % 4) * (D * CB) + m * (ND * CB);
-        constexpr int W = ND / 2 * CB / 2;
-        if constexpr (W == 4) {
-          const u32x4 x = *(const u32x4*)vp;
-          vf[j][0] = x[0], vf[j][1] = x[1], vf[j][2] = x[2], vf[j][3] = x[3];
-        } else if constexpr (W == 2) {
-          const u32x2 x = *(const u32x2*)vp;
-          vf[j][0] = x[0], vf[j][1] = x[1];
-        } else {
-          vf[j][0] = *(const uint32_t*)vp;
-        }
-      }
+    struct Step {
+      u32x4 k[2][CB == 2 ? NS : NS / 2];
+      uint32_t v[8][VW];  // eight keys, ND dimensions each
       f32x4 ks[2], vs[2];
-      if constexpr (quantised(KIND)) {
+      bool live[2];
+    };
+    // page ids of the two runs of 16 keys of a step, each within a page
+    auto find = [&](int k0, int (&page)[2]) INLINE {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          ks[t] = *(const f32x4*)(p.c.k_scale + run[t] + 4 * g);
-          vs[t] = *(const f32x4*)(p.c.v_scale + run[t] + 4 * g);
+      for (int t = 0; t < 2; ++t) page[t] = table[min(max(k0 + 16 * t, any_from), len - 1) >> p.page_shift];
+    };
+    auto load = [&](Step& s, int k0, const int (&page)[2]) INLINE {
+      const bool inside = k0 >= any_from && k0 + 32 <= len;
+      const int in_page = p.c.page_size - 1;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s.live[t] = page[t] >= 0 && page[t] < p.c.n_pages;
+        if (!s.live[t] && lane == 0) flag(p.a.status, HERSCHEL_OP_BAD_PAGE);
+        const int64_t base = ((int64_t)(s.live[t] ? page[t] : 0) * p.c.n_heads + head) << p.page_shift;
+        const int k = k0 + 16 * t;
+        auto row = [&](int key) INLINE { return (inside ? key : min(max(key, any_from), len - 1)) & in_page; };
+        const char* kp = (const char*)p.c.k + base * (D * CB) + (uint32_t)(row(k + m) * (D * CB) + 16 * g);
+#pragma unroll
+        for (int i = 0; i < (CB == 2 ? NS : NS / 2); ++i) s.k[t][i] = *(const u32x4*)(kp + 64 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const char* vp = (const char*)p.c.v + base * (D * CB) + (uint32_t)(row(k + 4 * g + j) * (D * CB) + m * (ND * CB));
+          uint32_t* to = s.v[4 * t + j];
+          if constexpr (VW == 4) {
+            const u32x4 x = *(const u32x4*)vp;
+            to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
+          } else if constexpr (VW == 2) {
+            const u32x2 x = *(const u32x2*)vp;
+            to[0] = x[0], to[1] = x[1];
+          } else {
+            to[0] = *(const uint32_t*)vp;
+          }
+        }
+        if constexpr (quantised(KIND)) {
+          if (inside) {
+            s.ks[t] = *(const f32x4*)(p.c.k_scale + base + ((k & in_page) + 4 * g));
+            s.vs[t] = *(const f32x4*)(p.c.v_scale + base + ((k & in_page) + 4 * g));
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              s.ks[t][j] = p.c.k_scale[base + row(k + 4 * g + j)];
+              s.vs[t][j] = p.c.v_scale[base + row(k + 4 * g + j)];
+            }
+          }
         }
       }
-
+    };
+    auto work = [&](Step& s, int k0) INLINE {
       // S^T = K Q^T
       f32x4 sc[RB][2];
 #pragma unroll
@@ -214,139 +239,173 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
+        for (int i = 0; i < NS; ++i) {
           u32x4 ka;
           if constexpr (!quantised(KIND)) {
-            ka = kf[t][s];
+            ka = s.k[t][i];
           } else {
-            const uint32_t w0 = kf[t][s / 2][2 * (s & 1)], w1 = kf[t][s / 2][2 * (s & 1) + 1];
+            const uint32_t w0 = s.k[t][i / 2][2 * (i & 1)], w1 = s.k[t][i / 2][2 * (i & 1) + 1];
             ka = u32x4{decode2<KIND, TYPE, false>(w0), decode2<KIND, TYPE, true>(w0), decode2<KIND, TYPE, false>(w1),
                        decode2<KIND, TYPE, true>(w1)};
           }
 #pragma unroll
-          for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16<TYPE>(ka, q[rb][s], sc[rb][t]);
+          for (int rb = 0; rb < RB; ++rb) sc[rb][t] = mfma16<TYPE>(ka, q[rb][i], sc[rb][t]);
         }
       }
-      // V^T: pairs of keys of one dimension
-      u32x4 vt[ND];
+      const bool edge = k0 + 32 > all_to || k0 < all_from || !s.live[0] || !s.live[1];
+      float f[8];  // of the scores: to powers of two, times the key's scale
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {  // keys 2 j, 2 j + 1
-#pragma unroll
-        for (int d = 0; d < ND / 2; ++d) {
-          uint32_t x, y;
-          if constexpr (!quantised(KIND)) {
-            x = vf[2 * j][d];
-            y = vf[2 * j + 1][d];
-          } else if (d & 1) {
-            x = decode2<KIND, PV, true>(vf[2 * j][d / 2]);
-            y = decode2<KIND, PV, true>(vf[2 * j + 1][d / 2]);
-          } else {
-            x = decode2<KIND, PV, false>(vf[2 * j][d / 2]);
-            y = decode2<KIND, PV, false>(vf[2 * j + 1][d / 2]);
-          }
-          vt[2 * d][j] = __builtin_amdgcn_perm(y, x, 0x05040100);
-          vt[2 * d + 1][j] = __builtin_amdgcn_perm(y, x, 0x07060302);
-        }
-      }
-      const bool edge = k0 + 32 > all_to || k0 < all_from || !live[0] || !live[1];
+      for (int i = 0; i < 8; ++i) f[i] = quantised(KIND) ? to_log2 * s.ks[i / 4][i % 4] : to_log2;
+      u32x4 pb[RB], pl[RB];
+      uint32_t seen[RB];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        float x[8];
-        uint32_t seen = 0xff;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          float f = sc[rb][i / 4][i % 4] * to_log2;
-          if constexpr (quantised(KIND)) f *= ks[i / 4][i % 4];
-          x[i] = f;
-        }
+        seen[rb] = 0xff;
         if (edge) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int key = k0 + 16 * (i / 4) + 4 * g + i % 4;
-            if (!(live[i / 4] && key < seen_to[rb] && key >= seen_from[rb])) {
-              x[i] = -INFINITY;
-              seen &= ~(1u << i);
-            }
+            if (!(s.live[i / 4] && key < seen_to[rb] && key >= seen_from[rb])) seen[rb] &= ~(1u << i);
           }
         }
-        float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-        if (__ballot(top > ref[rb] + LAZY)) {
+        float e[8];
+        auto exponentials = [&]() INLINE {
+          float t = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[rb][i / 4][i % 4], f[i], -ref[rb]));
+            if (edge) e[i] = (seen[rb] >> i) & 1 ? e[i] : 0.0f;
+            t += e[i];
+          }
+          return t;
+        };
+        float t = exponentials();
+        if (__ballot(!(t <= LARGE_SUM))) {
+          float top = FAR_BELOW;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) top = fmaxf(top, (seen[rb] >> i) & 1 ? sc[rb][i / 4][i % 4] * f[i] : FAR_BELOW);
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float to = fmaxf(ref[rb], top), by = __builtin_amdgcn_exp2f(ref[rb] - to);
+          const float to = fmaxf(ref[rb], top), by = shrink(ref[rb], to);
           ref[rb] = to;
           sum[rb] *= by;
 #pragma unroll
           for (int n = 0; n < ND; ++n) o[rb][n] *= by;
+          t = exponentials();
         }
-        float e[8];
+        sum[rb] += t;
+        if constexpr (quantised(KIND)) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          e[i] = __builtin_amdgcn_exp2f(x[i] - ref[rb]);
-          sum[rb] += e[i];
-          if constexpr (quantised(KIND)) e[i] = (seen >> i) & 1 ? e[i] * vs[i / 4][i % 4] : 0.0f;
+          for (int i = 0; i < 8; ++i) {
+            e[i] *= s.vs[i / 4][i % 4];
+            if (edge) e[i] = (seen[rb] >> i) & 1 ? e[i] : 0.0f;
+          }
         }
-        u32x4 pb, pl;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          pb[i] = pack2<PV>(e[2 * i], e[2 * i + 1]);
+          pb[rb][i] = pack2<PV>(e[2 * i], e[2 * i + 1]);
           if constexpr (SPLIT) {
             float r0, r1;
-            unpack2<PV>(pb[i], r0, r1);
-            pl[i] = pack2<PV>(e[2 * i] - r0, e[2 * i + 1] - r1);
+            unpack2<PV>(pb[rb][i], r0, r1);
+            pl[rb][i] = pack2<PV>(e[2 * i] - r0, e[2 * i + 1] - r1);
           }
         }
-        if (!edge) {
+      }
+      // O^T += V^T P^T, two dimensions of a lane's chunk at a time: V^T has pairs of keys of one dimension
 #pragma unroll
-          for (int n = 0; n < ND; ++n) {
-            o[rb][n] = mfma16<PV>(vt[n], pb, o[rb][n]);
-            if constexpr (SPLIT) o[rb][n] = mfma16<PV>(vt[n], pl, o[rb][n]);
+      for (int d = 0; d < ND / 2; ++d) {
+        u32x4 vt[2];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {  // keys 2 j, 2 j + 1
+          uint32_t x, y;
+          if constexpr (!quantised(KIND)) {
+            x = s.v[2 * j][d];
+            y = s.v[2 * j + 1][d];
+          } else if (d & 1) {
+            x = decode2<KIND, PV, true>(s.v[2 * j][d / 2]);
+            y = decode2<KIND, PV, true>(s.v[2 * j + 1][d / 2]);
+          } else {
+            x = decode2<KIND, PV, false>(s.v[2 * j][d / 2]);
+            y = decode2<KIND, PV, false>(s.v[2 * j + 1][d / 2]);
           }
-        } else {
-          // a value that is not finite must reach the rows that see its key and
-          // no other: it is taken out of the product, and added where seen
+          vt[0][j] = __builtin_amdgcn_perm(y, x, 0x05040100);
+          vt[1][j] = __builtin_amdgcn_perm(y, x, 0x07060302);
+        }
+        // A value that is not finite must reach the rows that see its key and no
+        // other: where rows differ it is taken out of the product, and added.
+        if (KIND != HERSCHEL_INT8 && edge && p.a.new_tokens > 1) {
           constexpr uint32_t ONE = PV == HERSCHEL_BF16 ? 0x3f80u : 0x3c00u;
           constexpr uint32_t INF = PV == HERSCHEL_BF16 ? 0x7f80u : 0x7c00u;
-          u32x4 sees;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            sees[i] = ((seen >> (2 * i)) & 1 ? ONE : 0u) | ((seen >> (2 * i + 1)) & 1 ? ONE << 16 : 0u);
-#pragma unroll
-          for (int n = 0; n < ND; ++n) {
-            u32x4 bad, va;
+          for (int h = 0; h < 2; ++h) {
+            u32x4 up, down, rest;  // +infinity or NaN, -infinity or NaN, finite
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              bad[i] = not_finite2<PV>(vt[n][i]);
-              va[i] = vt[n][i] & ~bad[i];
-            }
-            o[rb][n] = mfma16<PV>(va, pb, o[rb][n]);
-            if constexpr (SPLIT) o[rb][n] = mfma16<PV>(va, pl, o[rb][n]);
-            if (__ballot((bad[0] | bad[1] | bad[2] | bad[3]) != 0)) {
-              u32x4 up, down;  // +infinity or NaN, -infinity or NaN
+              const uint32_t w = vt[h][i], bad = not_finite2<PV>(w);
+              up[i] = down[i] = 0;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const uint32_t w = vt[n][i];
-                uint32_t u = 0, d = 0;
-#pragma unroll
-                for (int h = 0; h < 32; h += 16) {
-                  const uint32_t z = (w >> h) & 0xffffu;
-                  if ((bad[i] >> h) & 1) {
-                    if (z != (INF | 0x8000u)) u |= ONE << h;
-                    if (z != INF) d |= ONE << h;
-                  }
+              for (int z = 0; z < 32; z += 16) {
+                const uint32_t x = (w >> z) & 0xffffu;
+                if ((bad >> z) & 1) {
+                  if (x != (INF | 0x8000u)) up[i] |= ONE << z;
+                  if (x != INF) down[i] |= ONE << z;
                 }
-                up[i] = u;
-                down[i] = d;
               }
-              const f32x4 nu = mfma16<PV>(up, sees, f32x4{0, 0, 0, 0}), nd = mfma16<PV>(down, sees, f32x4{0, 0, 0, 0});
+              rest[i] = w & ~bad;
+            }
+            vt[h] = rest;
+            if (__ballot((up[0] | up[1] | up[2] | up[3] | down[0] | down[1] | down[2] | down[3]) != 0)) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                if (nu[i] > 0) o[rb][n][i] += INFINITY;
-                if (nd[i] > 0) o[rb][n][i] -= INFINITY;
+              for (int rb = 0; rb < RB; ++rb) {
+                u32x4 sees;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                  sees[i] = ((seen[rb] >> (2 * i)) & 1 ? ONE : 0u) | ((seen[rb] >> (2 * i + 1)) & 1 ? ONE << 16 : 0u);
+                const f32x4 zero = {0, 0, 0, 0}, nu = mfma16<PV>(up, sees, zero), nd = mfma16<PV>(down, sees, zero);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  if (nu[i] > 0) o[rb][2 * d + h][i] += INFINITY;
+                  if (nd[i] > 0) o[rb][2 * d + h][i] -= INFINITY;
+                }
               }
             }
           }
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int rb = 0; rb < RB; ++rb) {
+            o[rb][2 * d + h] = mfma16<PV>(vt[h], pb[rb], o[rb][2 * d + h]);
+            if constexpr (SPLIT) o[rb][2 * d + h] = mfma16<PV>(vt[h], pl[rb], o[rb][2 * d + h]);
+          }
+      }
+    };
+    int k0 = key_begin + wave * 32;
+    if (k0 < key_end) {
+      Step a, b;
+      int page[2];
+      find(k0, page);
+      load(a, k0, page);
+      find(k0 + TILE, page);
+      for (; !AHEAD;) {
+        work(a, k0);
+        if ((k0 += TILE) >= key_end) break;
+        load(a, k0, page);
+        find(k0 + TILE, page);
+      }
+      for (; AHEAD;) {
+        if (k0 + TILE < key_end) {
+          load(b, k0 + TILE, page);
+          find(k0 + 2 * TILE, page);
+        }
+        work(a, k0);
+        if ((k0 += TILE) >= key_end) break;
+        if (k0 + TILE < key_end) {
+          load(a, k0 + TILE, page);
+          find(k0 + 2 * TILE, page);
+        }
+        work(b, k0);
+        if ((k0 += TILE) >= key_end) break;
       }
     }
 
@@ -380,7 +439,7 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
         for (int n = 0; n < ND; ++n) acc[n] = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const float by = __builtin_amdgcn_exp2f(all[w * WS + D] - top);
+          const float by = shrink(all[w * WS + D], top);
           den += all[w * WS + D + 1] * by;
 #pragma unroll
           for (int n = 0; n < ND; ++n) acc[n] += all[w * WS + d0 + n] * by;
@@ -409,45 +468,55 @@ __global__ __launch_bounds__(256) void k_decode(DecodeArgs p) {
 }
 
 // Joins the parts of each sequence's head that more than one share holds: a
-// workgroup per (sequence, unit), 16 lanes a row.
+// workgroup per row, 16 lanes across the dimensions, each sixteenth part to a
+// group of them, the groups through LDS.
 template <int TYPE, int D, int RB>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
+  constexpr int ND = D / 16;
   extern __shared__ char smem[];
   int* s_pre = (int*)smem;
   __shared__ int s_wave[4];
-  constexpr int ND = D / 16;
+  __shared__ float s_part[16][D + 2];
   scan_line(p, s_pre, s_wave, false);
-  const int b = blockIdx.x / p.units, unit = blockIdx.x % p.units, tiles = s_pre[b + 1] - s_pre[b];
+  const int r = blockIdx.x % p.rows, of = blockIdx.x / p.rows;
+  const int b = of / p.c.n_heads, head = of % p.c.n_heads, unit = head * p.row_blocks + r / (RB * 16);
+  const int tiles = s_pre[b + 1] - s_pre[b];
   const int64_t U = (int64_t)s_pre[p.a.n_seqs] * p.units, G = U < DECODE_WGS ? U : DECODE_WGS;
   const int64_t at0 = (int64_t)s_pre[b] * p.units + (int64_t)unit * tiles;
   const int64_t first = share_of(at0, U, G), last = share_of(at0 + tiles - 1, U, G);
   if (first == last) return;
-  const int head = unit / p.row_blocks, row0 = unit % p.row_blocks * (RB * 16);
-  const int d0 = threadIdx.x % 16 * ND;
-  for (int rr = threadIdx.x / 16; rr < RB * 16; rr += 16) {
-    const int r = row0 + rr;
-    if (r >= p.rows) continue;
-    float top = FAR_BELOW, den = 0, acc[ND];
+  const int lane = threadIdx.x % 16, group = threadIdx.x / 16;
+  float top = FAR_BELOW, den = 0, acc[ND];
 #pragma unroll
-    for (int n = 0; n < ND; ++n) acc[n] = 0;
-    for (int64_t w = first; w <= last; ++w) {
-      const int64_t slot = 2 * w + (w == first && share_start(w, U, G) != at0 ? 1 : 0);
-      const float* from = p.part + (slot * (RB * 16) + rr) * (D + 2);
-      const float t = from[D], to = fmaxf(top, t);
-      const float old = __builtin_amdgcn_exp2f(top - to), by = __builtin_amdgcn_exp2f(t - to);
-      den = den * old + from[D + 1] * by;
+  for (int n = 0; n < ND; ++n) acc[n] = 0;
+  auto add = [&](const float* from) INLINE {
+    const float t = from[D], to = fmaxf(top, t);
+    const float old = shrink(top, to), by = shrink(t, to);
+    den = den * old + from[D + 1] * by;
 #pragma unroll
-      for (int n = 0; n < ND; ++n) acc[n] = acc[n] * old + from[d0 + n] * by;
-      top = to;
-    }
-    const float inv = den > 0 ? 1.0f / den : den == 0 ? 0.0f : den;
-    const int64_t at = ((int64_t)b * p.a.new_tokens + r / p.group) * p.a.q_heads + head * p.group + r % p.group;
-    uint32_t* out = (uint32_t*)((uint16_t*)p.a.out + at * D + d0);
-#pragma unroll
-    for (int n = 0; n < ND; n += 2) out[n / 2] = pack2<TYPE>(acc[n] * inv, acc[n + 1] * inv);
-    if (p.a.lse && threadIdx.x % 16 == 0)
-      p.a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+    for (int n = 0; n < ND; ++n) acc[n] = acc[n] * old + from[lane * ND + n] * by;
+    top = to;
+  };
+  for (int64_t w = first + group; w <= last; w += 16) {
+    const int64_t slot = 2 * w + (w == first && share_start(w, U, G) != at0 ? 1 : 0);
+    add(p.part + (slot * (RB * 16) + r % (RB * 16)) * (D + 2));
   }
+#pragma unroll
+  for (int n = 0; n < ND; ++n) s_part[group][lane * ND + n] = acc[n];
+  if (lane == 0) {
+    s_part[group][D] = top;
+    s_part[group][D + 1] = den;
+  }
+  __syncthreads();
+  if (group) return;
+  for (int i = 1; i < 16 && i <= last - first; ++i) add(s_part[i]);
+  const float inv = den > 0 ? 1.0f / den : den == 0 ? 0.0f : den;
+  const int64_t at = ((int64_t)b * p.a.new_tokens + r / p.group) * p.a.q_heads + head * p.group + r % p.group;
+  uint32_t* out = (uint32_t*)((uint16_t*)p.a.out + at * D + lane * ND);
+#pragma unroll
+  for (int n = 0; n < ND; n += 2) out[n / 2] = pack2<TYPE>(acc[n] * inv, acc[n + 1] * inv);
+  if (p.a.lse && lane == 0)
+    p.a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
 }
 
 template <int TYPE, int KIND, int D, int RB>
@@ -456,7 +525,8 @@ static int decode_launch(DecodeArgs& p) {
   const int rc = launch(k_decode<TYPE, KIND, D, RB>, dim3(DECODE_WGS), dim3(256), pre + 4 * 16 * (D + 2) * 4,
                         p.a.hip_stream, p);
   if (rc != HERSCHEL_OK) return rc;
-  return launch(k_decode_join<TYPE, D, RB>, dim3((unsigned)(p.a.n_seqs * p.units)), dim3(256), pre, p.a.hip_stream, p);
+  return launch(k_decode_join<TYPE, D, RB>, dim3((unsigned)(p.a.n_seqs * p.c.n_heads * p.rows)), dim3(256), pre,
+                p.a.hip_stream, p);
 }
 
 template <int TYPE, int KIND>

@@ -356,7 +356,10 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
 #pragma unroll
         for (int m = 1; m < WAVE; m *= 2) x += __shfl_xor(x, m);
         x *= a.scale * 1.44269504088896340736f;
-        const float next = fmaxf(top, x), by = __builtin_amdgcn_exp2f(top - next), e = __builtin_amdgcn_exp2f(x - next);
+        // factors are never 0, so that an infinite value or sum stays one
+        const float next = fmaxf(top, x), by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
+        float e = __builtin_amdgcn_exp2f(x - next);
+        if (e == 0) e = 0x1p-126f;
         top = next;
         den = den * by + e;
 #pragma unroll
