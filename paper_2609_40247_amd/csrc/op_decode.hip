@@ -21,8 +21,10 @@
 //    share of the line, found from the lengths on the device.  Where a share ends
 //    inside a sequence's head the parts are joined by a second small kernel.
 //
-//  - The next step's rows are loaded before this one is worked on, and the page
-//    ids of the one after: a wave has 16 KB (8 with codes) under way at any time.
+//  - A step's 16 KB (8 with codes) a wave are asked for at once; the waits are
+//    filled by the other waves of the SIMD.  (Loading the next step's rows before
+//    this one is worked on costs registers, and with them waves: 105 us became
+//    110 for 32 requests of 4096 tokens in bf16, 92 became 102 for 64 in fp8.)
 //
 // The reference of a row's exponentials moves only when a step's sum shows that
 // one of them is large; no maximum is computed otherwise.  Rows of keys beyond
@@ -35,7 +37,11 @@ namespace hop {
 #define INLINE __attribute__((always_inline))
 
 constexpr int TILE = 128;         // keys of a workgroup's step: 32 a wave
-constexpr int DECODE_WGS = 512;   // shares of the line: two workgroups a CU
+// Shares of the line: as many workgroups as the CUs hold.  Three a CU with codes
+// and one row block (64 requests 92 us against 105 with two), two where
+// registers allow no more or the reads are as fast (bf16 102 and 104 us).
+constexpr int MAX_SHARES = 768;
+constexpr int shares_of_cu(int kind, int row_blocks) { return quantised(kind) && row_blocks == 1 ? 3 : 2; }
 constexpr float FAR_BELOW = -3.0e38f;
 constexpr float LARGE_SUM = 4096.0f;  // half's largest value is 65504
 
@@ -47,7 +53,8 @@ struct DecodeArgs {
   int rows;      // new tokens * group
   int units;     // key heads * row blocks
   int row_blocks;
-  float* part;   // [2 * DECODE_WGS][RB * 16][head_dim + 2]: sums, reference, sum of exponentials
+  int2* span;    // [n_seqs * units] first part and last share of a row block; first part -1: nothing to join
+  float* part;   // [2 * MAX_SHARES][RB * 16][head_dim + 2]: sums, reference, sum of exponentials
 };
 
 // The first tile of a sequence that the window reaches, and its tiles.
@@ -70,6 +77,20 @@ __device__ __forceinline__ int seq_tiles(const DecodeArgs& p, int len) {
 // s_pre[b] = tiles of sequences before b, for all b <= n_seqs; 256 threads.
 __device__ __forceinline__ void scan_line(const DecodeArgs& p, int* s_pre, int* s_wave, bool report) {
   const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+  if (p.a.n_seqs <= WAVE) {
+    if (wave == 0) {
+      int x = lane < p.a.n_seqs ? seq_tiles(p, seq_len(p, lane, report)) : 0;
+#pragma unroll
+      for (int o = 1; o < WAVE; o *= 2) {
+        const int y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane < p.a.n_seqs) s_pre[lane + 1] = x;
+      if (lane == 0) s_pre[0] = 0;
+    }
+    __syncthreads();
+    return;
+  }
   int carry = 0;
   for (int b0 = 0; b0 < p.a.n_seqs; b0 += 256) {
     const int b = b0 + threadIdx.x;
@@ -95,13 +116,17 @@ __device__ __forceinline__ float shrink(float from, float to) {
   return fmaxf(__builtin_amdgcn_exp2f(from - to), 0x1p-126f);
 }
 
+// a / b of numbers that are not negative: a 64-bit division takes a microsecond.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+  return ((uint64_t)(a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // Share w of a line of U tiles in G shares: [w U / G, (w + 1) U / G).
-__device__ __forceinline__ int64_t share_start(int64_t w, int64_t U, int64_t G) { return w * U / G; }
+__device__ __forceinline__ int64_t share_start(int64_t w, int64_t U, int64_t G) { return divide(w * U, G); }
 // The share that holds tile x (G <= U, so no share is empty).
-__device__ __forceinline__ int64_t share_of(int64_t x, int64_t U, int64_t G) { return ((x + 1) * G - 1) / U; }
+__device__ __forceinline__ int64_t share_of(int64_t x, int64_t U, int64_t G) { return divide((x + 1) * G - 1, U); }
 
 template <int TYPE, int KIND, int D, int RB>
-__global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
+__global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeArgs p) {
   // With codes the second product runs in bf16, whose range holds exponential
   // times scale for any scale; for half inputs it runs twice, on the rounded
   // value and on what the rounding left, so that the result keeps half's precision.
@@ -110,8 +135,6 @@ __global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
   constexpr int NS = D / 32;       // steps of the first product
   constexpr int ND = D / 16;       // blocks of dimensions of the second; dimensions of a lane's chunk
   constexpr int CB = code_bytes(KIND);
-  // two steps' rows fit in registers beside the sums, but for 32 rows of 16-bit heads of 128
-  constexpr bool AHEAD = quantised(KIND) || D == 64 || RB == 1;
   constexpr int VW = ND / 2 * CB / 2;  // words of a lane's chunk of V
   extern __shared__ char smem[];
   int* s_pre = (int*)smem;
@@ -120,7 +143,8 @@ __global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
 
   const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), m = lane % 16, g = lane / 16;
   scan_line(p, s_pre, s_wave, blockIdx.x == 0);
-  const int64_t U = (int64_t)s_pre[p.a.n_seqs] * p.units, G = U < gridDim.x ? U : gridDim.x;
+  auto uniform = [](int x) INLINE { return __builtin_amdgcn_readfirstlane(x); };  // what came through LDS
+  const int64_t U = (int64_t)uniform(s_pre[p.a.n_seqs]) * p.units, G = U < gridDim.x ? U : gridDim.x;
   if (blockIdx.x >= G) return;
   const int64_t begin = share_start(blockIdx.x, U, G), end = share_start(blockIdx.x + 1, U, G);
   // a negative scale goes into Q's signs
@@ -132,19 +156,21 @@ __global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
     int b = 0;
     for (int n = p.a.n_seqs; n > 1;) {
       const int half = n / 2;
-      if ((int64_t)s_pre[b + half] * p.units <= pos) {
+      if ((int64_t)uniform(s_pre[b + half]) * p.units <= pos) {
         b += half;
         n -= half;
       } else {
         n = half;
       }
     }
-    const int len = seq_len(p, b, false), tiles = s_pre[b + 1] - s_pre[b];
-    const int64_t rem = pos - (int64_t)s_pre[b] * p.units;
-    const int unit = (int)(rem / tiles), tile = (int)(rem % tiles);
+    const int before = uniform(s_pre[b]), tiles = uniform(s_pre[b + 1]) - before, len = uniform(seq_len(p, b, false));
+    const int64_t rem = pos - (int64_t)before * p.units;
+    const int unit = (int)divide(rem, tiles), tile = (int)(rem - (int64_t)unit * tiles);
     const int n_tiles = (int)min((int64_t)(tiles - tile), end - pos);
     const int head = unit / p.row_blocks, row0 = unit % p.row_blocks * (RB * 16);
-    const int32_t* table = p.a.block_table + b * p.a.table_stride;
+    // through the scalar cache: a page id is the whole wave's
+    typedef const __attribute__((address_space(4))) int32_t Table;
+    Table* table = (Table*)(uintptr_t)(p.a.block_table + b * p.a.table_stride);
 
     // Q: lane (r, g) of block rb holds row r, elements in the order of the keys' chunks;
     // lanes beyond the last row repeat the first one, unused
@@ -382,35 +408,21 @@ __global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
     };
     int k0 = key_begin + wave * 32;
     if (k0 < key_end) {
-      Step a, b;
+      Step s;
       int page[2];
       find(k0, page);
-      load(a, k0, page);
-      find(k0 + TILE, page);
-      for (; !AHEAD;) {
-        work(a, k0);
-        if ((k0 += TILE) >= key_end) break;
-        load(a, k0, page);
+      for (; k0 < key_end; k0 += TILE) {
+        load(s, k0, page);
         find(k0 + TILE, page);
-      }
-      for (; AHEAD;) {
-        if (k0 + TILE < key_end) {
-          load(b, k0 + TILE, page);
-          find(k0 + 2 * TILE, page);
-        }
-        work(a, k0);
-        if ((k0 += TILE) >= key_end) break;
-        if (k0 + TILE < key_end) {
-          load(a, k0 + TILE, page);
-          find(k0 + 2 * TILE, page);
-        }
-        work(b, k0);
-        if ((k0 += TILE) >= key_end) break;
+        work(s, k0);
       }
     }
 
     // The four waves' parts of these rows, joined through LDS block by block.
     const bool whole = tile == 0 && n_tiles == tiles;
+    if (tile == 0 && tid == 0)
+      p.span[(int64_t)b * p.units + unit] =
+          whole ? int2{-1, 0} : int2{2 * (int)blockIdx.x + (pos == begin ? 0 : 1), (int)share_of(pos + tiles - 1, U, G)};
     const int64_t slot = 2 * (int64_t)blockIdx.x + (pos == begin ? 0 : 1);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
@@ -473,18 +485,12 @@ __global__ __launch_bounds__(256, 2) void k_decode(DecodeArgs p) {
 template <int TYPE, int D, int RB>
 __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
   constexpr int ND = D / 16;
-  extern __shared__ char smem[];
-  int* s_pre = (int*)smem;
-  __shared__ int s_wave[4];
   __shared__ float s_part[16][D + 2];
-  scan_line(p, s_pre, s_wave, false);
   const int r = blockIdx.x % p.rows, of = blockIdx.x / p.rows;
   const int b = of / p.c.n_heads, head = of % p.c.n_heads, unit = head * p.row_blocks + r / (RB * 16);
-  const int tiles = s_pre[b + 1] - s_pre[b];
-  const int64_t U = (int64_t)s_pre[p.a.n_seqs] * p.units, G = U < DECODE_WGS ? U : DECODE_WGS;
-  const int64_t at0 = (int64_t)s_pre[b] * p.units + (int64_t)unit * tiles;
-  const int64_t first = share_of(at0, U, G), last = share_of(at0 + tiles - 1, U, G);
-  if (first == last) return;
+  const int2 span = p.span[(int64_t)b * p.units + unit];
+  if (span.x < 0) return;
+  const int first = span.x / 2, last = span.y;  // shares; a later share's part is its first
   const int lane = threadIdx.x % 16, group = threadIdx.x / 16;
   float top = FAR_BELOW, den = 0, acc[ND];
 #pragma unroll
@@ -497,8 +503,8 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
     for (int n = 0; n < ND; ++n) acc[n] = acc[n] * old + from[lane * ND + n] * by;
     top = to;
   };
-  for (int64_t w = first + group; w <= last; w += 16) {
-    const int64_t slot = 2 * w + (w == first && share_start(w, U, G) != at0 ? 1 : 0);
+  for (int w = first + group; w <= last; w += 16) {
+    const int64_t slot = w == first ? span.x : 2 * w;
     add(p.part + (slot * (RB * 16) + r % (RB * 16)) * (D + 2));
   }
 #pragma unroll
@@ -522,10 +528,10 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
 template <int TYPE, int KIND, int D, int RB>
 static int decode_launch(DecodeArgs& p) {
   const size_t pre = ((p.a.n_seqs + 1 + 3) & ~3) * 4;
-  const int rc = launch(k_decode<TYPE, KIND, D, RB>, dim3(DECODE_WGS), dim3(256), pre + 4 * 16 * (D + 2) * 4,
+  const int rc = launch(k_decode<TYPE, KIND, D, RB>, dim3(256 * shares_of_cu(KIND, RB)), dim3(256), pre + 4 * 16 * (D + 2) * 4,
                         p.a.hip_stream, p);
   if (rc != HERSCHEL_OK) return rc;
-  return launch(k_decode_join<TYPE, D, RB>, dim3((unsigned)(p.a.n_seqs * p.c.n_heads * p.rows)), dim3(256), pre,
+  return launch(k_decode_join<TYPE, D, RB>, dim3((unsigned)(p.a.n_seqs * p.c.n_heads * p.rows)), dim3(256), 0,
                 p.a.hip_stream, p);
 }
 
@@ -550,7 +556,9 @@ extern "C" int herschel_attn_decode_workspace(int32_t n_seqs, int32_t new_tokens
                                               const herschel_cache* cache, size_t* bytes) {
   using namespace hop;
   if (!bytes || !decode_sizes_ok(n_seqs, new_tokens, q_heads, cache)) return HERSCHEL_EINVAL;
-  *bytes = (size_t)2 * DECODE_WGS * decode_rows(new_tokens * (q_heads / cache->n_heads)) * (cache->head_dim + 2) * 4;
+  const int rows = new_tokens * (q_heads / cache->n_heads), block = decode_rows(rows);
+  *bytes = (size_t)2 * MAX_SHARES * block * (cache->head_dim + 2) * 4 +
+           (size_t)n_seqs * cache->n_heads * ((rows + block - 1) / block) * sizeof(int2);
   return HERSCHEL_OK;
 }
 
@@ -576,6 +584,7 @@ extern "C" int herschel_attn_decode(const herschel_decode_args* args, const hers
   p.row_blocks = (p.rows + block - 1) / block;
   p.units = cache->n_heads * p.row_blocks;
   p.part = (float*)a.workspace;
+  p.span = (int2*)(p.part + (size_t)2 * MAX_SHARES * block * (cache->head_dim + 2));
   const bool bf = a.type == HERSCHEL_BF16;
   switch (cache->kind) {
     case HERSCHEL_FP8:
