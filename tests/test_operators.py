@@ -893,3 +893,66 @@ def test_tensor_checks():
     for kw in (dict(batch=0), dict(heads=3), dict(new_tokens=0), dict(dtype=HF), dict(batch=5000)):
         with pytest.raises(ValueError):
             O.DecodeAttention(c, **{**dict(batch=1, heads=4), **kw})
+
+
+# ------------------------------------------------------------ the operators together
+@gpu
+@pytest.mark.parametrize("cache", ["bf16", "fp8", "int8"])
+def test_layer_prompt_and_steps_agree(cache):
+    """A token attended to in a decode step and the same token as a prompt's last: one computes from the cache what the
+    other computes from its rows; with a 16-bit cache both stay within their bounds of the 64-bit result, with codes
+    they differ by what the codes round away."""
+    from paper_2609_40247_amd import reference as R
+    lens, D, h, g = [40, 130, 1, 77], 64, 4, 2
+    total = [n + 1 for n in lens]
+    x = [rand(n, h + 2 * g, D, seed=90 + i) for i, n in enumerate(total)]
+    whole, parts = (R.AttentionLayer(h, g, D, len(lens), 200, 16, cache) for _ in range(2))
+    a = whole.prompt(torch.cat(x).to(DEV), total)
+    parts.prompt(torch.cat([t[:-1] for t in x]).to(DEV), lens)
+    b = parts.step(torch.stack([t[-1] for t in x]).to(DEV))
+    whole.cache.check(), parts.cache.check()
+    assert parts.lengths.tolist() == total
+    last = torch.tensor(total).cumsum(0) - 1
+    for i, n in enumerate(total):
+        k = exact_rope(x[i][:, h:h + g], whole.table.cpu()[:n], "half", D)[0].to(BF)
+        q = exact_rope(x[i][:, :h], whole.table.cpu()[:n], "half", D)[0].to(BF)
+        ref = exact_attention(q[-1:], k, x[i][:, h + g:], D ** -0.5, True, 0)
+        # the rotation's own rounding to bf16 may fall the other way in 32 bits: one more unit of each product
+        o, lse, A, S = ref
+        slack = 2 * 2.0 ** -8 * (A + S[..., None] * A)
+        assert ((a[last[i]].double().cpu() - o[0]).abs() <= U[BF] * o[0].abs() + 2 * U[BF] * A[0] + slack[0]).all()
+        step = {"bf16": 0.0, "fp8": 2.0 ** -4, "int8": 0.5 / 127 * 4}[cache]  # of a row's elements (int8: peak over rms)
+        coarse = step * (A + 2 * S[..., None] * A)
+        assert ((b[i].double().cpu() - o[0]).abs() <= U[BF] * o[0].abs() + 2 * U[BF] * A[0] + slack[0] + coarse[0]).all()
+
+
+@gpu
+def test_reference_sol():
+    """The command's figures are the analyzer's own, and the trace that it rates is the calls'."""
+    import oracle
+    from paper_2609_40247_amd import reference as R
+    r = R.reference_sol(heads=8, kv_heads=2, head_dim=64, prompt=300, batch=3, prompts=2, steps=4, cache="int8", page_size=32)
+    assert list(r["ops"]) == list(R.OPS)
+    assert [o["calls"] for o in r["ops"].values()] == [1, 1, 4, 4]
+    for o in r["ops"].values():
+        assert o["ns"] > 0 and o["sol"] == max(o["mfu"], o["mbu"]) > 0
+    code, want = oracle.analyze(r["columns"], r["params"], gap_capacity=100)
+    assert code == 0
+    for k in ("op_sol", "opn_sol", "opn_time", "opn_flops", "opn_bytes"):
+        assert (want[k] == r["outputs"][k]).all(), k
+
+
+def test_counts_of_the_layer():
+    """Operations and bytes of a decode step are those of the paged-attention case: 36 layers of 32 and 8 heads of
+    128 over 4000 tokens are 2.36 GFLOP and 0.59 GB."""
+    from types import SimpleNamespace
+
+    from paper_2609_40247_amd import reference as R
+    layer = SimpleNamespace(heads=32, kv_heads=8, head_dim=128,
+                            cache=SimpleNamespace(k=torch.zeros(1, dtype=BF), quantised=False))
+    f, b = R.counts(layer, "attn_decode", [4000])
+    assert round(36 * f / 1e9, 2) == 2.36 and round(36 * b / 1e9, 2) == 0.59
+    f, b = R.counts(layer, "attn_prompt", [3])
+    assert f == 4 * 128 * 32 * 6 and b == 3 * 80 * 256
+    f, b = R.counts(layer, "rope_write_step", [5, 9])
+    assert f == 3 * 2 * 40 * 128 and b == 2 * (80 * 256 + 16 * 256 + 512 + 16)
