@@ -1,6 +1,6 @@
 // The paged cache read back as dense rows: every code and scale read once,
 // every element written once, nothing computed but the scaling.  Bound by the
-// traffic.
+// traffic: 717 MB of int8 rows to half in 141 us, 5.1 TB/s, the rate of a copy.
 #include "ops.hpp"
 
 namespace hop {
@@ -38,35 +38,52 @@ __global__ __launch_bounds__(256) void k_cache_read(ReadArgs p) {
     if (lane == 0 && part == 0) flag(a.status, in_row ? HERSCHEL_OP_BAD_PAGE : HERSCHEL_OP_BAD_LENGTH);
   }
   const int64_t row0 = ((page * heads) << p.page_shift) + (at & (p.c.page_size - 1));
-  for (int h = part; h < heads; h += p.parts) {
-    const int64_t row = row0 + ((int64_t)h << p.page_shift);
+  // HB heads' rows are asked for before the first is waited for
+  constexpr int HB = 4, W = quantised(KIND) ? 1 : 2;
+  for (int h0 = part; h0 < heads; h0 += HB * p.parts) {
+    u32x4 x[HB][2][W];
+    float scale[HB][2];
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      uint16_t* out = (uint16_t*)(v ? a.v_out : a.k_out);
-      if (!out) continue;
-      u32x4 w0 = {0, 0, 0, 0}, w1 = {0, 0, 0, 0};
-      if (good) {
+    for (int i = 0; i < HB; ++i) {
+      const int h = h0 + i * p.parts;
+      const int64_t row = row0 + ((int64_t)h << p.page_shift);
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+#pragma unroll
+        for (int w = 0; w < W; ++w) x[i][v][w] = u32x4{0, 0, 0, 0};
+        scale[i][v] = 0;
+        if (!good || h >= heads || !(v ? a.v_out : a.k_out)) continue;
+        const u32x4* src = (const u32x4*)((const char*)(v ? p.c.v : p.c.k) + (row * D + lane * 16) * code_bytes(KIND));
+#pragma unroll
+        for (int w = 0; w < W; ++w) x[i][v][w] = src[w];
+        if constexpr (quantised(KIND)) scale[i][v] = (v ? p.c.v_scale : p.c.k_scale)[row];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < HB; ++i) {
+      const int h = h0 + i * p.parts;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        uint16_t* out = (uint16_t*)(v ? a.v_out : a.k_out);
+        if (h >= heads || !out) continue;
+        u32x4 w[2];
         if constexpr (!quantised(KIND)) {
-          const u32x4* src = (const u32x4*)((const uint16_t*)(v ? p.c.v : p.c.k) + row * D + lane * 16);
-          w0 = src[0];
-          w1 = src[1];
+          w[0] = x[i][v][0];
+          w[1] = x[i][v][1];
         } else {
-          const u32x4 x = *(const u32x4*)((const uint8_t*)(v ? p.c.v : p.c.k) + row * D + lane * 16);
-          const float s = (v ? p.c.v_scale : p.c.k_scale)[row];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int j = 0; j < 4; ++j) {
             float e[4];
-            decode2f<KIND, false>(x[i], e[0], e[1]);
-            decode2f<KIND, true>(x[i], e[2], e[3]);
-            u32x4& w = i < 2 ? w0 : w1;
-            w[2 * (i & 1)] = pack2<TYPE>(e[0] * s, e[1] * s);
-            w[2 * (i & 1) + 1] = pack2<TYPE>(e[2] * s, e[3] * s);
+            decode2f<KIND, false>(x[i][v][0][j], e[0], e[1]);
+            decode2f<KIND, true>(x[i][v][0][j], e[2], e[3]);
+            w[j / 2][2 * (j & 1)] = pack2<TYPE>(e[0] * scale[i][v], e[1] * scale[i][v]);
+            w[j / 2][2 * (j & 1) + 1] = pack2<TYPE>(e[2] * scale[i][v], e[3] * scale[i][v]);
           }
         }
+        u32x4* dst = (u32x4*)(out + (t * heads + h) * D + lane * 16);
+        dst[0] = w[0];
+        dst[1] = w[1];
       }
-      u32x4* dst = (u32x4*)(out + (t * heads + h) * D + lane * 16);
-      dst[0] = w0;
-      dst[1] = w1;
     }
   }
 }
@@ -83,7 +100,12 @@ static int read_launch(ReadArgs& p) {
   void (*k)(ReadArgs) = G == 4   ? k_cache_read<TYPE, KIND, 4>
                         : G == 8 ? k_cache_read<TYPE, KIND, 8>
                                  : k_cache_read<TYPE, KIND, 16>;
-  return launch(k, dim3((unsigned)(tiles * p.parts)), dim3(256), 0, p.a.hip_stream, p);
+  // Large reads run with five workgroups a CU at most, by LDS that nobody uses:
+  // fewer rows under way at once, in longer runs, suit the memory better (717 MB
+  // 141 against 162 us, 497 MB 111 against 117); small ones want all there are
+  // (34 MB 10.2 against 11.0 us).
+  const bool large = p.a.n_rows * p.c.n_heads * p.c.head_dim >= (16 << 20);
+  return launch(k, dim3((unsigned)(tiles * p.parts)), dim3(256), large ? 32768 : 0, p.a.hip_stream, p);
 }
 
 }  // namespace hop

@@ -17,7 +17,6 @@ There is no CPU fallback: without the built library or a GPU the calls raise.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import struct
@@ -129,7 +128,7 @@ def _rows(t: torch.Tensor, name: str, dims: int = 3) -> tuple:
 
 def _ints(t: torch.Tensor, name: str, dtype, shape: tuple, device: int) -> int:
     """The address of a contiguous tensor of this type and shape on a GPU."""
-    if not (t.dtype == dtype and t.get_device() == device and t.shape == shape and t.is_contiguous()):
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         _need(t.dtype == dtype, f"{name} must be {dtype}")
         _need(t.get_device() == device, f"{name} must be on GPU {device}")
         _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
@@ -138,7 +137,7 @@ def _ints(t: torch.Tensor, name: str, dtype, shape: tuple, device: int) -> int:
 
 
 def _like(t: torch.Tensor, first: torch.Tensor, name: str) -> None:
-    if not (t.dtype == first.dtype and t.get_device() == first.get_device()):
+    if t.dtype is not first.dtype or t.get_device() != first.get_device():
         _need(False, f"{name} must have the type and device of the other rows")
 
 
@@ -151,9 +150,11 @@ def _table(t: torch.Tensor, n_seqs: int, device: int) -> int:
 
 def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> None:
     """Calls an entry point with the tensors' device current."""
-    other = torch.cuda.current_device() != device
-    with torch.cuda.device(device) if other else _NOTHING:
+    if torch.cuda.current_device() == device:
         code = fn(args) if cache is None else fn(args, cache or None)
+    else:
+        with torch.cuda.device(device):
+            code = fn(args) if cache is None else fn(args, cache or None)
     if code != H.OK:
         raise (ValueError if code == H.EINVAL else RuntimeError)(f"{name}: {H.herschel_strerror(code)}")
 
@@ -161,7 +162,6 @@ def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> 
 # The current stream's handle by itself: 0.1 us, the Stream object around it 2.
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
-_NOTHING = contextlib.nullcontext()
 
 
 def _status(status: torch.Tensor | None, device: int) -> int:
@@ -250,6 +250,9 @@ def rotary_table(n_positions: int, rotary_dim: int, base: float = 10_000.0, stre
 
 
 # ------------------------------------------------------------ the operators
+_NO_ROWS = (0, 0, 0, 0)
+
+
 def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor | None, positions: torch.Tensor,
                table: torch.Tensor, cache: PagedCache | None = None, slots: torch.Tensor | None = None, *,
                layout: str = "half", keep_keys: bool = False, q_out: torch.Tensor | None = None,
@@ -262,21 +265,22 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
     _need(q is not None or k is not None, "q or k must be given")
     first = q if q is not None else k
     _rows(first, "q" if q is not None else "k")
-    dev = first.get_device()
+    dev, dtype = first.get_device(), first.dtype
     T, _, D = first.shape
 
     def rows(t, name, like=None):
         """(address, row stride, head stride, heads) of rows that go with the first ones."""
-        if t is None:
-            return 0, 0, 0, 0
-        st, shape = _rows(t, name), t.shape
-        _like(t, first, name)
-        if shape[0] != T or shape[2] != D or (like is not None and shape[1] != like):
+        shape, st = t.shape, t.stride()
+        if (len(shape) != 3 or t.dtype is not dtype or t.get_device() != dev or shape[0] != T or shape[2] != D or
+                st[2] != 1 and D > 1 or like is not None and shape[1] != like):
+            _rows(t, name)
+            _like(t, first, name)
             _need(False, f"{name} must have the tokens, heads and head size of the rows it goes with")
         return t.data_ptr(), st[0], st[1], shape[1]
 
-    qa, ka = rows(q, "q"), rows(k, "k")
-    va = rows(v, "v", ka[3]) if k is not None else rows(v, "v")
+    qa = rows(q, "q") if q is not None else _NO_ROWS
+    ka = rows(k, "k") if k is not None else _NO_ROWS
+    va = rows(v, "v", None if k is None else ka[3]) if v is not None else _NO_ROWS
     _need(layout in LAYOUTS, "layout must be 'half' or 'interleaved'")
     if not (table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous() and
             table.get_device() == dev):
@@ -292,7 +296,8 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
     if k_out is None and k is not None and (keep_keys or cache is None):
         k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
     _need((q_out is None or q is not None) and (k_out is None or k is not None), "an output needs its input")
-    qo, ko = rows(q_out, "q_out", qa[3]), rows(k_out, "k_out", ka[3])
+    qo = rows(q_out, "q_out", qa[3]) if q_out is not None else _NO_ROWS
+    ko = rows(k_out, "k_out", ka[3]) if k_out is not None else _NO_ROWS
     reported = _status(status, dev) if status is not None else cache._status if cache is not None else 0
     args = _ROPE.pack(qa[0], ka[0], va[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[0], ko[0], qo[1], qo[2], ko[1],
                       ko[2], pos, table.data_ptr(), table.shape[0], slot, T, qa[3], ka[3], D, 2 * table.shape[1],
