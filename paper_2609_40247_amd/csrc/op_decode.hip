@@ -228,14 +228,14 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeAr
 #pragma unroll
         for (int i = 0; i < (CB == 2 ? NS : NS / 2); ++i) s.k[t][i] = *(const u32x4*)(kp + 64 * i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 4; ++j) {  // whole rows, read once: past the caches (32 x 4096 in bf16 102 to 93 us)
           const char* vp = (const char*)p.c.v + base * (D * CB) + (uint32_t)(row(k + 4 * g + j) * (D * CB) + m * (ND * CB));
           uint32_t* to = s.v[4 * t + j];
           if constexpr (VW == 4) {
-            const u32x4 x = *(const u32x4*)vp;
+            const u32x4 x = __builtin_nontemporal_load((const u32x4*)vp);
             to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
           } else if constexpr (VW == 2) {
-            const u32x2 x = *(const u32x2*)vp;
+            const u32x2 x = __builtin_nontemporal_load((const u32x2*)vp);
             to[0] = x[0], to[1] = x[1];
           } else {
             to[0] = *(const uint32_t*)vp;

@@ -133,8 +133,10 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs p) {
     if (dst && holds) {
       const herschel_strides so = part == 0 ? a.q_out_strides : a.k_out_strides;
       dst += t * so.row + head * so.head;
-      *(u32x4*)(dst + at0) = w0;
-      *(u32x4*)(dst + at1) = w1;
+      // past the caches, which hold what is still to be read: 8192 tokens 47.8 to 38.3 us,
+      // with the codes as well 35.1
+      __builtin_nontemporal_store(w0, (u32x4*)(dst + at0));
+      __builtin_nontemporal_store(w1, (u32x4*)(dst + at1));
     }
     if constexpr (KIND >= 0) {
       if (part == 0 || row0 < 0) continue;
@@ -156,8 +158,8 @@ __global__ __launch_bounds__(256) void k_rope(RopeArgs p) {
         const float scale = row_scale<KIND>(m, inv);
         if (holds) {
           uint8_t* to = (uint8_t*)(part == 1 ? p.c.k : p.c.v) + row * D;
-          *(u32x2*)(to + at0) = u32x2{encode4<KIND>(x, inv), encode4<KIND>(x + 4, inv)};
-          *(u32x2*)(to + at1) = u32x2{encode4<KIND>(x + 8, inv), encode4<KIND>(x + 12, inv)};
+          __builtin_nontemporal_store(u32x2{encode4<KIND>(x, inv), encode4<KIND>(x + 4, inv)}, (u32x2*)(to + at0));
+          __builtin_nontemporal_store(u32x2{encode4<KIND>(x + 8, inv), encode4<KIND>(x + 12, inv)}, (u32x2*)(to + at1));
           if (lane == 0) (part == 1 ? p.c.k_scale : p.c.v_scale)[row] = scale;
         }
       }
@@ -254,13 +256,13 @@ static int rope_launch(RopeArgs& p) {
   }
   // Lanes of a row, row groups that share a token, and workgroups that share
   // it.  Few tokens: as many groups as rows, one row each, the launch's time
-  // is latency.  Many: a group takes up to four rows with one load of cos and sin.
+  // is latency.  Many: a group takes up to three rows with one load of cos and sin.
   const int G = a.head_dim <= 64 ? 4 : a.head_dim <= 128 ? 8 : 16, per = 256 / G;
   const bool few = a.n_tokens * rows < 16384;
   p.groups = per;
   p.parts = 1;
-  while (p.groups > 1 && p.groups / 2 * (few ? 1 : 4) >= rows) p.groups /= 2;
-  if (p.groups == per) p.parts = (rows + per * (few ? 1 : 4) - 1) / (per * (few ? 1 : 4));
+  while (p.groups > 1 && p.groups / 2 * (few ? 1 : 3) >= rows) p.groups /= 2;
+  if (p.groups == per) p.parts = (rows + per * (few ? 1 : 3) - 1) / (per * (few ? 1 : 3));
   const int tokens = per / p.groups;
   const int64_t blocks = (a.n_tokens + tokens - 1) / tokens * p.parts;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
