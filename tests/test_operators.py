@@ -33,6 +33,11 @@ gpu = pytest.mark.gpu
 DEV = "cuda"
 
 
+def named(value):
+    """A parameter's name, the same in every process: some values print as addresses."""
+    return "-".join(value) if isinstance(value, dict) else str(value)
+
+
 def rand(*shape, seed=0, dtype=BF, gain=1.0):
     g = torch.Generator().manual_seed(seed)
     return (torch.randn(*shape, generator=g) * gain).to(dtype)
@@ -749,7 +754,7 @@ BAD_CACHES = [dict(k=None), dict(v=FAKE + 8), dict(n_pages=0), dict(n_heads=0), 
               dict(n_heads=1 << 24)]
 
 
-@pytest.mark.parametrize("bad", BAD_CACHES, ids=str)
+@pytest.mark.parametrize("bad", BAD_CACHES, ids=named)
 def test_bad_caches_are_refused(bad):
     c = ctypes.byref(fake_cache(**bad))
     L = lib()
@@ -765,14 +770,14 @@ def test_bad_caches_are_refused(bad):
     dict(table=None), dict(table=FAKE + 4), dict(n_positions=0), dict(n_tokens=-1), dict(q_heads=0), dict(kv_heads=3),
     dict(head_dim=62, rotary_dim=62), dict(head_dim=65), dict(head_dim=0), dict(rotary_dim=66), dict(rotary_dim=31),
     dict(rotary_dim=-2), dict(layout=2), dict(type=O.FP8), dict(type=O.F16), dict(q_strides=O._Strides(-1, 64)),
-    dict(k_strides=O._Strides(64, -64)), dict(q_heads=1 << 20)], ids=str)
+    dict(k_strides=O._Strides(64, -64)), dict(q_heads=1 << 20)], ids=named)
 def test_bad_rope_calls_are_refused(bad):
     assert lib().herschel_rope_write(ctypes.byref(rope_args(**bad)), ctypes.byref(fake_cache())) == H.EINVAL
 
 
 @pytest.mark.parametrize("bad", [dict(n_seqs=0), dict(n_rows=-1), dict(n_rows=1 << 31), dict(table_stride=-1),
                                  dict(cu=None), dict(block_table=None), dict(k_out=FAKE + 2), dict(type=O.F16),
-                                 dict(type=O.INT8)], ids=str)
+                                 dict(type=O.INT8)], ids=named)
 def test_bad_read_calls_are_refused(bad):
     assert lib().herschel_cache_read(ctypes.byref(read_args(**bad)), ctypes.byref(fake_cache())) == H.EINVAL
 
@@ -781,7 +786,7 @@ def test_bad_read_calls_are_refused(bad):
     dict(n_seqs=0), dict(n_q=-1), dict(n_k=1 << 31), dict(max_q=-1), dict(head_dim=96), dict(kv_heads=0),
     dict(q_heads=3), dict(type=O.FP8), dict(window=-1), dict(scale=math.nan), dict(scale=math.inf), dict(cu_q=None),
     dict(cu_k=None), dict(q=None), dict(k=None), dict(out=FAKE + 4), dict(q=FAKE + 1),
-    dict(v_strides=O._Strides(-1, 0))], ids=str)
+    dict(v_strides=O._Strides(-1, 0))], ids=named)
 def test_bad_prompt_calls_are_refused(bad):
     assert lib().herschel_attn_prompt(ctypes.byref(prompt_args(**bad))) == H.EINVAL
 
@@ -792,7 +797,7 @@ def test_bad_prompt_calls_are_refused(bad):
     (dict(block_table=None), H.EINVAL), (dict(table_stride=-1), H.EINVAL), (dict(type=O.F16), H.EINVAL),
     (dict(window=-1), H.EINVAL), (dict(scale=math.nan), H.EINVAL), (dict(q_seq_stride=-1), H.EINVAL),
     (dict(workspace=None), H.EWORKSPACE), (dict(workspace=FAKE + 128), H.EWORKSPACE),
-    (dict(workspace_bytes=1000), H.EWORKSPACE)], ids=str)
+    (dict(workspace_bytes=1000), H.EWORKSPACE)], ids=named)
 def test_bad_decode_calls_are_refused(bad, code):
     assert lib().herschel_attn_decode(ctypes.byref(decode_args(**bad)), ctypes.byref(fake_cache())) == code
 
