@@ -150,7 +150,7 @@ def _table(t: torch.Tensor, n_seqs: int, device: int) -> int:
 
 def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> None:
     """Calls an entry point with the tensors' device current."""
-    if torch.cuda.current_device() == device:
+    if _device() == device:
         code = fn(args) if cache is None else fn(args, cache or None)
     else:
         with torch.cuda.device(device):
@@ -160,8 +160,10 @@ def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> 
 
 
 # The current stream's handle by itself: 0.1 us, the Stream object around it 2.
+# The device likewise: the tensors have initialised torch's GPU state by then.
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _status(status: torch.Tensor | None, device: int) -> int:
@@ -262,46 +264,64 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
 
     Returns (q rotated, k rotated): new tensors, ``q_out`` and ``k_out`` where given (they may be q and k
     themselves); k's is None unless ``keep_keys`` or ``k_out`` asks for it or there is no cache."""
-    _need(q is not None or k is not None, "q or k must be given")
     first = q if q is not None else k
-    _rows(first, "q" if q is not None else "k")
-    dev, dtype = first.get_device(), first.dtype
-    T, _, D = first.shape
+    if first is None:
+        raise ValueError("q or k must be given")
+    dev, dtype, shape = first.get_device(), first.dtype, first.shape
+    if dev < 0 or dtype not in TYPES or len(shape) != 3:
+        _rows(first, "q" if q is not None else "k")
+    T, _, D = shape
 
     def rows(t, name, like=None):
         """(address, row stride, head stride, heads) of rows that go with the first ones."""
-        shape, st = t.shape, t.stride()
-        if (len(shape) != 3 or t.dtype is not dtype or t.get_device() != dev or shape[0] != T or shape[2] != D or
-                st[2] != 1 and D > 1 or like is not None and shape[1] != like):
+        (n, heads, d), (row, head, step) = t.shape, t.stride()
+        if (t.dtype is not dtype or t.get_device() != dev or n != T or d != D or step != 1 and D > 1 or
+                like is not None and heads != like):
             _rows(t, name)
             _like(t, first, name)
             _need(False, f"{name} must have the tokens, heads and head size of the rows it goes with")
-        return t.data_ptr(), st[0], st[1], shape[1]
+        return t.data_ptr(), row, head, heads
 
+    for t, name in ((k, "k"), (v, "v"), (q_out, "q_out"), (k_out, "k_out")):
+        if t is not None and t.dim() != 3:
+            _rows(t, name)
     qa = rows(q, "q") if q is not None else _NO_ROWS
     ka = rows(k, "k") if k is not None else _NO_ROWS
     va = rows(v, "v", None if k is None else ka[3]) if v is not None else _NO_ROWS
-    _need(layout in LAYOUTS, "layout must be 'half' or 'interleaved'")
-    if not (table.dtype == torch.float32 and table.dim() == 3 and table.shape[2] == 2 and table.is_contiguous() and
+    if layout not in LAYOUTS:
+        raise ValueError("layout must be 'half' or 'interleaved'")
+    pairs = table.shape
+    if not (table.dtype is torch.float32 and len(pairs) == 3 and pairs[2] == 2 and table.is_contiguous() and
             table.get_device() == dev):
-        _need(False, "table must be float32 [positions, pairs, 2], contiguous, on the rows' device")
+        raise ValueError("table must be float32 [positions, pairs, 2], contiguous, on the rows' device")
     pos, slot = _ints(positions, "positions", torch.int64, (T,), dev), 0
     if cache is not None:
-        _need(k is not None and v is not None and slots is not None, "a cache needs k, v and slots")
-        _need(ka[3] == cache.n_heads and D == cache.head_dim, "the cache has another number of heads or head size")
+        if k is None or v is None or slots is None:
+            raise ValueError("a cache needs k, v and slots")
+        if ka[3] != cache.n_heads or D != cache.head_dim:
+            raise ValueError("the cache has another number of heads or head size")
         cache._fits(k)
         slot = _ints(slots, "slots", torch.int64, (T,), dev)
-    if q_out is None and q is not None:
+    if q_out is not None:
+        _need(q is not None, "q_out needs q")
+        qo = rows(q_out, "q_out", qa[3])
+    elif q is not None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    if k_out is None and k is not None and (keep_keys or cache is None):
+        qo = q_out.data_ptr(), qa[3] * D, D
+    else:
+        qo = _NO_ROWS
+    if k_out is not None:
+        _need(k is not None, "k_out needs k")
+        ko = rows(k_out, "k_out", ka[3])
+    elif k is not None and (keep_keys or cache is None):
         k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-    _need((q_out is None or q is not None) and (k_out is None or k is not None), "an output needs its input")
-    qo = rows(q_out, "q_out", qa[3]) if q_out is not None else _NO_ROWS
-    ko = rows(k_out, "k_out", ka[3]) if k_out is not None else _NO_ROWS
+        ko = k_out.data_ptr(), ka[3] * D, D
+    else:
+        ko = _NO_ROWS
     reported = _status(status, dev) if status is not None else cache._status if cache is not None else 0
     args = _ROPE.pack(qa[0], ka[0], va[0], qa[1], qa[2], ka[1], ka[2], va[1], va[2], qo[0], ko[0], qo[1], qo[2], ko[1],
-                      ko[2], pos, table.data_ptr(), table.shape[0], slot, T, qa[3], ka[3], D, 2 * table.shape[1],
-                      LAYOUTS[layout], TYPES[first.dtype], reported, _stream(dev))
+                      ko[2], pos, table.data_ptr(), pairs[0], slot, T, qa[3], ka[3], D, 2 * pairs[1],
+                      LAYOUTS[layout], TYPES[dtype], reported, _stream(dev))
     _call((lib or _lib()).herschel_rope_write, dev, "rope_write", args, 0 if cache is None else cache._at)
     return q_out, k_out
 
@@ -319,11 +339,20 @@ def cache_read(cache: PagedCache, block_table: torch.Tensor, cu: torch.Tensor, *
     starts, table = _ints(cu, "cu", torch.int32, cu.shape, dev), _table(block_table, n, dev)
     _need(total >= 0, "total must not be negative")
     shape = (total, cache.n_heads, cache.head_dim)
-    k_out = cache.k.new_empty(shape, dtype=dtype) if k_out is None else k_out
-    v_out = cache.k.new_empty(shape, dtype=dtype) if v_out is None else v_out
-    cache._fits(k_out)
-    args = _READ.pack(table, block_table.shape[1], starts, n, total, _ints(k_out, "k_out", dtype, shape, dev),
-                      _ints(v_out, "v_out", dtype, shape, dev), TYPES[dtype], cache._status, _stream(dev))
+    if not (cache.quantised or dtype is cache.k.dtype):
+        raise ValueError("a 16-bit cache has the type of the rows")
+    if k_out is None:
+        k_out = cache.k.new_empty(shape, dtype=dtype)
+        to_k = k_out.data_ptr()
+    else:
+        to_k = _ints(k_out, "k_out", dtype, shape, dev)
+    if v_out is None:
+        v_out = torch.empty_like(k_out)
+        to_v = v_out.data_ptr()
+    else:
+        to_v = _ints(v_out, "v_out", dtype, shape, dev)
+    args = _READ.pack(table, block_table.shape[1], starts, n, total, to_k, to_v, TYPES[dtype], cache._status,
+                      _stream(dev))
     _call((lib or _lib()).herschel_cache_read, dev, "cache_read", args, cache._at)
     return k_out, v_out
 
@@ -351,12 +380,15 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     _need(window >= 0, "window must not be negative")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        to = out.data_ptr()
+    else:
+        to = _ints(out, "out", q.dtype, q.shape, dev)
     lse = q.new_empty((n_q, heads), dtype=torch.float32) if return_lse else None
     args = _PROMPT.pack(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
-        _ints(out, "out", q.dtype, q.shape, dev), lse.data_ptr() if return_lse else 0, from_q, from_k,
+        to, lse.data_ptr() if return_lse else 0, from_q, from_k,
         cu_q.shape[0] - 1, n_q, n_k, max_q, heads, kv_heads, D, TYPES[q.dtype], bool(causal), window,
-        D ** -0.5 if scale is None else scale, _status(status, dev), _stream(dev))
+        D ** -0.5 if scale is None else scale, 0 if status is None else _status(status, dev), _stream(dev))
     _call((lib or _lib()).herschel_attn_prompt, dev, "attn_prompt", args)
     return (out, lse) if return_lse else out
 
@@ -394,19 +426,22 @@ class DecodeAttention:
         B = shape[0]
         _need(q.dtype == self.dtype, "q must have the type that DecodeAttention was made for")
         c._fits(q)
-        _need(1 <= B <= self.batch and shape[1:] == (self.new_tokens, self.heads, c.head_dim),
+        _need(1 <= B <= self.batch and shape == (B, self.new_tokens, self.heads, c.head_dim),
               "q must have the sizes that the workspace is for")
         table, lens = _table(block_table, B, dev), _ints(seq_lens, "seq_lens", torch.int32, (B,), dev)
         _need(window >= 0, "window must not be negative")
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            to = out.data_ptr()
+        else:
+            to = _ints(out, "out", q.dtype, shape, dev)
         lse = q.new_empty(shape[:3], dtype=torch.float32) if return_lse else None
         stream = _stream(dev)
         ws = self._workspaces.get(stream)
         if ws is None:
             ws = self._workspaces[stream] = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device)
         args = _DECODE.pack(
-            q.data_ptr(), sq[0], sq[1], sq[2], _ints(out, "out", q.dtype, shape, dev),
+            q.data_ptr(), sq[0], sq[1], sq[2], to,
             lse.data_ptr() if return_lse else 0, table, block_table.shape[1], lens, B, self.new_tokens, self.heads,
             TYPES[q.dtype], window, c.head_dim ** -0.5 if scale is None else scale, ws.data_ptr(),
             self.workspace_bytes, c._status, stream)
