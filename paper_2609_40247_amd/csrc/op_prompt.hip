@@ -66,6 +66,45 @@ __device__ __forceinline__ void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, GROUP);
 }
 
+// A row's outputs from the keys [lo, hi) one by one, by a wave whose lanes go
+// across the dimensions.  Factors are never 0, so that an infinite value or sum
+// stays one.
+template <int TYPE, int D>
+__device__ __forceinline__ void row_by_key(const uint16_t* q, const uint16_t* kbase, const uint16_t* vbase,
+                                           const herschel_prompt_args& a, int lo, int hi, int64_t at) {
+  const int lane = threadIdx.x % WAVE;
+  float qv[D / WAVE], acc[D / WAVE], top = NO_KEY, den = 0, unused;
+#pragma unroll
+  for (int d = 0; d < D / WAVE; ++d) {
+    unpack2<TYPE>(q[d * WAVE + lane], qv[d], unused);
+    acc[d] = 0;
+  }
+  for (int key = lo; key < hi; ++key) {
+    float x = 0, v[D / WAVE];
+#pragma unroll
+    for (int d = 0; d < D / WAVE; ++d) {
+      float k;
+      unpack2<TYPE>(kbase[key * a.k_strides.row + d * WAVE + lane], k, unused);
+      unpack2<TYPE>(vbase[key * a.v_strides.row + d * WAVE + lane], v[d], unused);
+      x += qv[d] * k;
+    }
+#pragma unroll
+    for (int m = 1; m < WAVE; m *= 2) x += __shfl_xor(x, m);
+    x *= a.scale * 1.44269504088896340736f;
+    const float next = fmaxf(top, x), by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
+    float e = __builtin_amdgcn_exp2f(x - next);
+    if (e == 0) e = 0x1p-126f;
+    top = next;
+    den = den * by + e;
+#pragma unroll
+    for (int d = 0; d < D / WAVE; ++d) acc[d] = acc[d] * by + e * v[d];
+  }
+#pragma unroll
+  for (int d = 0; d < D / WAVE; ++d)
+    ((uint16_t*)a.out)[at * D + d * WAVE + lane] = (uint16_t)pack2<TYPE>(den == 0 ? 0.0f : acc[d] / den, 0.0f);
+  if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+}
+
 template <int TYPE, int D, int WAVES, bool VEC>
 __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   constexpr int QROWS = 32 * WAVES, THREADS = WAVE * WAVES;
@@ -333,44 +372,11 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) check += o[d][i] - o[d][i];
   if (__ballot(!(check == 0))) {
-    // row by row, the wave's lanes across the dimensions
-    const uint16_t* qb = (const uint16_t*)a.q + q0 * a.q_strides.row + qh * a.q_strides.head;
     const int rows = min(32, nq - first_row);
     for (int r = 0; r < rows; ++r) {
-      const int lo = __shfl(from, r), hi = __shfl(to, r);
-      float qv[D / WAVE], acc[D / WAVE], top = NO_KEY, den = 0, unused;
-#pragma unroll
-      for (int d = 0; d < D / WAVE; ++d) {
-        unpack2<TYPE>(qb[(first_row + r) * a.q_strides.row + d * WAVE + lane], qv[d], unused);
-        acc[d] = 0;
-      }
-      for (int key = lo; key < hi; ++key) {
-        float x = 0, v[D / WAVE];
-#pragma unroll
-        for (int d = 0; d < D / WAVE; ++d) {
-          float k;
-          unpack2<TYPE>(kbase[key * a.k_strides.row + d * WAVE + lane], k, unused);
-          unpack2<TYPE>(vbase[key * a.v_strides.row + d * WAVE + lane], v[d], unused);
-          x += qv[d] * k;
-        }
-#pragma unroll
-        for (int m = 1; m < WAVE; m *= 2) x += __shfl_xor(x, m);
-        x *= a.scale * 1.44269504088896340736f;
-        // factors are never 0, so that an infinite value or sum stays one
-        const float next = fmaxf(top, x), by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
-        float e = __builtin_amdgcn_exp2f(x - next);
-        if (e == 0) e = 0x1p-126f;
-        top = next;
-        den = den * by + e;
-#pragma unroll
-        for (int d = 0; d < D / WAVE; ++d) acc[d] = acc[d] * by + e * v[d];
-      }
       const int64_t at = (q0 + first_row + r) * a.q_heads + qh;
-#pragma unroll
-      for (int d = 0; d < D / WAVE; ++d)
-        ((uint16_t*)a.out)[at * D + d * WAVE + lane] = (uint16_t)pack2<TYPE>(den == 0 ? 0.0f : acc[d] / den, 0.0f);
-      if (a.lse && lane == 0)
-        a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+      row_by_key<TYPE, D>((const uint16_t*)a.q + (q0 + first_row + r) * a.q_strides.row + qh * a.q_strides.head, kbase, vbase,
+                          a, __shfl(from, r), __shfl(to, r), at);
     }
     return;
   }
@@ -388,6 +394,239 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   if (a.lse && g == 0) a.lse[at] = sum == 0 ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
 }
 
+// Few rows: 32 to a workgroup, whose four waves share the keys, 32 at a time.
+//
+// Where workgroups of 128 rows would leave most of the card idle, what counts is
+// the chain of tiles that one wave goes through: here it is four times shorter
+// (with 32 heads of 128, 128 rows 6.7 us against 9.3, 512 rows 12.2 against 16.7,
+// 16 rows over 2048 keys 22.6 against 53.7).  The rows are a token's query heads
+// of one key head, then the next token's, so that a call with fewer than 32
+// tokens fills its workgroups too.  A key goes to one wave only, through LDS that
+// is the wave's own (loads in the products' layout touch a row per lane: 2048
+// keys take 25.8 us), so no wave waits for another before the parts are joined.
+// The next step's keys are asked for once the scores are there, its values after
+// the second product.
+constexpr int FEW_WAVES = 4;  // eight: 2048 keys 20 us against 23, but 512 rows 16.7 against 12.2
+template <int TYPE, int D, bool VEC>
+__global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p) {
+  const herschel_prompt_args& a = p.a;
+  constexpr int W = FEW_WAVES;
+  constexpr int DT = D / 32, NS = D / 16;
+  constexpr int NC = D / 8;          // 16-byte chunks of a row
+  constexpr int PART = 16 * DT / W;  // values of a lane that a wave joins
+  constexpr int BYTES = 32 * D * 2;
+  // a wave's keys and values; at the end, the first and second half of its sums
+  __shared__ __align__(16) char s_k[W * BYTES];
+  __shared__ __align__(16) char s_v[W * BYTES];
+  __shared__ float s_ref[W][32], s_sum[W][32];
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = __builtin_amdgcn_readfirstlane(tid / WAVE), n = lane % 32, g = lane / 32;
+  uint32_t id = blockIdx.x;  // longest first
+  const int kh = (int)(id % a.kv_heads);
+  id /= a.kv_heads;
+  const int b = (int)(id % a.n_seqs), level = p.levels - 1 - (int)(id / a.n_seqs);
+  // lengths taken as the nearest valid
+  const int64_t q0w = a.cu_q[b], q1w = a.cu_q[b + 1], k0w = a.cu_k[b], k1w = a.cu_k[b + 1];
+  const int64_t q0 = min(max(q0w, (int64_t)0), a.n_q), q1 = min(max(q1w, q0), a.n_q);
+  const int64_t kk0 = min(max(k0w, (int64_t)0), a.n_k), kk1 = min(max(k1w, kk0), a.n_k);
+  const int nq = (int)min(q1 - q0, (int64_t)a.max_q), nk = (int)(kk1 - kk0);
+  if (level == 0 && kh == 0 && tid == 0 && (q0 != q0w || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
+    flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+  const int row0 = level * 32, rows = nq * p.group;
+  if (row0 >= rows) return;
+  const int shift = nk - (int)(q1 - q0);  // causal: token i sees keys up to i + shift
+
+  // this lane's row (the last one again past it), and the keys it sees: [from, to)
+  const int row = min(row0 + n, rows - 1), tok = row / p.group, qh = kh * p.group + row % p.group;
+  auto sees_to = [&](int t) INLINE { return a.causal ? min(nk, max(0, t + shift + 1)) : nk; };
+  auto sees_from = [&](int t) INLINE { return a.window > 0 ? max(0, t + shift - a.window + 1) : 0; };
+  const int to = sees_to(tok), from = sees_from(tok);
+  // the workgroup's
+  const int first = row0 / p.group, last = min(row0 + 31, rows - 1) / p.group;
+  const int any_to = sees_to(last), any_from = sees_from(first), all_to = sees_to(first), all_from = sees_from(last);
+
+  const uint16_t* qrow = (const uint16_t*)a.q + (q0 + tok) * a.q_strides.row + qh * a.q_strides.head;
+  const uint32_t sign = a.scale < 0 ? 0x80008000u : 0u;
+  u32x4 q[NS];
+#pragma unroll
+  for (int s = 0; s < NS; ++s) q[s] = VEC ? *(const u32x4*)(qrow + 16 * s + 8 * g) : load_elements(qrow + 16 * s + 8 * g);
+  const float to_log2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 0x1p-100f);
+  const uint16_t* kbase = (const uint16_t*)a.k + kk0 * a.k_strides.row + kh * a.k_strides.head;
+  const uint16_t* vbase = (const uint16_t*)a.v + kk0 * a.v_strides.row + kh * a.v_strides.head;
+
+  f32x16 o[DT];
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] = 0;
+  float ref = NO_KEY, sum = 0;
+  // A load takes RPC whole rows; LDS chunk c of a row holds the row's chunk
+  // c ^ f(row), as above.
+  constexpr int RPC = WAVE / NC, LOADS = 32 / RPC;
+  auto fk = [](int r) INLINE { return (D == 128 ? r : r >> 1) & (NC - 1); };
+  auto fv = [](int r) INLINE { return D == 128 ? (r & 3) * 4 : (r >> 1 & 1) * 4; };
+  char* const my_k = s_k + wave * BYTES;
+  char* const my_v = s_v + wave * BYTES;
+  const int crow = lane / NC, cc = lane % NC;
+  const uint32_t koff = (uint32_t)(crow * a.k_strides.row + cc * 8) * 2;
+  const uint32_t voff = (uint32_t)(crow * a.v_strides.row + cc * 8) * 2;
+  auto load = [&](u32x4 (&to)[LOADS], const uint16_t* base, int64_t stride, uint32_t off, int k0) INLINE {
+    if (VEC && k0 + 32 <= nk) {
+      const char* src = (const char*)(base + k0 * stride);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) to[i] = *(const u32x4*)(src + i * RPC * stride * 2 + off);
+    } else {  // rows past the sequence's end read its last row
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        const uint16_t* src = base + min(k0 + i * RPC + crow, nk - 1) * stride + cc * 8;
+        to[i] = VEC ? *(const u32x4*)src : load_elements(src);
+      }
+    }
+  };
+  // LDS written by the wave is read by its other lanes
+  auto written = [&]() INLINE {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+  };
+  u32x4 k[LOADS], v[LOADS];
+  const int vrow = 4 * g + lane % 16 / 4, vcol = 2 * (lane / 16 % 2) + lane % 4 / 2;
+  int k0 = any_from / 32 * 32 + wave * 32;
+  if (k0 < any_to) {
+    load(k, kbase, a.k_strides.row, koff, k0);
+    load(v, vbase, a.v_strides.row, voff, k0);
+  }
+#pragma unroll
+  for (int s = 0; s < NS; ++s) q[s] ^= sign;  // a negative scale goes into Q's signs: what is left is not negative
+  for (; k0 < any_to; k0 += 32 * W) {
+    f32x16 sc;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sc[i] = 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = i * RPC + crow;
+      *(u32x4*)(my_k + r * (D * 2) + (cc ^ fk(r)) * 16) = k[i];
+    }
+    written();
+#pragma unroll
+    for (int s = 0; s < NS; ++s)
+      sc = mfma32<TYPE>(*(const u32x4*)(my_k + n * (D * 2) + (((2 * s + g) ^ fk(n)) * 16)), q[s], sc);
+    const bool more = k0 + 32 * W < any_to;
+    if (more) load(k, kbase, a.k_strides.row, koff, k0 + 32 * W);
+    if (k0 + 32 > all_to || k0 < all_from) {
+      const int lo = from - k0 - 4 * g, hi = to - k0 - 4 * g;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = 8 * (i / 4) + i % 4;
+        sc[i] = c < hi && c >= lo ? sc[i] : -INFINITY;
+      }
+    }
+    u32x4 pb[2];
+    auto exponentials = [&]() INLINE {
+      float s = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * i], to_log2, -ref));
+        const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * i + 1], to_log2, -ref));
+        s += e0 + e1;
+        pb[i / 4][i % 4] = pack2<TYPE>(e0, e1);
+      }
+      return s;
+    };
+    float t = exponentials();
+    if (__ballot(!(t <= LARGE))) {
+      float top = sc[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float next = fmaxf(ref, top * to_log2), by = __builtin_amdgcn_exp2f(ref - next);
+      ref = next;
+      sum *= by;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= by;
+      t = exponentials();
+    }
+    sum += t;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      const int r = i * RPC + crow;
+      *(u32x4*)(my_v + r * (D * 2) + (cc ^ fv(r)) * 16) = v[i];
+    }
+    written();
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 vt;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int key = 16 * s + 8 * i + vrow;
+          const char* at = my_v + key * (D * 2) + ((4 * d + vcol) ^ fv(vrow)) * 16 + lane % 2 * 8;
+          const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsHalves*)at));
+          vt[2 * i] = w[0];
+          vt[2 * i + 1] = w[1];
+        }
+        o[d] = mfma32<TYPE>(vt, pb[s], o[d]);
+      }
+    written();
+    if (more) load(v, vbase, a.v_strides.row, voff, k0 + 32 * W);
+  }
+  // The waves' parts, joined through LDS: wave w the values w PART ... of every lane.
+  sum += __shfl_xor(sum, 32);
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) ((float*)(d < DT / 2 ? my_k : my_v))[(d % (DT / 2) * 16 + i) * WAVE + lane] = o[d][i];
+  if (g == 0) {
+    s_ref[wave][n] = ref;
+    s_sum[wave][n] = sum;
+  }
+  __syncthreads();
+  float acc[PART], den = 0, top = NO_KEY;
+#pragma unroll
+  for (int w = 0; w < W; ++w) top = fmaxf(top, s_ref[w][n]);
+#pragma unroll
+  for (int i = 0; i < PART; ++i) acc[i] = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float by = __builtin_amdgcn_exp2f(s_ref[w][n] - top);
+    den += s_sum[w][n] * by;
+#pragma unroll
+    for (int i = 0; i < PART; ++i)
+      acc[i] += ((const float*)((wave < W / 2 ? s_k : s_v) + w * BYTES))[(wave % (W / 2) * PART + i) * WAVE + lane] * by;
+  }
+  float check = den - den;  // 0, or NaN if a sum is not finite
+#pragma unroll
+  for (int i = 0; i < PART; ++i) check += acc[i] - acc[i];
+  if (__syncthreads_or(!(check == 0))) {
+    for (int r = row0 + wave; r < min(row0 + 32, rows); r += W) {
+      const int t = r / p.group, h = kh * p.group + r % p.group;
+      row_by_key<TYPE, D>((const uint16_t*)a.q + (q0 + t) * a.q_strides.row + h * a.q_strides.head, kbase, vbase, a,
+                          sees_from(t), sees_to(t), (q0 + t) * a.q_heads + h);
+    }
+    return;
+  }
+  if (row0 + n >= rows) return;
+  const float inv = den > 0 ? 1.0f / den : 0.0f;  // no key seen: 0
+  const int64_t at = (q0 + tok) * a.q_heads + qh;
+#pragma unroll
+  for (int i = 0; i < PART; i += 4) {  // four dimensions in order
+    const int x = wave * PART + i;
+    uint16_t* out = (uint16_t*)a.out + at * D + 32 * (x / 16) + 8 * (x % 16 / 4) + 4 * g;
+    *(u32x2*)out = u32x2{pack2<TYPE>(acc[i] * inv, acc[i + 1] * inv), pack2<TYPE>(acc[i + 2] * inv, acc[i + 3] * inv)};
+  }
+  if (a.lse && g == 0 && wave == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+}
+
+template <int TYPE, int D>
+static int prompt_few(PromptArgs& p, bool vec) {
+  const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, blocks = levels * p.a.n_seqs * p.a.kv_heads;
+  if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
+  p.levels = (int)levels;
+  return launch(vec ? k_prompt_few<TYPE, D, true> : k_prompt_few<TYPE, D, false>, dim3((unsigned)blocks),
+                dim3(FEW_WAVES * WAVE), 0, p.a.hip_stream, p);
+}
+
 template <int TYPE, int D, int WAVES>
 static int prompt_launch(PromptArgs& p, bool vec) {
   p.levels = (p.a.max_q + 32 * WAVES - 1) / (32 * WAVES);
@@ -401,7 +640,11 @@ static int prompt_launch(PromptArgs& p, bool vec) {
                 dim3(WAVES * WAVE), 0, p.a.hip_stream, p);
 }
 
-// Eight waves (256 rows) or four (128).  Eight in turns are faster where there
+// Few rows: as long as 32 of them (of one key head) a workgroup make no more
+// workgroups than the card holds at once, about 20,000 in all (24 x 16 rows of 16
+// heads of 64 4.7 us against 5.7, 24 x 64 6.2 against 6.6; 24 x 128 11.6 against
+// 9.3, 1024 rows of 32 heads of 128 27.0 against 26.4).
+// Else eight waves (256 rows) or four (128).  Eight in turns are faster where there
 // is enough for every CU twice over: 4096 rows of 32 heads of 128 145 us against
 // 156, 8192 983 against 1080; below, what counts is more and smaller workgroups:
 // 512 rows 23 against 18 us, 8 heads of 4096 95 against 83.  With heads of 64
@@ -409,6 +652,8 @@ static int prompt_launch(PromptArgs& p, bool vec) {
 // twice: 186 against 175 us).
 template <int TYPE>
 static int prompt_size(PromptArgs& p, bool vec) {
+  if (p.a.n_q * p.a.q_heads <= 20480 && (int64_t)p.a.max_q * p.group < 0x7fffffe0)
+    return p.a.head_dim == 64 ? prompt_few<TYPE, 64>(p, vec) : prompt_few<TYPE, 128>(p, vec);
   if (p.a.head_dim == 64) return prompt_launch<TYPE, 64, 4>(p, vec);
   const int64_t rows = p.a.n_q / p.a.n_seqs;
   if (rows >= 1024 && rows / 256 * p.a.n_seqs * p.a.q_heads >= 512) return prompt_launch<TYPE, 128, 8>(p, vec);

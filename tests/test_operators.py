@@ -472,10 +472,20 @@ def test_attn_prompt(case, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("case", PROMPT_CASES, ids=str)
+def test_attn_prompt_among_many_rows(case, dtype):
+    """The same beside a long sequence that sees no key: calls of few rows and of many are worked on differently."""
+    nq, nk, hq, hk, D, causal, window = case
+    run_prompt(nq + [30_000 // hq], (nk or nq) + [0], hq, hk, D, dtype, causal, window)
+
+
+@gpu
 @pytest.mark.parametrize("strided", ["rows", "odd"])
 @pytest.mark.parametrize("D", [64, 128])
-def test_attn_prompt_strides(strided, D):
-    run_prompt([70, 33], [70, 90], 4, 2, D, BF, True, 0, strided=strided)
+@pytest.mark.parametrize("more", [0, 8000])
+def test_attn_prompt_strides(strided, D, more):
+    run_prompt([70, 33, more], [70, 90, 0], 4, 2, D, BF, True, 0, strided=strided)
 
 
 @gpu
@@ -489,16 +499,18 @@ def test_attn_prompt_hidden_values_have_no_effect(D, dtype):
         v[101, 1, 6] = math.inf
         v[102, 0, 7] = -math.inf
         k[149, 1] = math.nan
-    run_prompt([150], [150], 4, 2, D, dtype, True, 0, edit=edit)
-    run_prompt([40], [200], 4, 2, D, dtype, True, 30, edit=edit)  # behind the window
+    for more in (0, 8000):
+        run_prompt([150, more], [150, 0], 4, 2, D, dtype, True, 0, edit=edit)
+        run_prompt([40, more], [200, 0], 4, 2, D, dtype, True, 30, edit=edit)  # behind the window
 
     def rising(q, k, v):
         k *= torch.linspace(0, 6, k.shape[0])[:, None, None].to(k.dtype)
         q[:, :, 0] = 4
         k[:, :, 0] = torch.linspace(-30, 30, k.shape[0])[:, None].to(k.dtype)
-    run_prompt([180], [180], 2, 1, D, dtype, True, 0, edit=rising, scale=0.25)
-    run_prompt([40], [150], 2, 1, D, dtype, False, 0, scale=0.0)
-    run_prompt([40], [150], 2, 1, D, dtype, True, 0, scale=-0.1)
+    for more in (0, 16_000):
+        run_prompt([180, more], [180, 0], 2, 1, D, dtype, True, 0, edit=rising, scale=0.25)
+        run_prompt([40, more], [150, 0], 2, 1, D, dtype, False, 0, scale=0.0)
+        run_prompt([40, more], [150, 0], 2, 1, D, dtype, True, 0, scale=-0.1)
 
 
 LONG_CASES = [  # queries, keys, heads, kv heads, causal, window, values that are not finite
