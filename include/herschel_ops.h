@@ -133,9 +133,15 @@ typedef struct {
   int32_t causal;             /* query i of nq sees key j of nk iff j <= i + nk - nq */
   int32_t window;             /* > 0: and j > i + nk - nq - window; 0: no window */
   float scale;                /* of the scores; finite */
+  void *workspace;            /* herschel_attn_prompt_workspace() bytes, 16-byte aligned, no two calls at once; or */
+  size_t workspace_bytes;     /* NULL or fewer bytes: long keys are then not shared among more workgroups */
   uint32_t *status;
   void *hip_stream;
 } herschel_prompt_args;
+
+/* Bytes of workspace with which a call of these sizes is fastest; 0 for most. */
+int herschel_attn_prompt_workspace(int32_t n_seqs, int64_t n_q, int64_t n_k, int32_t max_q, int32_t q_heads,
+                                   int32_t kv_heads, int32_t head_dim, size_t *bytes);
 
 /* out = softmax over the keys seen of (scale q.k) times v.  A query that sees
  * no key has out 0 and lse -infinity.  Keys not seen have no effect, whatever

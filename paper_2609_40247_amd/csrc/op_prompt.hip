@@ -25,6 +25,8 @@
 //    key's exponential is 0, which an infinite or NaN value turns into NaN: a
 //    wave whose sums are not finite at the end computes its rows again, key by
 //    key, with nothing but the keys that each row sees.
+#include <algorithm>
+
 #include "ops.hpp"
 
 namespace hop {
@@ -40,7 +42,16 @@ struct PromptArgs {
   int group;
   int levels;  // query tiles of the longest sequence
   int spread;  // XCDs that share a key head's workgroups; 0: heads in turn
+  int splits;  // parts of each workgroup's keys (gridDim.y); above 1 they meet in k_prompt_join
 };
+
+// A row's part: sums of its values, reference and sum of its exponentials.
+template <int D>
+constexpr int PART_FLOATS = D + 4;
+template <int D>
+__device__ __forceinline__ float* row_part(const herschel_prompt_args& a, int part, int64_t at) {
+  return (float*)a.workspace + (part * (a.n_q * a.q_heads) + at) * PART_FLOATS<D>;
+}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 LdsHalves;
@@ -105,7 +116,7 @@ __device__ __forceinline__ void row_by_key(const uint16_t* q, const uint16_t* kb
   if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
 }
 
-template <int TYPE, int D, int WAVES, bool VEC>
+template <int TYPE, int D, int WAVES, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   constexpr int QROWS = 32 * WAVES, THREADS = WAVE * WAVES;
   const herschel_prompt_args& a = p.a;
@@ -155,8 +166,13 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   // the workgroup's
   const int last = min(row0 + QROWS, nq) - 1;
   const int wg_to = a.causal ? min(nk, max(0, last + shift + 1)) : nk;
-  const int wg_from = a.window > 0 ? min(wg_to, max(0, row0 + shift - a.window + 1)) / KT * KT : 0;
-  const int tiles = (wg_to - wg_from + KT - 1) / KT;
+  int wg_from = a.window > 0 ? min(wg_to, max(0, row0 + shift - a.window + 1)) / KT * KT : 0;
+  int tiles = (wg_to - wg_from + KT - 1) / KT;
+  if constexpr (SPLIT) {
+    const int begin = (int)((int64_t)tiles * blockIdx.y / p.splits);
+    tiles = (int)((int64_t)tiles * (blockIdx.y + 1) / p.splits) - begin;
+    wg_from += begin * KT;
+  }
   // keys outside these may be hidden from a row of this wave
   const int first_row = row0 + wave * 32;
   const int all_to = first_row + 32 > nq ? 0 : a.causal ? min(nk, max(0, first_row + shift + 1)) : nk;
@@ -366,6 +382,17 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   }
 
   sum += __shfl_xor(sum, 32);
+  if constexpr (SPLIT) {
+    if (row >= nq) return;
+    float* part = row_part<D>(a, blockIdx.y, (q0 + row) * a.q_heads + qh);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(part + 32 * d + 8 * i + 4 * g) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    if (g == 0) part[D] = ref, part[D + 1] = sum;
+    return;
+  }
   float check = sum - sum;  // 0, or NaN if a sum is not finite
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -407,7 +434,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
 // The next step's keys are asked for once the scores are there, its values after
 // the second product.
 constexpr int FEW_WAVES = 4;  // eight: 2048 keys 20 us against 23, but 512 rows 16.7 against 12.2
-template <int TYPE, int D, bool VEC>
+template <int TYPE, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p) {
   const herschel_prompt_args& a = p.a;
   constexpr int W = FEW_WAVES;
@@ -489,14 +516,20 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   };
   u32x4 k[LOADS], v[LOADS];
   const int vrow = 4 * g + lane % 16 / 4, vcol = 2 * (lane / 16 % 2) + lane % 4 / 2;
-  int k0 = any_from / 32 * 32 + wave * 32;
-  if (k0 < any_to) {
+  int begin = any_from / 32 * 32, end = any_to;
+  if constexpr (SPLIT) {
+    const int steps = max(0, end - begin + 31) / 32;
+    end = min(end, begin + 32 * (int)((int64_t)steps * (blockIdx.y + 1) / p.splits));
+    begin += 32 * (int)((int64_t)steps * blockIdx.y / p.splits);
+  }
+  int k0 = begin + wave * 32;
+  if (k0 < end) {
     load(k, kbase, a.k_strides.row, koff, k0);
     load(v, vbase, a.v_strides.row, voff, k0);
   }
 #pragma unroll
   for (int s = 0; s < NS; ++s) q[s] ^= sign;  // a negative scale goes into Q's signs: what is left is not negative
-  for (; k0 < any_to; k0 += 32 * W) {
+  for (; k0 < end; k0 += 32 * W) {
     f32x16 sc;
 #pragma unroll
     for (int i = 0; i < 16; ++i) sc[i] = 0;
@@ -509,7 +542,7 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
 #pragma unroll
     for (int s = 0; s < NS; ++s)
       sc = mfma32<TYPE>(*(const u32x4*)(my_k + n * (D * 2) + (((2 * s + g) ^ fk(n)) * 16)), q[s], sc);
-    const bool more = k0 + 32 * W < any_to;
+    const bool more = k0 + 32 * W < end;
     if (more) load(k, kbase, a.k_strides.row, koff, k0 + 32 * W);
     if (k0 + 32 > all_to || k0 < all_from) {
       const int lo = from - k0 - 4 * g, hi = to - k0 - 4 * g;
@@ -595,6 +628,18 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
     for (int i = 0; i < PART; ++i)
       acc[i] += ((const float*)((wave < W / 2 ? s_k : s_v) + w * BYTES))[(wave % (W / 2) * PART + i) * WAVE + lane] * by;
   }
+  const int64_t at = (q0 + tok) * a.q_heads + qh;
+  if constexpr (SPLIT) {
+    if (row0 + n >= rows) return;
+    float* part = row_part<D>(a, blockIdx.y, at);
+#pragma unroll
+    for (int i = 0; i < PART; i += 4) {
+      const int x = wave * PART + i;
+      *(f32x4*)(part + 32 * (x / 16) + 8 * (x % 16 / 4) + 4 * g) = f32x4{acc[i], acc[i + 1], acc[i + 2], acc[i + 3]};
+    }
+    if (g == 0 && wave == 0) part[D] = top, part[D + 1] = den;
+    return;
+  }
   float check = den - den;  // 0, or NaN if a sum is not finite
 #pragma unroll
   for (int i = 0; i < PART; ++i) check += acc[i] - acc[i];
@@ -608,7 +653,6 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   }
   if (row0 + n >= rows) return;
   const float inv = den > 0 ? 1.0f / den : 0.0f;  // no key seen: 0
-  const int64_t at = (q0 + tok) * a.q_heads + qh;
 #pragma unroll
   for (int i = 0; i < PART; i += 4) {  // four dimensions in order
     const int x = wave * PART + i;
@@ -618,13 +662,86 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   if (a.lse && g == 0 && wave == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
 }
 
+// Joins the parts of each row: a wave per row, four rows in turn.
+constexpr int JOIN_ROWS = 16;
+constexpr int MAX_SPLITS = 16;
+template <int TYPE, int D>
+__global__ __launch_bounds__(256) void k_prompt_join(PromptArgs p) {
+  const herschel_prompt_args& a = p.a;
+  constexpr int ND = D / WAVE;
+  const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+  const int b = (int)(blockIdx.x % a.n_seqs);
+  const int64_t x0 = (int64_t)(blockIdx.x / a.n_seqs) * JOIN_ROWS;
+  // lengths taken as the nearest valid
+  const int64_t q0 = min(max((int64_t)a.cu_q[b], (int64_t)0), a.n_q), q1 = min(max((int64_t)a.cu_q[b + 1], q0), a.n_q);
+  const int64_t kk0 = min(max((int64_t)a.cu_k[b], (int64_t)0), a.n_k), kk1 = min(max((int64_t)a.cu_k[b + 1], kk0), a.n_k);
+  const int64_t rows = min(q1 - q0, (int64_t)a.max_q) * a.q_heads;
+  const int nk = (int)(kk1 - kk0), shift = nk - (int)(q1 - q0);
+  for (int64_t x = x0 + wave; x < min(x0 + JOIN_ROWS, rows); x += 4) {
+    const int64_t at = q0 * a.q_heads + x;
+    float r = NO_KEY, t = 0;
+    if (lane < p.splits) {
+      const float* part = row_part<D>(a, lane, at);
+      r = part[D], t = part[D + 1];
+    }
+    float v[MAX_SPLITS][ND];
+#pragma unroll
+    for (int i = 0; i < MAX_SPLITS; ++i)
+      if (i < p.splits)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) v[i][d] = row_part<D>(a, i, at)[lane * ND + d];
+    float top = r;
+#pragma unroll
+    for (int m = 1; m < MAX_SPLITS; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    top = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, top)));
+    const float by = __builtin_amdgcn_exp2f(r - top);
+    float den = 0, acc[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[d] = 0;
+#pragma unroll
+    for (int i = 0; i < MAX_SPLITS; ++i)
+      if (i < p.splits) {
+        const float f = __shfl(by, i);
+        den += __shfl(t, i) * f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) acc[d] += v[i][d] * f;
+      }
+    float check = den - den;  // 0, or NaN if a sum is not finite
+#pragma unroll
+    for (int d = 0; d < ND; ++d) check += acc[d] - acc[d];
+    if (__ballot(!(check == 0))) {
+      const int tok = (int)(x / a.q_heads), qh = (int)(x % a.q_heads), kh = qh / p.group;
+      row_by_key<TYPE, D>((const uint16_t*)a.q + (q0 + tok) * a.q_strides.row + qh * a.q_strides.head,
+                          (const uint16_t*)a.k + kk0 * a.k_strides.row + kh * a.k_strides.head,
+                          (const uint16_t*)a.v + kk0 * a.v_strides.row + kh * a.v_strides.head, a,
+                          a.window > 0 ? max(0, tok + shift - a.window + 1) : 0,
+                          a.causal ? min(nk, max(0, tok + shift + 1)) : nk, at);
+      continue;
+    }
+    const float inv = den > 0 ? 1.0f / den : 0.0f;  // no key seen: 0
+    uint16_t* out = (uint16_t*)a.out + at * D + lane * ND;
+    if constexpr (ND == 2) *(uint32_t*)out = pack2<TYPE>(acc[0] * inv, acc[1] * inv);
+    else *out = (uint16_t)pack2<TYPE>(acc[0] * inv, 0.0f);
+    if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+  }
+}
+
+template <int TYPE, int D>
+static int prompt_join(PromptArgs& p) {
+  const int64_t blocks = ((int64_t)p.a.max_q * p.a.q_heads + JOIN_ROWS - 1) / JOIN_ROWS * p.a.n_seqs;
+  if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
+  return launch(k_prompt_join<TYPE, D>, dim3((unsigned)blocks), dim3(256), 0, p.a.hip_stream, p);
+}
+
 template <int TYPE, int D>
 static int prompt_few(PromptArgs& p, bool vec) {
   const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, blocks = levels * p.a.n_seqs * p.a.kv_heads;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
   p.levels = (int)levels;
-  return launch(vec ? k_prompt_few<TYPE, D, true> : k_prompt_few<TYPE, D, false>, dim3((unsigned)blocks),
-                dim3(FEW_WAVES * WAVE), 0, p.a.hip_stream, p);
+  auto kernel = vec ? p.splits > 1 ? k_prompt_few<TYPE, D, true, true> : k_prompt_few<TYPE, D, true, false>
+                    : p.splits > 1 ? k_prompt_few<TYPE, D, false, true> : k_prompt_few<TYPE, D, false, false>;
+  const int rc = launch(kernel, dim3((unsigned)blocks, p.splits), dim3(FEW_WAVES * WAVE), 0, p.a.hip_stream, p);
+  return rc == HERSCHEL_OK && p.splits > 1 ? prompt_join<TYPE, D>(p) : rc;
 }
 
 template <int TYPE, int D, int WAVES>
@@ -636,47 +753,114 @@ static int prompt_launch(PromptArgs& p, bool vec) {
   int64_t blocks = (int64_t)p.levels * p.a.n_seqs * p.a.q_heads;
   if (p.spread) blocks = (blocks / (G < 8 ? G : 8) + p.spread - 1) / p.spread * 8;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
-  return launch(vec ? k_prompt<TYPE, D, WAVES, true> : k_prompt<TYPE, D, WAVES, false>, dim3((unsigned)blocks),
+  if constexpr (WAVES == 4)
+    if (p.splits > 1) {
+      const int rc = launch(vec ? k_prompt<TYPE, D, 4, true, true> : k_prompt<TYPE, D, 4, false, true>,
+                            dim3((unsigned)blocks, p.splits), dim3(4 * WAVE), 0, p.a.hip_stream, p);
+      return rc == HERSCHEL_OK ? prompt_join<TYPE, D>(p) : rc;
+    }
+  return launch(vec ? k_prompt<TYPE, D, WAVES, true, false> : k_prompt<TYPE, D, WAVES, false, false>, dim3((unsigned)blocks),
                 dim3(WAVES * WAVE), 0, p.a.hip_stream, p);
 }
 
+// What a call runs as, from its sizes and types alone (lengths are on the device:
+// sequences count as their mean).
+//
 // Few rows: as long as 32 of them (of one key head) a workgroup make no more
-// workgroups than the card holds at once, about 20,000 in all (24 x 16 rows of 16
-// heads of 64 4.7 us against 5.7, 24 x 64 6.2 against 6.6; 24 x 128 11.6 against
-// 9.3, 1024 rows of 32 heads of 128 27.0 against 26.4).
+// workgroups than the card holds at once, about 20,000 rows in all (24 x 16 rows
+// of 16 heads of 64 4.7 us against 5.7, 24 x 64 6.2 against 6.6; 24 x 128 11.6
+// against 9.3, 1024 rows of 32 heads of 128 27.0 against 26.4).  Over many keys
+// workgroups of 128 rows read them fewer times, so rows times keys times dimensions
+// have a limit too (of 128, 4 x 64 rows of 32 heads over 4096 keys, 4.3e9, 44
+// against 49, 512 rows, 8.6e9, 57 against 51; 777 rows of 8 heads over 12000 83
+// against 64; of 64, 4096 rows of 4 heads, 4.3e9, 27 against 35).
+//
 // Else eight waves (256 rows) or four (128).  Eight in turns are faster where there
 // is enough for every CU twice over: 4096 rows of 32 heads of 128 145 us against
 // 156, 8192 983 against 1080; below, what counts is more and smaller workgroups:
 // 512 rows 23 against 18 us, 8 heads of 4096 95 against 83.  With heads of 64
 // the exponentials take longer than the products and turns lose (4096 rows
 // twice: 186 against 175 us).
+//
+// Parts: where the workgroups would not fill the card and keys are many, each
+// workgroup's keys go to several.  The second launch and the parts' way through
+// memory take 5 to 10 us.  Of few rows, four parts or more unless keys are very
+// many: 16 rows of 32 heads over 2048 keys 15.4 us against 22.5, over 8192 21.6
+// against 77; in two parts 2048 rows of 4 heads would take 27 against 23.  Of many,
+// from 4096 keys on, to fill the card's places for workgroups once, or twice in up
+// to four parts: 8192 rows of 4 heads 108 against 153, 4096 of 8 71 against 80, 512
+// of 32 over 8192 keys 82 against 153 (in eight parts 93); 2048 rows of 16 heads
+// would take 53 against 44.
+struct PromptPlan {
+  int waves;  // 0: few rows
+  int splits;
+  size_t bytes;
+};
+static PromptPlan prompt_plan(int64_t n_seqs, int64_t n_q, int64_t n_k, int64_t max_q, int64_t q_heads, int64_t kv_heads, int D) {
+  PromptPlan plan{4, 1, 0};
+  const int64_t rows = std::max<int64_t>(1, n_q / n_seqs), keys = n_k / n_seqs;
+  int64_t splits = 1;
+  if (n_q * q_heads <= 20480 && n_q * q_heads * keys <= (5ll << 30) / D && max_q * (q_heads / kv_heads) < 0x7fffffe0) {
+    plan.waves = 0;
+    splits = std::min<int64_t>(512 / std::max<int64_t>(1, (n_q * q_heads + 31) / 32), keys / 512);
+    if (splits < 4 && keys < 8192) splits = 1;
+  } else if (D == 128 && rows >= 1024 && rows / 256 * n_seqs * q_heads >= 512) {
+    plan.waves = 8;
+  } else if (keys >= 4096) {
+    const int64_t groups = (rows + 127) / 128 * n_seqs * q_heads;
+    splits = std::min(std::max(512 / groups, std::min<int64_t>(1024 / groups, 4)), keys / 1024);
+  }
+  if (splits > 1) {
+    plan.splits = (int)std::min<int64_t>(splits, MAX_SPLITS);
+    plan.bytes = (size_t)plan.splits * n_q * q_heads * (D + 4) * 4;
+  }
+  return plan;
+}
+
+template <int TYPE, int D>
+static int prompt_size(PromptArgs& p, const PromptPlan& plan, bool vec) {
+  if (plan.waves == 0) return prompt_few<TYPE, D>(p, vec);
+  if constexpr (D == 128)
+    if (plan.waves == 8) return prompt_launch<TYPE, 128, 8>(p, vec);
+  return prompt_launch<TYPE, D, 4>(p, vec);
+}
 template <int TYPE>
-static int prompt_size(PromptArgs& p, bool vec) {
-  if (p.a.n_q * p.a.q_heads <= 20480 && (int64_t)p.a.max_q * p.group < 0x7fffffe0)
-    return p.a.head_dim == 64 ? prompt_few<TYPE, 64>(p, vec) : prompt_few<TYPE, 128>(p, vec);
-  if (p.a.head_dim == 64) return prompt_launch<TYPE, 64, 4>(p, vec);
-  const int64_t rows = p.a.n_q / p.a.n_seqs;
-  if (rows >= 1024 && rows / 256 * p.a.n_seqs * p.a.q_heads >= 512) return prompt_launch<TYPE, 128, 8>(p, vec);
-  return prompt_launch<TYPE, 128, 4>(p, vec);
+static int prompt_dim(PromptArgs& p, const PromptPlan& plan, bool vec) {
+  return p.a.head_dim == 64 ? prompt_size<TYPE, 64>(p, plan, vec) : prompt_size<TYPE, 128>(p, plan, vec);
+}
+
+static bool prompt_sizes_ok(int32_t n_seqs, int64_t n_q, int64_t n_k, int32_t max_q, int32_t q_heads, int32_t kv_heads, int32_t head_dim) {
+  return n_seqs >= 1 && n_q >= 0 && n_k >= 0 && max_q >= 0 && n_q <= 0x7fffffff && n_k <= 0x7fffffff &&
+         (head_dim == 64 || head_dim == 128) && kv_heads >= 1 && q_heads >= 1 && q_heads % kv_heads == 0;
 }
 
 }  // namespace hop
+
+extern "C" int herschel_attn_prompt_workspace(int32_t n_seqs, int64_t n_q, int64_t n_k, int32_t max_q, int32_t q_heads,
+                                              int32_t kv_heads, int32_t head_dim, size_t* bytes) {
+  using namespace hop;
+  if (!bytes || !prompt_sizes_ok(n_seqs, n_q, n_k, max_q, q_heads, kv_heads, head_dim)) return HERSCHEL_EINVAL;
+  *bytes = prompt_plan(n_seqs, n_q, n_k, max_q, q_heads, kv_heads, head_dim).bytes;
+  return HERSCHEL_OK;
+}
 
 extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
   using namespace hop;
   if (!args) return HERSCHEL_EINVAL;
   const herschel_prompt_args& a = *args;
-  if (a.n_seqs < 1 || a.n_q < 0 || a.n_k < 0 || a.max_q < 0 || a.n_q > 0x7fffffff || a.n_k > 0x7fffffff) return HERSCHEL_EINVAL;
-  if (a.head_dim != 64 && a.head_dim != 128) return HERSCHEL_EINVAL;
-  if (a.kv_heads < 1 || a.q_heads < 1 || a.q_heads % a.kv_heads || !type_ok(a.type)) return HERSCHEL_EINVAL;
+  if (!prompt_sizes_ok(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim) || !type_ok(a.type))
+    return HERSCHEL_EINVAL;
+  if (a.workspace && !aligned(a.workspace, 16)) return HERSCHEL_EWORKSPACE;
   if (a.window < 0 || !isfinite(a.scale) || !a.cu_q || !a.cu_k) return HERSCHEL_EINVAL;
   if (!strides_ok(a.q_strides) || !strides_ok(a.k_strides) || !strides_ok(a.v_strides)) return HERSCHEL_EINVAL;
   if ((a.n_q && (!a.q || !a.out || !aligned(a.q, 2) || !aligned(a.out, 8))) ||
       (a.n_k && (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2))))
     return HERSCHEL_EINVAL;
   if (a.n_q == 0 || a.max_q == 0) return HERSCHEL_OK;
-  PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0};
+  PromptPlan plan = prompt_plan(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim);
+  if (!a.workspace || a.workspace_bytes < plan.bytes) plan.splits = 1;
+  PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0, plan.splits};
   // 16-byte loads, and a tile's rows within 31 bits of bytes
   const bool vec = a.k_strides.row < (1 << 23) && a.v_strides.row < (1 << 23) && chunks_aligned(a.q, a.q_strides) && chunks_aligned(a.k, a.k_strides) && chunks_aligned(a.v, a.v_strides);
-  return a.type == HERSCHEL_BF16 ? prompt_size<HERSCHEL_BF16>(p, vec) : prompt_size<HERSCHEL_F16>(p, vec);
+  return a.type == HERSCHEL_BF16 ? prompt_dim<HERSCHEL_BF16>(p, plan, vec) : prompt_dim<HERSCHEL_F16>(p, plan, vec);
 }

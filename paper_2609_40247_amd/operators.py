@@ -18,6 +18,7 @@ There is no CPU fallback: without the built library or a GPU the calls raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import struct
 
@@ -65,7 +66,7 @@ class HerschelPromptArgs(ctypes.Structure):
                 ("v_strides", _Strides), ("out", _P), ("lse", _P), ("cu_q", _P), ("cu_k", _P), ("n_seqs", _I32),
                 ("n_q", _I64), ("n_k", _I64), ("max_q", _I32), ("q_heads", _I32), ("kv_heads", _I32),
                 ("head_dim", _I32), ("type", _I32), ("causal", _I32), ("window", _I32), ("scale", ctypes.c_float),
-                ("status", _P), ("hip_stream", _P)]
+                ("workspace", _P), ("workspace_bytes", ctypes.c_size_t), ("status", _P), ("hip_stream", _P)]
 
 
 class HerschelDecodeArgs(ctypes.Structure):
@@ -79,7 +80,7 @@ class HerschelDecodeArgs(ctypes.Structure):
 # instead of 1 to 2, and a decode step's calls are as short as their host time.
 _ROPE = struct.Struct("@3P6q2P4q2PqPq6i2P")
 _READ = struct.Struct("@PqPiq2Pi2P")
-_PROMPT = struct.Struct("@3P6q4Pi2q7if2P")
+_PROMPT = struct.Struct("@3P6q4Pi2q7ifPN2P")
 _DECODE = struct.Struct("@P3q3PqP5ifPN2P")
 
 _ready = {}
@@ -94,6 +95,9 @@ def load(variant: str | None = None) -> ctypes.CDLL:
                         ("herschel_attn_decode", 2)):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = ctypes.c_int, [_P] * n
+        lib.herschel_attn_prompt_workspace.restype = ctypes.c_int
+        lib.herschel_attn_prompt_workspace.argtypes = [_I32, _I64, _I64, _I32, _I32, _I32, _I32,
+                                                       ctypes.POINTER(ctypes.c_size_t)]
         lib.herschel_attn_decode_workspace.restype = ctypes.c_int
         lib.herschel_attn_decode_workspace.argtypes = [_I32, _I32, _I32, _P, ctypes.POINTER(ctypes.c_size_t)]
         if variant:
@@ -357,6 +361,14 @@ def cache_read(cache: PagedCache, block_table: torch.Tensor, cu: torch.Tensor, *
     return k_out, v_out
 
 
+@functools.lru_cache(maxsize=1024)
+def _prompt_workspace(lib, *sizes) -> int:
+    """Bytes of workspace for a call of these sizes (0: none)."""
+    size = ctypes.c_size_t(0)
+    lib.herschel_attn_prompt_workspace(*sizes, ctypes.byref(size))
+    return int(size.value)
+
+
 def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor | None = None,
                 *, max_q: int, scale: float | None = None, causal: bool = True, window: int = 0,
                 return_lse: bool = False, out: torch.Tensor | None = None, status: torch.Tensor | None = None, lib=None):
@@ -384,12 +396,16 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     else:
         to = _ints(out, "out", q.dtype, q.shape, dev)
     lse = q.new_empty((n_q, heads), dtype=torch.float32) if return_lse else None
+    lib, n_seqs = lib or _lib(), cu_q.shape[0] - 1
+    size = _prompt_workspace(lib, n_seqs, n_q, n_k, max_q, heads, kv_heads, D)
+    workspace = q.new_empty(size, dtype=torch.uint8) if size else None
     args = _PROMPT.pack(
         q.data_ptr(), k.data_ptr(), v.data_ptr(), sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
         to, lse.data_ptr() if return_lse else 0, from_q, from_k,
-        cu_q.shape[0] - 1, n_q, n_k, max_q, heads, kv_heads, D, TYPES[q.dtype], bool(causal), window,
-        D ** -0.5 if scale is None else scale, 0 if status is None else _status(status, dev), _stream(dev))
-    _call((lib or _lib()).herschel_attn_prompt, dev, "attn_prompt", args)
+        n_seqs, n_q, n_k, max_q, heads, kv_heads, D, TYPES[q.dtype], bool(causal), window,
+        D ** -0.5 if scale is None else scale, workspace.data_ptr() if size else 0, size,
+        0 if status is None else _status(status, dev), _stream(dev))
+    _call(lib.herschel_attn_prompt, dev, "attn_prompt", args)
     return (out, lse) if return_lse else out
 
 

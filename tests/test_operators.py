@@ -553,6 +553,93 @@ def test_attn_prompt_long(case, dtype):
         at_q, at_k = at_q + n, at_k + m
 
 
+PART_CASES = [  # queries, keys, heads, kv heads, D, causal, window, strided
+    ([3, 40, 0], [2100, 6000, 9], 8, 2, 128, True, 0, False),
+    ([64], [2500], 4, 1, 64, True, 0, "rows"),
+    ([1, 70], [4100, 30], 5, 1, 64, False, 1000, False),
+    ([33], [9000], 16, 4, 128, True, 3, "odd"),             # parts without a key
+]
+MANY_PART_CASES = [  # workgroups of 128 rows
+    ([530], [5200], 16, 2, 128, True, 0, False, BF),
+    ([1900, 100], [8300, 100], 11, 11, 64, True, 2600, "rows", HF),
+    ([1350], [4100], 8, 1, 128, False, 0, "odd", BF),
+]
+
+
+def splits_of(nq, nk, hq, hk, D):
+    """Bytes of workspace in parts of a row."""
+    size = ctypes.c_size_t(0)
+    assert lib().herschel_attn_prompt_workspace(len(nq), sum(nq), sum(nk), max(nq), hq, hk, D, ctypes.byref(size)) == H.OK
+    return size.value / (sum(nq) * hq * (D + 4) * 4)
+
+
+def test_attn_prompt_workspace_is_for_few_rows_over_many_keys():
+    for nq, nk, hq, hk, D, *_ in PART_CASES + MANY_PART_CASES:
+        assert splits_of(nq, nk, hq, hk, D) in range(2, 17)
+    assert splits_of([4096], [4096], 32, 8, 128) == 0
+    assert splits_of([100], [100], 32, 8, 128) == 0
+    size = ctypes.c_size_t(0)
+    for bad in ((0, 1, 1, 1, 1, 1, 64), (1, -1, 1, 1, 1, 1, 64), (1, 1, 1, 1, 3, 2, 64), (1, 1, 1, 1, 1, 1, 96)):
+        assert lib().herschel_attn_prompt_workspace(*bad, ctypes.byref(size)) == H.EINVAL
+    assert lib().herschel_attn_prompt_workspace(1, 1, 1, 1, 1, 1, 64, None) == H.EINVAL
+    assert lib().herschel_attn_prompt(ctypes.byref(prompt_args(workspace=FAKE + 8, workspace_bytes=1 << 30))) == H.EWORKSPACE
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("case", PART_CASES, ids=str)
+def test_attn_prompt_in_parts(case, dtype):
+    nq, nk, hq, hk, D, causal, window, strided = case
+    run_prompt(nq, nk, hq, hk, D, dtype, causal, window, strided=strided)
+
+
+@gpu
+@pytest.mark.parametrize("case", MANY_PART_CASES, ids=str)
+def test_attn_prompt_of_many_rows_in_parts(case):
+    nq, nk, hq, hk, D, causal, window, strided, dtype = case
+    run_prompt(nq, nk, hq, hk, D, dtype, causal, window, strided=strided)
+
+
+@gpu
+def test_attn_prompt_in_parts_hidden_values_have_no_effect():
+    def edit(q, k, v):
+        v[2100, 0, 5] = math.nan
+        v[4099, 0, 6] = math.inf
+        v[10, 1, 7] = -math.inf
+        k[4098, 1] = math.nan
+    run_prompt([40], [4100], 4, 2, 128, BF, True, 0, edit=edit)
+    run_prompt([40], [4100], 4, 2, 64, HF, True, 4000, edit=edit)
+    run_prompt([1400], [4100], 8, 2, 128, HF, True, 0, edit=edit)
+
+
+@gpu
+def test_attn_prompt_in_parts_in_a_graph_and_without_workspace(monkeypatch):
+    q, k, v = (rand(n, h, 128, seed=i).to(DEV) for i, (n, h) in enumerate(((50, 8), (5000, 2), (5000, 2))))
+    cu_q, cu_k = (torch.tensor([0, n], dtype=torch.int32, device=DEV) for n in (50, 5000))
+    call = lambda: O.attn_prompt(q, k, v, cu_q, cu_k, max_q=50)
+    eager = call()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        out = call()
+    for step in range(4):
+        q.copy_(rand(50, 8, 128, seed=20 + step))
+        eager = call()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+    monkeypatch.setattr(O, "_prompt_workspace", lambda *a: 0)
+    whole = call()
+    ref = exact_attention(q.cpu(), k.cpu(), v.cpu(), 128 ** -0.5, True, 0)
+    for got in (eager, whole):
+        check_attention(got, None, ref, BF, U[BF], 5000, 128)
+
+
 @gpu
 def test_attn_prompt_faults():
     q = rand(40, 2, 64).to(DEV)
