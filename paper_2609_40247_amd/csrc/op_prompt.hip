@@ -278,17 +278,25 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
     }
     reads_ahead<2 * NS, 1, 0>();
   };
-  auto softmax = [&](int t) INLINE {
+  // a wave's first tile moves the reference in any case
+  auto softmax = [&](int t, bool first) INLINE {
     if (masked(t)) {
       const int k0 = wg_from + t * KT, lo = from - k0 - 4 * g, hi = to - k0 - 4 * g;
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
         const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
-        sc[i / 16][i % 16] = c < hi && c >= lo ? sc[i / 16][i % 16] : -INFINITY;
+        sc[i / 16][i % 16] = c < hi ? sc[i / 16][i % 16] : -INFINITY;
       }
+      if (a.window > 0)
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const int c = 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4;
+          sc[i / 16][i % 16] = c >= lo ? sc[i / 16][i % 16] : -INFINITY;
+        }
     }
-    float s = exponentials();
-    if (__ballot(!(s <= LARGE))) {
+    float s = 0;
+    if (!first) s = exponentials();
+    if (first || __ballot(!(s <= LARGE))) {
       float top = sc[0][0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
@@ -326,6 +334,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
       load_v(0, s_v);
       if (tiles > 1) load_k(1, s_k + KBYTES);
       meet(tiles > 1 ? KL : 0);
+      bool first = true;
       // Tile t, from kc and vc, while later tiles are copied to kn and vn: the
       // pointers' restrict is what lets reads pass copies still under way.
       auto work = [&](int t, const char* __restrict kc, const char* __restrict vc, char* __restrict kn,
@@ -334,8 +343,9 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
         if (t + 2 < tiles) load_k(t + 2, kn);
         if (!hidden(t)) {
           scores(kc);
-          softmax(t);
+          softmax(t, first);
           product(vc);
+          first = false;
         }
       };
       int kb0 = 0, kb1 = 1, kb2 = 2;  // K's buffers of tiles t, t + 1, t + 2
@@ -355,7 +365,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
       meet(0);
       if (!hidden(0)) {
         scores(s_k);
-        softmax(0);
+        softmax(0, true);
       }
       // The first four waves (one a SIMD) and the last four take turns: while one
       // half runs the products of a step, the other runs the exponentials.
@@ -370,7 +380,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
         meet(-1);
         if (t + 3 < tiles) load_k(t + 3, s_k + b0 * KBYTES);
         if (t + 2 < tiles) load_v(t + 2, s_v + b2 * KBYTES);
-        if (t + 1 < tiles && !hidden(t + 1)) softmax(t + 1);
+        if (t + 1 < tiles && !hidden(t + 1)) softmax(t + 1, false);
         meet(0);
         const int x = b0;
         b0 = b1;
@@ -549,8 +559,11 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int c = 8 * (i / 4) + i % 4;
-        sc[i] = c < hi && c >= lo ? sc[i] : -INFINITY;
+        sc[i] = c < hi ? sc[i] : -INFINITY;
       }
+      if (a.window > 0)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sc[i] = 8 * (i / 4) + i % 4 >= lo ? sc[i] : -INFINITY;
     }
     u32x4 pb[2];
     auto exponentials = [&]() INLINE {
@@ -564,8 +577,10 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
       }
       return s;
     };
-    float t = exponentials();
-    if (__ballot(!(t <= LARGE))) {
+    const bool first = k0 == begin + wave * 32;  // moves the reference in any case
+    float t = 0;
+    if (!first) t = exponentials();
+    if (first || __ballot(!(t <= LARGE))) {
       float top = sc[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
