@@ -59,8 +59,7 @@ struct DecodeArgs {
 
 // The first tile of a sequence that the window reaches, and its tiles.
 __device__ __forceinline__ int first_tile(const DecodeArgs& p, int len) {
-  const int lo = p.a.window > 0 ? len - p.a.new_tokens - p.a.window + 1 : 0;
-  return lo > 0 ? lo / TILE : 0;
+  return window_from(len - p.a.new_tokens, p.a.window) / TILE;
 }
 __device__ __forceinline__ int seq_len(const DecodeArgs& p, int b, bool report) {
   const int len = p.a.seq_lens[b];
@@ -181,7 +180,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeAr
       const int r = row0 + rb * 16 + m;
       const int tok = r < p.rows ? r / p.group : 0, qh = head * p.group + (r < p.rows ? r % p.group : 0);
       seen_to[rb] = len - p.a.new_tokens + tok + 1;  // keys before this
-      seen_from[rb] = p.a.window > 0 ? seen_to[rb] - p.a.window : 0;
+      seen_from[rb] = window_from(seen_to[rb] - 1, p.a.window);
       const uint16_t* src = (const uint16_t*)p.a.q + b * p.a.q_seq_stride + tok * p.a.q_strides.row + qh * p.a.q_strides.head;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
@@ -200,8 +199,8 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeAr
     }
     const int key_begin = (first_tile(p, len) + tile) * TILE, key_end = min(len, key_begin + n_tiles * TILE);
     // keys that every row sees need no mask; those that some row sees are read
-    const int all_to = len - p.a.new_tokens + 1, all_from = p.a.window > 0 ? len - p.a.window : 0;
-    const int any_from = max(0, p.a.window > 0 ? len - p.a.new_tokens - p.a.window + 1 : 0);
+    const int all_to = len - p.a.new_tokens + 1, all_from = window_from(len - 1, p.a.window);
+    const int any_from = window_from(len - p.a.new_tokens, p.a.window);
 
     struct Step {
       u32x4 k[2][CB == 2 ? NS : NS / 2];

@@ -162,11 +162,11 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   // this lane's query row, and the keys it sees: [from, to)
   const int row = row0 + wave * 32 + n;
   const int to = row >= nq ? 0 : a.causal ? min(nk, max(0, row + shift + 1)) : nk;
-  const int from = a.window > 0 ? max(0, row + shift - a.window + 1) : 0;
+  const int from = window_from(row + shift, a.window);
   // the workgroup's
   const int last = min(row0 + QROWS, nq) - 1;
   const int wg_to = a.causal ? min(nk, max(0, last + shift + 1)) : nk;
-  int wg_from = a.window > 0 ? min(wg_to, max(0, row0 + shift - a.window + 1)) / KT * KT : 0;
+  int wg_from = min(wg_to, window_from(row0 + shift, a.window)) / KT * KT;
   int tiles = (wg_to - wg_from + KT - 1) / KT;
   if constexpr (SPLIT) {
     const int begin = (int)((int64_t)tiles * blockIdx.y / p.splits);
@@ -176,10 +176,10 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   // keys outside these may be hidden from a row of this wave
   const int first_row = row0 + wave * 32;
   const int all_to = first_row + 32 > nq ? 0 : a.causal ? min(nk, max(0, first_row + shift + 1)) : nk;
-  const int all_from = a.window > 0 ? max(0, first_row + 31 + shift - a.window + 1) : 0;
+  const int all_from = window_from(first_row + 31 + shift, a.window);
   // keys outside these are hidden from all rows of the wave
   const int any_to = a.causal ? min(nk, max(0, first_row + 32 + shift)) : nk;
-  const int any_from = a.window > 0 ? max(0, first_row + shift - a.window + 1) : 0;
+  const int any_from = window_from(first_row + shift, a.window);
 
   // A negative scale goes into Q's signs: what is left is not negative.
   u32x4 q[NS];
@@ -475,7 +475,7 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   // this lane's row (the last one again past it), and the keys it sees: [from, to)
   const int row = min(row0 + n, rows - 1), tok = row / p.group, qh = kh * p.group + row % p.group;
   auto sees_to = [&](int t) INLINE { return a.causal ? min(nk, max(0, t + shift + 1)) : nk; };
-  auto sees_from = [&](int t) INLINE { return a.window > 0 ? max(0, t + shift - a.window + 1) : 0; };
+  auto sees_from = [&](int t) INLINE { return window_from(t + shift, a.window); };
   const int to = sees_to(tok), from = sees_from(tok);
   // the workgroup's
   const int first = row0 / p.group, last = min(row0 + 31, rows - 1) / p.group;
@@ -729,7 +729,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs p) {
       row_by_key<TYPE, D>((const uint16_t*)a.q + (q0 + tok) * a.q_strides.row + qh * a.q_strides.head,
                           (const uint16_t*)a.k + kk0 * a.k_strides.row + kh * a.k_strides.head,
                           (const uint16_t*)a.v + kk0 * a.v_strides.row + kh * a.v_strides.head, a,
-                          a.window > 0 ? max(0, tok + shift - a.window + 1) : 0,
+                          window_from(tok + shift, a.window),
                           a.causal ? min(nk, max(0, tok + shift + 1)) : nk, at);
       continue;
     }

@@ -107,6 +107,9 @@ __device__ __forceinline__ uint32_t not_finite2(uint32_t w) {
   return ((w & E) == E ? 0xffffu : 0u) | (((w >> 16) & E) == E ? 0xffff0000u : 0u);
 }
 
+// The first key that a window of w keys up to key x holds (w 0: no window); for any w, as x - w may pass 32 bits.
+__device__ __forceinline__ int window_from(int x, int w) { return w > 0 && x >= w ? x - w + 1 : 0; }
+
 __device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) {
   if (status) atomicOr(status, bit);
 }

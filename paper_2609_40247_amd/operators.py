@@ -389,7 +389,7 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     from_q = _ints(cu_q, "cu_q", torch.int32, cu_q.shape, dev)
     from_k = from_q if cu_k is None else _ints(cu_k, "cu_k", torch.int32, cu_q.shape, dev)
     _need(0 <= max_q <= n_q, "max_q must be a number of q's rows")
-    _need(window >= 0, "window must not be negative")
+    _need(0 <= window < 2 ** 31, "window must be 0 or a number of keys below 2^31")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
@@ -445,7 +445,7 @@ class DecodeAttention:
         _need(1 <= B <= self.batch and shape == (B, self.new_tokens, self.heads, c.head_dim),
               "q must have the sizes that the workspace is for")
         table, lens = _table(block_table, B, dev), _ints(seq_lens, "seq_lens", torch.int32, (B,), dev)
-        _need(window >= 0, "window must not be negative")
+        _need(0 <= window < 2 ** 31, "window must be 0 or a number of keys below 2^31")
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
             to = out.data_ptr()

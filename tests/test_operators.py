@@ -664,6 +664,16 @@ def test_attn_prompt_faults():
     assert O.attn_prompt(q[:0], q[:0], q[:0], torch.tensor([0, 0], dtype=torch.int32, device=DEV), max_q=0).shape == (0, 2, 64)
 
 
+@gpu
+@pytest.mark.parametrize("case", [([100, 5, 140], [40, 0, 139], 2, 1, 64, False), ([300], [200], 4, 4, 128, False),
+                                  ([300], [200], 4, 1, 128, True)], ids=str)
+def test_attn_prompt_widest_windows(case):
+    """Windows that reach below the first key by nearly 2^31: the same as none, also with more queries than keys."""
+    nq, nk, hq, hk, D, causal = case
+    for window in (2 ** 31 - 1, 2 ** 31 - 100):
+        run_prompt(nq, nk, hq, hk, D, BF, causal, window)
+
+
 # ------------------------------------------------------------ decode
 def run_decode(lens, hq, hk, D, dtype, kind, page, new=1, window=0, edit=None, strided=False, seed=0, scale=None):
     B = len(lens)
@@ -709,6 +719,15 @@ DECODE_CASES = [  # lengths, heads, kv heads, D, page, new, window
 def test_attn_decode(case, dtype, kind):
     lens, hq, hk, D, page, new, window = case
     run_decode(lens, hq, hk, D, dtype, kind, page, new, window)
+
+
+@gpu
+@pytest.mark.parametrize("kind", [BF, F8], ids=str)
+def test_attn_decode_widest_windows(kind):
+    """Windows that reach below the first key by nearly 2^31, with fewer cached tokens than new ones."""
+    for window in (2 ** 31 - 1, 2 ** 31 - 3):
+        run_decode([3, 0, 130, 2, 64], 8, 2, 128, BF, kind, 16, 4, window)
+        run_decode([700, 1], 4, 2, 64, BF, kind, 16, 1, window)
 
 
 @gpu
@@ -1060,3 +1079,15 @@ def test_counts_of_the_layer():
     assert f == 4 * 128 * 32 * 6 and b == 3 * 80 * 256
     f, b = R.counts(layer, "rope_write_step", [5, 9])
     assert f == 3 * 2 * 40 * 128 and b == 2 * (80 * 256 + 16 * 256 + 512 + 16)
+
+
+@gpu
+def test_windows_beyond_32_bits_are_refused():
+    x = rand(4, 2, 64).to(DEV)
+    cu = torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    c = make_cache(BF, 2, 2, 16, 64)
+    dec = O.DecodeAttention(c, batch=1, heads=2)
+    with pytest.raises(ValueError, match="window"):
+        O.attn_prompt(x, x, x, cu, max_q=4, window=2 ** 31)
+    with pytest.raises(ValueError, match="window"):
+        dec(x[None, :1], torch.zeros(1, 2, dtype=torch.int32, device=DEV), cu[:1], window=2 ** 31)
