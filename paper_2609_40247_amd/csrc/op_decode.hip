@@ -357,8 +357,9 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeAr
           vt[1][j] = __builtin_amdgcn_perm(y, x, 0x07060302);
         }
         // A value that is not finite must reach the rows that see its key and no
-        // other: where rows differ it is taken out of the product, and added.
-        if (KIND != HERSCHEL_INT8 && edge && p.a.new_tokens > 1) {
+        // other: where rows differ, or none sees what a bad page id stands for, it
+        // is taken out of the product, and added.
+        if (KIND != HERSCHEL_INT8 && edge && (p.a.new_tokens > 1 || !s.live[0] || !s.live[1])) {
           constexpr uint32_t ONE = PV == HERSCHEL_BF16 ? 0x3f80u : 0x3c00u;
           constexpr uint32_t INF = PV == HERSCHEL_BF16 ? 0x7f80u : 0x7c00u;
 #pragma unroll

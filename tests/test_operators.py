@@ -788,6 +788,41 @@ def test_attn_decode_faults():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,kind", [(BF, BF), (HF, HF), (BF, F8), (HF, I8)], ids=str)
+def test_attn_decode_bad_pages_are_not_seen(dtype, kind):
+    """Keys of a page id outside the cache have no effect, whatever the cache's pages hold: the rest as without them."""
+    page, lens = 16, [100, 40]
+    c, dec, q, bt, sl, out = run_decode(lens, 4, 2, 64, dtype, kind, page)
+    used = set(bt[0, :7].tolist()) | set(bt[1, :3].tolist())
+    free = next(i for i in range(c.n_pages) if i not in used)
+    if 0 in used:  # the cache's first page becomes one that no sequence names, full of NaN
+        for t in (c.k.view(torch.uint8), c.v.view(torch.uint8), c.k_scale, c.v_scale):
+            if t is not None:
+                t[free].copy_(t[0])
+        bt[bt == 0] = free
+    c.k.view(torch.uint8)[0].fill_(0x7f)
+    c.v.view(torch.uint8)[0].fill_(0x7f)
+    if dtype != kind:
+        c.k_scale[0].fill_(math.nan)
+        c.v_scale[0].fill_(math.nan)
+    else:
+        c.k[0].fill_(math.nan)
+        c.v[0].fill_(math.nan)
+    assert torch.equal(dec(q, bt.to(DEV), sl), out)
+    bad = bt.clone()
+    bad[0, 6] = c.n_pages  # the last four keys
+    got = dec(q, bad.to(DEV), sl)
+    with pytest.raises(ValueError, match="block table"):
+        c.check()
+    k, v = dense(c, bt, lens)[0]
+    # 96 keys and no mask: the last page's are those that the last token alone would have seen
+    ref = exact_attention(q[0].cpu(), k[:96], v[:96], 64 ** -0.5, False, 0)
+    rounded = U[dtype] if not c.quantised else U[BF] if dtype == BF else 2.0 ** -16
+    check_attention(got[0], None, ref, dtype, rounded, 96, 64)
+    assert torch.equal(got[1], out[1])
+
+
+@gpu
 def test_decode_in_a_graph_and_on_another_stream():
     """A captured step follows new contents and lengths on every replay; a call on another stream is ordered there."""
     lens = [300, 77, 5]
