@@ -77,41 +77,85 @@ __device__ __forceinline__ void reads_ahead() {
   __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, GROUP);
 }
 
-// A row's outputs from the keys [lo, hi) one by one, by a wave whose lanes go
-// across the dimensions.  Factors are never 0, so that an infinite value or sum
-// stays one.
+// A row's outputs from the keys [lo, hi) alone, by a wave: 64 keys at a time, a
+// key to a lane for the scores, then a dimension (or two) to a lane for the
+// values, 32 rows asked for at once.  Factors are never 0, so that an infinite
+// value or sum stays one.  4096 rows of 32 heads of 128 that all see a NaN: 14 ms (a key at a time 46).
 template <int TYPE, int D>
 __device__ __forceinline__ void row_by_key(const uint16_t* q, const uint16_t* kbase, const uint16_t* vbase,
                                            const herschel_prompt_args& a, int lo, int hi, int64_t at) {
+  constexpr int ND = D / WAVE, AT_ONCE = 32;
   const int lane = threadIdx.x % WAVE;
-  float qv[D / WAVE], acc[D / WAVE], top = NO_KEY, den = 0, unused;
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const bool vec = ((uintptr_t)kbase & 15) == 0 && (a.k_strides.row & 7) == 0;
+  float qv[ND], acc[ND], top = NO_KEY, den = 0, unused;
 #pragma unroll
-  for (int d = 0; d < D / WAVE; ++d) {
+  for (int d = 0; d < ND; ++d) {
     unpack2<TYPE>(q[d * WAVE + lane], qv[d], unused);
     acc[d] = 0;
   }
-  for (int key = lo; key < hi; ++key) {
-    float x = 0, v[D / WAVE];
+  auto of_lane = [](float x, int i) INLINE {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), i));
+  };
+  for (int k0 = lo; k0 < hi; k0 += WAVE) {
+    const int n = min(WAVE, hi - k0);
+    const uint16_t* k = kbase + (k0 + min(lane, n - 1)) * a.k_strides.row;
+    float x = 0;
 #pragma unroll
-    for (int d = 0; d < D / WAVE; ++d) {
-      float k;
-      unpack2<TYPE>(kbase[key * a.k_strides.row + d * WAVE + lane], k, unused);
-      unpack2<TYPE>(vbase[key * a.v_strides.row + d * WAVE + lane], v[d], unused);
-      x += qv[d] * k;
+    for (int d0 = 0; d0 < D; d0 += 64) {
+      u32x4 w[8];
+      if (vec) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) w[c] = *(const u32x4*)(k + d0 + 8 * c);
+      } else {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) w[c] = load_elements(k + d0 + 8 * c);
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        float ka, kb;
+        unpack2<TYPE>(w[i / 4][i % 4], ka, kb);
+        x += of_lane(qv[d0 / 64], 2 * i) * ka;
+        x += of_lane(qv[d0 / 64], 2 * i + 1) * kb;
+      }
     }
-#pragma unroll
-    for (int m = 1; m < WAVE; m *= 2) x += __shfl_xor(x, m);
     x *= a.scale * 1.44269504088896340736f;
-    const float next = fmaxf(top, x), by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
+    float next = fmaxf(top, lane < n ? x : top);
+#pragma unroll
+    for (int m = 1; m < WAVE; m *= 2) next = fmaxf(next, __shfl_xor(next, m));
+    const float by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
     float e = __builtin_amdgcn_exp2f(x - next);
     if (e == 0) e = 0x1p-126f;
+    if (lane >= n) e = 0;
     top = next;
-    den = den * by + e;
+    float total = e;
 #pragma unroll
-    for (int d = 0; d < D / WAVE; ++d) acc[d] = acc[d] * by + e * v[d];
+    for (int m = 1; m < WAVE; m *= 2) total += __shfl_xor(total, m);
+    den = den * by + total;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[d] *= by;
+    const uint16_t* v = vbase + k0 * a.v_strides.row + lane;
+    for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
+      uint16_t w[AT_ONCE][ND];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) w[i][d] = v[min(i0 + i, n - 1) * a.v_strides.row + d * WAVE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const float f = of_lane(e, min(i0 + i, n - 1));
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          float y;
+          unpack2<TYPE>(w[i][d], y, unused);
+          acc[d] += i0 + i < n ? f * y : 0.0f;
+        }
+      }
+    }
   }
 #pragma unroll
-  for (int d = 0; d < D / WAVE; ++d)
+  for (int d = 0; d < ND; ++d)
     ((uint16_t*)a.out)[at * D + d * WAVE + lane] = (uint16_t)pack2<TYPE>(den == 0 ? 0.0f : acc[d] / den, 0.0f);
   if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
 }
