@@ -37,11 +37,16 @@ namespace hop {
 #define INLINE __attribute__((always_inline))
 
 constexpr int TILE = 128;         // keys of a workgroup's step: 32 a wave
-// Shares of the line: as many workgroups as the CUs hold.  Three a CU with codes
-// and one row block (64 requests 92 us against 105 with two), two where
-// registers allow no more or the reads are as fast (bf16 102 and 104 us).
-constexpr int MAX_SHARES = 768;
-constexpr int shares_of_cu(int kind, int row_blocks) { return quantised(kind) && row_blocks == 1 ? 3 : 2; }
+// Shares of the line: as many workgroups as the CUs hold, by registers.  Of heads
+// of 128 three a CU with codes and one row block (64 requests 92 us against 105
+// with two), else two (bf16 102 and 104 us; more with two blocks spill: 126 us
+// become 141).  A step of heads of 64 has half the bytes to wait for and fewer
+// registers: four (64 requests in fp8 56 us against 61 with three), with two row
+// blocks of codes three (three long contexts 86 against 92 with two).
+constexpr int MAX_SHARES = 1024;
+constexpr int shares_of_cu(int kind, int row_blocks, int dim) {
+  return dim == 64 ? (row_blocks == 1 ? 4 : quantised(kind) ? 3 : 2) : quantised(kind) && row_blocks == 1 ? 3 : 2;
+}
 constexpr float FAR_BELOW = -3.0e38f;
 constexpr float LARGE_SUM = 4096.0f;  // half's largest value is 65504
 
@@ -125,7 +130,7 @@ __device__ __forceinline__ int64_t share_start(int64_t w, int64_t U, int64_t G) 
 __device__ __forceinline__ int64_t share_of(int64_t x, int64_t U, int64_t G) { return divide((x + 1) * G - 1, U); }
 
 template <int TYPE, int KIND, int D, int RB>
-__global__ __launch_bounds__(256, shares_of_cu(KIND, RB)) void k_decode(DecodeArgs p) {
+__global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(DecodeArgs p) {
   // With codes the second product runs in bf16, whose range holds exponential
   // times scale for any scale; for half inputs it runs twice, on the rounded
   // value and on what the rounding left, so that the result keeps half's precision.
@@ -528,7 +533,7 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
 template <int TYPE, int KIND, int D, int RB>
 static int decode_launch(DecodeArgs& p) {
   const size_t pre = ((p.a.n_seqs + 1 + 3) & ~3) * 4;
-  const int rc = launch(k_decode<TYPE, KIND, D, RB>, dim3(256 * shares_of_cu(KIND, RB)), dim3(256), pre + 4 * 16 * (D + 2) * 4,
+  const int rc = launch(k_decode<TYPE, KIND, D, RB>, dim3(256 * shares_of_cu(KIND, RB, D)), dim3(256), pre + 4 * 16 * (D + 2) * 4,
                         p.a.hip_stream, p);
   if (rc != HERSCHEL_OK) return rc;
   return launch(k_decode_join<TYPE, D, RB>, dim3((unsigned)(p.a.n_seqs * p.c.n_heads * p.rows)), dim3(256), 0,
