@@ -218,6 +218,19 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
 #pragma unroll
       for (int t = 0; t < 2; ++t) page[t] = table[min(max(k0 + 16 * t, any_from), len - 1) >> p.page_shift];
     };
+    // A lane's places in a run of 16 keys: its key's row, the first of its four values' rows, their scales.
+    const uint32_t koff = m * (D * CB) + 16 * g, voff = 4 * g * (D * CB) + m * (ND * CB), soff = 4 * g;
+    auto load_v = [&](uint32_t* to, const char* from) INLINE {  // whole rows, read once: past the caches (32 x 4096 in bf16 102 to 93 us)
+      if constexpr (VW == 4) {
+        const u32x4 x = __builtin_nontemporal_load((const u32x4*)from);
+        to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
+      } else if constexpr (VW == 2) {
+        const u32x2 x = __builtin_nontemporal_load((const u32x2*)from);
+        to[0] = x[0], to[1] = x[1];
+      } else {
+        to[0] = *(const uint32_t*)from;
+      }
+    };
     auto load = [&](Step& s, int k0, const int (&page)[2]) INLINE {
       const bool inside = k0 >= any_from && k0 + 32 <= len;
       const int in_page = p.c.page_size - 1;
@@ -227,33 +240,29 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
         if (!s.live[t] && lane == 0) flag(p.a.status, HERSCHEL_OP_BAD_PAGE);
         const int64_t base = ((int64_t)(s.live[t] ? page[t] : 0) * p.c.n_heads + head) << p.page_shift;
         const int k = k0 + 16 * t;
-        auto row = [&](int key) INLINE { return (inside ? key : min(max(key, any_from), len - 1)) & in_page; };
-        const char* kp = (const char*)p.c.k + base * (D * CB) + (uint32_t)(row(k + m) * (D * CB) + 16 * g);
+        if (inside) {  // addresses of the wave, offsets of the lane: nothing to compute
+          const int64_t at = base + (k & in_page);
+          const char *kp = (const char*)p.c.k + at * (D * CB), *vp = (const char*)p.c.v + at * (D * CB);
 #pragma unroll
-        for (int i = 0; i < (CB == 2 ? NS : NS / 2); ++i) s.k[t][i] = *(const u32x4*)(kp + 64 * i);
+          for (int i = 0; i < (CB == 2 ? NS : NS / 2); ++i) s.k[t][i] = *(const u32x4*)(kp + koff + 64 * i);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {  // whole rows, read once: past the caches (32 x 4096 in bf16 102 to 93 us)
-          const char* vp = (const char*)p.c.v + base * (D * CB) + (uint32_t)(row(k + 4 * g + j) * (D * CB) + m * (ND * CB));
-          uint32_t* to = s.v[4 * t + j];
-          if constexpr (VW == 4) {
-            const u32x4 x = __builtin_nontemporal_load((const u32x4*)vp);
-            to[0] = x[0], to[1] = x[1], to[2] = x[2], to[3] = x[3];
-          } else if constexpr (VW == 2) {
-            const u32x2 x = __builtin_nontemporal_load((const u32x2*)vp);
-            to[0] = x[0], to[1] = x[1];
-          } else {
-            to[0] = *(const uint32_t*)vp;
+          for (int j = 0; j < 4; ++j) load_v(s.v[4 * t + j], vp + voff + j * (D * CB));
+          if constexpr (quantised(KIND)) {
+            s.ks[t] = *(const f32x4*)(p.c.k_scale + at + soff);
+            s.vs[t] = *(const f32x4*)(p.c.v_scale + at + soff);
           }
-        }
-        if constexpr (quantised(KIND)) {
-          if (inside) {
-            s.ks[t] = *(const f32x4*)(p.c.k_scale + base + ((k & in_page) + 4 * g));
-            s.vs[t] = *(const f32x4*)(p.c.v_scale + base + ((k & in_page) + 4 * g));
-          } else {
+        } else {
+          auto row = [&](int key) INLINE { return base + (min(max(key, any_from), len - 1) & in_page); };
+          const char* kp = (const char*)p.c.k + row(k + m) * (D * CB) + 16 * g;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              s.ks[t][j] = p.c.k_scale[base + row(k + 4 * g + j)];
-              s.vs[t][j] = p.c.v_scale[base + row(k + 4 * g + j)];
+          for (int i = 0; i < (CB == 2 ? NS : NS / 2); ++i) s.k[t][i] = *(const u32x4*)(kp + 64 * i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int64_t at = row(k + 4 * g + j);
+            load_v(s.v[4 * t + j], (const char*)p.c.v + at * (D * CB) + m * (ND * CB));
+            if constexpr (quantised(KIND)) {
+              s.ks[t][j] = p.c.k_scale[at];
+              s.vs[t][j] = p.c.v_scale[at];
             }
           }
         }
