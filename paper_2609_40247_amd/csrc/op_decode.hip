@@ -151,6 +151,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
   const int64_t U = (int64_t)uniform(s_pre[p.a.n_seqs]) * p.units, G = U < gridDim.x ? U : gridDim.x;
   if (blockIdx.x >= G) return;
   const int64_t begin = share_start(blockIdx.x, U, G), end = share_start(blockIdx.x + 1, U, G);
+  const uint32_t n_pages = (uint32_t)min(p.c.n_pages, (int64_t)INT32_MAX + 1);
   // a negative scale goes into Q's signs
   const float to_log2 = fabsf(p.a.scale) * 1.44269504088896340736f;
   const uint32_t sign = p.a.scale < 0 ? 0x80008000u : 0u;
@@ -236,9 +237,10 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
       const int in_page = p.c.page_size - 1;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        s.live[t] = page[t] >= 0 && page[t] < p.c.n_pages;
+        s.live[t] = (uint32_t)page[t] < n_pages;
+        const int id = uniform(s.live[t] ? page[t] : 0);  // the wave's, also where one lane reports
         if (!s.live[t] && lane == 0) flag(p.a.status, HERSCHEL_OP_BAD_PAGE);
-        const int64_t base = ((int64_t)(s.live[t] ? page[t] : 0) * p.c.n_heads + head) << p.page_shift;
+        const int64_t base = ((int64_t)id * p.c.n_heads + head) << p.page_shift;
         const int k = k0 + 16 * t;
         if (inside) {  // addresses of the wave, offsets of the lane: nothing to compute
           const int64_t at = base + (k & in_page);
