@@ -58,6 +58,7 @@ struct DecodeArgs {
   int rows;      // new tokens * group
   int units;     // key heads * row blocks
   int row_blocks;
+  bool q_vec;    // Q's chunks of 16 bytes are aligned
   int2* span;    // [n_seqs * units] first part and last share of a row block; first part -1: nothing to join
   float* part;   // [2 * MAX_SHARES][RB * 16][head_dim + 2]: sums, reference, sum of exponentials
 };
@@ -152,9 +153,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
   if (blockIdx.x >= G) return;
   const int64_t begin = share_start(blockIdx.x, U, G), end = share_start(blockIdx.x + 1, U, G);
   const uint32_t n_pages = (uint32_t)min(p.c.n_pages, (int64_t)INT32_MAX + 1);
-  // a negative scale goes into Q's signs
-  const float to_log2 = fabsf(p.a.scale) * 1.44269504088896340736f;
-  const uint32_t sign = p.a.scale < 0 ? 0x80008000u : 0u;
+  const float to_log2 = p.a.scale * 1.44269504088896340736f;
 
   for (int64_t pos = begin; pos < end;) {
     // the sequence, unit and tile at this place of the line
@@ -177,32 +176,6 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
     typedef const __attribute__((address_space(4))) int32_t Table;
     Table* table = (Table*)(uintptr_t)(p.a.block_table + b * p.a.table_stride);
 
-    // Q: lane (r, g) of block rb holds row r, elements in the order of the keys' chunks;
-    // lanes beyond the last row repeat the first one, unused
-    u32x4 q[RB][NS];
-    int seen_to[RB], seen_from[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int r = row0 + rb * 16 + m;
-      const int tok = r < p.rows ? r / p.group : 0, qh = head * p.group + (r < p.rows ? r % p.group : 0);
-      seen_to[rb] = len - p.a.new_tokens + tok + 1;  // keys before this
-      seen_from[rb] = window_from(seen_to[rb] - 1, p.a.window);
-      const uint16_t* src = (const uint16_t*)p.a.q + b * p.a.q_seq_stride + tok * p.a.q_strides.row + qh * p.a.q_strides.head;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const int d = CB == 2 ? 32 * s + 8 * g : 64 * (s / 2) + 16 * g + 8 * (s & 1);
-        q[rb][s] = (((uintptr_t)src & 15) == 0 ? *(const u32x4*)(src + d) : load_elements(src + d)) ^ sign;
-      }
-    }
-    f32x4 o[RB][ND];
-    float ref[RB], sum[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      ref[rb] = FAR_BELOW;
-      sum[rb] = 0;
-#pragma unroll
-      for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
-    }
     const int key_begin = (first_tile(p, len) + tile) * TILE, key_end = min(len, key_begin + n_tiles * TILE);
     // keys that every row sees need no mask; those that some row sees are read
     const int all_to = len - p.a.new_tokens + 1, all_from = window_from(len - 1, p.a.window);
@@ -219,6 +192,35 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
 #pragma unroll
       for (int t = 0; t < 2; ++t) page[t] = table[min(max(k0 + 16 * t, any_from), len - 1) >> p.page_shift];
     };
+    // All that the first step waits for is asked for in one go: page ids, Q, rows.
+    int k0 = key_begin + wave * 32, page[2] = {0, 0};
+    if (k0 < key_end) find(k0, page);
+    // Q: lane (r, g) of block rb holds row r, elements in the order of the keys' chunks;
+    // lanes beyond the last row repeat the first one, unused
+    u32x4 q[RB][NS];
+    int seen_to[RB], seen_from[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const int r = row0 + rb * 16 + m;
+      const int tok = r < p.rows ? r / p.group : 0, qh = head * p.group + (r < p.rows ? r % p.group : 0);
+      seen_to[rb] = len - p.a.new_tokens + tok + 1;  // keys before this
+      seen_from[rb] = window_from(seen_to[rb] - 1, p.a.window);
+      const uint16_t* src = (const uint16_t*)p.a.q + b * p.a.q_seq_stride + tok * p.a.q_strides.row + qh * p.a.q_strides.head;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const int d = CB == 2 ? 32 * s + 8 * g : 64 * (s / 2) + 16 * g + 8 * (s & 1);
+        q[rb][s] = p.q_vec ? *(const u32x4*)(src + d) : load_elements(src + d);
+      }
+    }
+    f32x4 o[RB][ND];
+    float ref[RB], sum[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      ref[rb] = FAR_BELOW;
+      sum[rb] = 0;
+#pragma unroll
+      for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
+    }
     // A lane's places in a run of 16 keys: its key's row, the first of its four values' rows, their scales.
     const uint32_t koff = m * (D * CB) + 16 * g, voff = 4 * g * (D * CB) + m * (ND * CB), soff = 4 * g;
     auto load_v = [&](uint32_t* to, const char* from) INLINE {  // whole rows, read once: past the caches (32 x 4096 in bf16 102 to 93 us)
@@ -422,16 +424,11 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           }
       }
     };
-    int k0 = key_begin + wave * 32;
-    if (k0 < key_end) {
-      Step s;
-      int page[2];
-      find(k0, page);
-      for (; k0 < key_end; k0 += TILE) {
-        load(s, k0, page);
-        find(k0 + TILE, page);
-        work(s, k0);
-      }
+    Step s;
+    for (; k0 < key_end; k0 += TILE) {
+      load(s, k0, page);
+      find(k0 + TILE, page);
+      work(s, k0);
     }
 
     // The four waves' parts of these rows, joined through LDS block by block.
@@ -594,6 +591,7 @@ extern "C" int herschel_attn_decode(const herschel_decode_args* args, const hers
   p.a = a;
   p.c = *cache;
   p.page_shift = log2i(cache->page_size);
+  p.q_vec = chunks_aligned(a.q, a.q_strides) && (a.q_seq_stride & 7) == 0;
   p.group = a.q_heads / cache->n_heads;
   p.rows = a.new_tokens * p.group;
   const int block = decode_rows(p.rows);
