@@ -24,7 +24,19 @@
 //  - A step's 16 KB (8 with codes) a wave are asked for at once; the waits are
 //    filled by the other waves of the SIMD.  (Loading the next step's rows before
 //    this one is worked on costs registers, and with them waves: 105 us became
-//    110 for 32 requests of 4096 tokens in bf16, 92 became 102 for 64 in fp8.)
+//    110 for 32 requests of 4096 tokens in bf16, 92 became 102 for 64 in fp8.  Its
+//    keys once the scores are there and its values after the second product spill
+//    with fp8, 79 became 136 us, and gain nothing with int8, 52 became 54.)
+//  - The second kernel costs 5 to 7 us.  Joining in the first, by the workgroup
+//    whose part is the last one there, costs more: parts written through the
+//    caches to where all XCDs see them 14.0 us against 12.9 for one request of 4000
+//    tokens, 140 against 121 for three long contexts.
+//
+// 64 requests of 512 to 8704 tokens in fp8, 396 MB: 78 us, 5.1 TB/s, a copy's rate.
+// One of 4000 tokens in bf16, 16 MB: 12.8 us, two kernels' latency.  Four drafted
+// tokens of three long contexts in int8, 473 MB: 107 us, 4.4 TB/s; with 20 rows of
+// 32 in use, codes that become halves and every product of the second kind done
+// twice, vector instructions take half of that.
 //
 // The reference of a row's exponentials moves only when a step's sum shows that
 // one of them is large; no maximum is computed otherwise.  Rows of keys beyond
