@@ -47,7 +47,56 @@ struct PromptArgs {
   int levels;  // query tiles of the longest sequence
   int spread;  // XCDs that share a key head's workgroups; 0: heads in turn
   int splits;  // parts of each workgroup's keys (gridDim.y); above 1 they meet in k_prompt_join
+  int packed;  // few rows: workgroups are numbered by the levels that the sequences have, not levels by sequences
 };
+
+// The rows and level (of 32) of workgroup `id` of packed ones: sequence after
+// sequence, each from its last level (the longest) down; false beyond the last.
+// Starts that fall count as the largest before them, so that the levels never
+// exceed the rows' and one for each sequence.
+__device__ __forceinline__ bool find_level(const herschel_prompt_args& a, int heads, uint32_t id, int& b, int& level, int64_t& q0,
+                                           int64_t& q1) {
+  const int lane = threadIdx.x % WAVE;
+  auto at = [](int x, int l) INLINE { return __builtin_amdgcn_readlane(x, l); };
+  int past = 0;
+  for (int b0 = 0; b0 < a.n_seqs; b0 += WAVE) {
+    int lo = (int)min((int64_t)max(a.cu_q[min(b0 + lane, a.n_seqs)], 0), a.n_q);
+    int hi = (int)min((int64_t)max(a.cu_q[min(b0 + lane + 1, a.n_seqs)], 0), a.n_q);
+    if (__ballot(hi < lo || lo < past)) {
+      lo = max(lo, past);
+#pragma unroll
+      for (int o = 1; o < WAVE; o *= 2) lo = max(lo, __shfl_up(lo, o));  // the first lanes get their own
+      hi = max(hi, lo);
+    }
+    const int n = (int)(((int64_t)min(hi - lo, a.max_q) * heads + 31) / 32);
+    int sum = n;
+#pragma unroll
+    for (int o = 1; o < WAVE; o *= 2) {
+      const int y = __shfl_up(sum, o);
+      if (lane >= o) sum += y;
+    }
+    const uint64_t reached = __ballot((uint32_t)sum > id);
+    if (reached) {
+      const int l = __builtin_ctzll(reached);
+      b = b0 + l;
+      level = at(sum, l) - 1 - (int)id;
+      q0 = at(lo, l);
+      q1 = at(hi, l);
+      return true;
+    }
+    id -= (uint32_t)at(sum, WAVE - 1);
+    past = at(hi, WAVE - 1);
+  }
+  return false;
+}
+
+// What the workgroups of single sequences report where there may be none: the first wave of the grid.
+__device__ __forceinline__ void report_lengths(const herschel_prompt_args& a) {
+  for (int b = threadIdx.x; b < a.n_seqs; b += WAVE) {
+    const int64_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1], k0 = a.cu_k[b], k1 = a.cu_k[b + 1];
+    if (q0 < 0 || q1 < q0 || q1 > a.n_q || q1 - q0 > a.max_q || k0 < 0 || k1 < k0 || k1 > a.n_k) flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+  }
+}
 
 // A row's part: sums of its values, reference and sum of its exponentials.
 template <int D>
@@ -491,6 +540,13 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
 // keys take 25.8 us), so no wave waits for another before the parts are joined.
 // The next step's keys are asked for once the scores are there, its values after
 // the second product.
+//
+// Packed sequences of different lengths would leave most workgroups of a grid of
+// levels by sequences without rows, and one waits for the lengths to find that
+// out: here the grid has the levels that the rows allow and one a sequence (8
+// sequences of 1 to 600 tokens, 16 heads of 64: 23.5 to 10.2 us).  Workgroups of
+// 128 rows have fewer levels, and the search costs them as much (24 x 1 to 300
+// tokens 10.5 against 11.8 us).
 constexpr int FEW_WAVES = 4;  // eight: 2048 keys 20 us against 23, but 512 rows 16.7 against 12.2
 template <int TYPE, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p) {
@@ -508,10 +564,15 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   uint32_t id = blockIdx.x;  // longest first
   const int kh = (int)(id % a.kv_heads);
   id /= a.kv_heads;
-  const int b = (int)(id % a.n_seqs), level = p.levels - 1 - (int)(id / a.n_seqs);
+  int b = (int)(id % a.n_seqs), level = p.levels - 1 - (int)(id / a.n_seqs);
+  int64_t q0, q1;
+  if (p.packed) {
+    if (blockIdx.x == 0 && tid < WAVE) report_lengths(a);
+    if (!find_level(a, p.group, id, b, level, q0, q1)) return;
+  }
   // lengths taken as the nearest valid
   const int64_t q0w = a.cu_q[b], q1w = a.cu_q[b + 1], k0w = a.cu_k[b], k1w = a.cu_k[b + 1];
-  const int64_t q0 = min(max(q0w, (int64_t)0), a.n_q), q1 = min(max(q1w, q0), a.n_q);
+  if (!p.packed) q0 = min(max(q0w, (int64_t)0), a.n_q), q1 = min(max(q1w, q0), a.n_q);
   const int64_t kk0 = min(max(k0w, (int64_t)0), a.n_k), kk1 = min(max(k1w, kk0), a.n_k);
   const int nq = (int)min(q1 - q0, (int64_t)a.max_q), nk = (int)(kk1 - kk0);
   if (level == 0 && kh == 0 && tid == 0 && (q0 != q0w || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
@@ -798,7 +859,9 @@ static int prompt_join(PromptArgs& p) {
 
 template <int TYPE, int D>
 static int prompt_few(PromptArgs& p, bool vec) {
-  const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, blocks = levels * p.a.n_seqs * p.a.kv_heads;
+  const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, most = p.a.n_q * p.group / 32 + p.a.n_seqs;
+  p.packed = p.a.n_seqs > 1 && p.splits == 1 && most < levels * p.a.n_seqs;
+  const int64_t blocks = (p.packed ? most : levels * p.a.n_seqs) * p.a.kv_heads;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
   p.levels = (int)levels;
   auto kernel = vec ? p.splits > 1 ? k_prompt_few<TYPE, D, true, true> : k_prompt_few<TYPE, D, true, false>
@@ -836,7 +899,10 @@ static int prompt_launch(PromptArgs& p, bool vec) {
 // workgroups of 128 rows read them fewer times, so rows times keys times dimensions
 // have a limit too (of 128, 4 x 64 rows of 32 heads over 4096 keys, 4.3e9, 44
 // against 49, 512 rows, 8.6e9, 57 against 51; 777 rows of 8 heads over 12000 83
-// against 64; of 64, 4096 rows of 4 heads, 4.3e9, 27 against 35).
+// against 64; of 64, 4096 rows of 4 heads, 4.3e9, 27 against 35).  Heads of 64 gain
+// up to 960 workgroups (16 heads: 24 x 1 to 300 tokens 9.0 us against 10.5, 100 to
+// 900 three times 12.4 against 21.0, 900 twice 16.3 against 21.2, one of 1800 20.3
+// against 36.5; 24 x 100, 1296 workgroups, 11.4 against 8.7).
 //
 // Else eight waves (256 rows) or four (128).  Eight in turns are faster where there
 // is enough for every CU twice over: 4096 rows of 32 heads of 128 145 us against
@@ -863,7 +929,8 @@ static PromptPlan prompt_plan(int64_t n_seqs, int64_t n_q, int64_t n_k, int64_t 
   PromptPlan plan{4, 1, 0};
   const int64_t rows = std::max<int64_t>(1, n_q / n_seqs), keys = n_k / n_seqs;
   int64_t splits = 1;
-  if (n_q * q_heads <= 20480 && n_q * q_heads * keys <= (5ll << 30) / D && max_q * (q_heads / kv_heads) < 0x7fffffe0) {
+  const int64_t few = (n_q * (q_heads / kv_heads) / 32 + n_seqs) * kv_heads;  // workgroups of 32 rows, at most
+  if ((n_q * q_heads <= 20480 || (D == 64 && few <= 960)) && n_q * q_heads * keys <= (5ll << 30) / D && max_q * (q_heads / kv_heads) < 0x7fffffe0) {
     plan.waves = 0;
     splits = std::min<int64_t>(512 / std::max<int64_t>(1, (n_q * q_heads + 31) / 32), keys / 512);
     if (splits < 4 && keys < 8192) splits = 1;
@@ -922,7 +989,7 @@ extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
   if (a.n_q == 0 || a.max_q == 0) return HERSCHEL_OK;
   PromptPlan plan = prompt_plan(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim);
   if (!a.workspace || a.workspace_bytes < plan.bytes) plan.splits = 1;
-  PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0, plan.splits};
+  PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0, plan.splits, 0};
   // 16-byte loads, and a tile's rows within 31 bits of bytes
   const bool vec = a.k_strides.row < (1 << 23) && a.v_strides.row < (1 << 23) && chunks_aligned(a.q, a.q_strides) && chunks_aligned(a.k, a.k_strides) && chunks_aligned(a.v, a.v_strides);
   return a.type == HERSCHEL_BF16 ? prompt_dim<HERSCHEL_BF16>(p, plan, vec) : prompt_dim<HERSCHEL_F16>(p, plan, vec);

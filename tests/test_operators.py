@@ -471,6 +471,46 @@ def test_attn_prompt(case, dtype):
     run_prompt(nq, nk or nq, hq, hk, D, dtype, causal, window)
 
 
+RAGGED_CASES = [  # queries, keys, heads, kv heads, D, causal, window
+    ([600] + [1, 0, 3, 17] * 2, None, 8, 2, 64, True, 0),
+    ([0, 0, 5, 0, 90, 1], [7, 0, 5, 0, 200, 0], 10, 2, 128, True, 40),
+    ([(7 * i) % 11 for i in range(150)], None, 2, 2, 64, True, 0),             # beyond 64 sequences
+    ([0] * 130 + [70] + [0] * 3 + [33], None, 3, 1, 128, False, 0),
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", RAGGED_CASES, ids=lambda c: f"{len(c[0])}-{sum(c[0])}-{c[4]}")
+def test_attn_prompt_ragged(case):
+    """Packed sequences of very different lengths, empty ones between and at the ends."""
+    nq, nk, hq, hk, D, causal, window = case
+    run_prompt(nq, nk or nq, hq, hk, D, BF, causal, window)
+
+
+@gpu
+def test_attn_prompt_faults_of_ragged_sequences():
+    """Starts that fall, exceed the rows or are negative among many sequences: reported, every row still written."""
+    q = rand(300, 4, 64).to(DEV)
+    good = [0, 1, 1, 4, 200] + [200 + 25 * i for i in range(1, 5)]
+
+    def go(cu_q, cu_k, max_q=196):
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        out = torch.full_like(q, math.nan)
+        O.attn_prompt(q, q[:, :2], q[:, 2:], torch.tensor(cu_q, dtype=torch.int32, device=DEV),
+                      torch.tensor(cu_k, dtype=torch.int32, device=DEV), max_q=max_q, status=status, out=out)
+        return status.item(), out
+    bits, want = go(good, good)
+    assert bits == 0 and torch.isfinite(want).all()
+    for i, value in ((2, 0), (4, 2), (4, -9), (8, 500), (3, 2 ** 31 - 1)):
+        bad = list(good)
+        bad[i] = value
+        assert go(good, bad)[0] == O.BAD_LENGTH
+        bits, out = go(bad, good, max_q=300)
+        assert bits == O.BAD_LENGTH and torch.isfinite(out).all()
+    bits, out = go(good, good, max_q=100)
+    assert bits == O.BAD_LENGTH and torch.equal(out[:104], want[:104]) and torch.equal(out[200:], want[200:])
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [BF, HF], ids=str)
 @pytest.mark.parametrize("case", PROMPT_CASES, ids=str)
