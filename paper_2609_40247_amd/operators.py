@@ -278,7 +278,10 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
 
     def rows(t, name, like=None):
         """(address, row stride, head stride, heads) of rows that go with the first ones."""
-        (n, heads, d), (row, head, step) = t.shape, t.stride()
+        shape, stride = t.shape, t.stride()
+        if len(shape) != 3:
+            _rows(t, name)
+        (n, heads, d), (row, head, step) = shape, stride
         if (t.dtype is not dtype or t.get_device() != dev or n != T or d != D or step != 1 and D > 1 or
                 like is not None and heads != like):
             _rows(t, name)
@@ -286,9 +289,6 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
             _need(False, f"{name} must have the tokens, heads and head size of the rows it goes with")
         return t.data_ptr(), row, head, heads
 
-    for t, name in ((k, "k"), (v, "v"), (q_out, "q_out"), (k_out, "k_out")):
-        if t is not None and t.dim() != 3:
-            _rows(t, name)
     qa = rows(q, "q") if q is not None else _NO_ROWS
     ka = rows(k, "k") if k is not None else _NO_ROWS
     va = rows(v, "v", None if k is None else ka[3]) if v is not None else _NO_ROWS
@@ -382,21 +382,24 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     _like(k, q, "k")
     _like(v, q, "v")
     dev, (n_q, heads, D), (n_k, kv_heads, _) = q.get_device(), q.shape, k.shape
-    _need(D == 64 or D == 128, "attention needs heads of 64 or 128")
-    _need(k.shape == v.shape and k.shape[2] == D, "k and v must have one shape, and q's head size")
-    _need(kv_heads >= 1 and heads >= 1 and heads % kv_heads == 0, "q's heads must be a multiple of k's")
-    _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, "cu_q must hold a sequence's start and end")
-    from_q = _ints(cu_q, "cu_q", torch.int32, cu_q.shape, dev)
-    from_k = from_q if cu_k is None else _ints(cu_k, "cu_k", torch.int32, cu_q.shape, dev)
-    _need(0 <= max_q <= n_q, "max_q must be a number of q's rows")
-    _need(0 <= window < 2 ** 31, "window must be 0 or a number of keys below 2^31")
+    starts = cu_q.shape
+    if not ((D == 64 or D == 128) and k.shape == v.shape == (n_k, kv_heads, D) and kv_heads >= 1 and heads >= 1 and
+            heads % kv_heads == 0 and len(starts) == 1 and starts[0] >= 2 and 0 <= max_q <= n_q and 0 <= window < 2 ** 31):
+        _need(D == 64 or D == 128, "attention needs heads of 64 or 128")
+        _need(k.shape == v.shape and k.shape[2] == D, "k and v must have one shape, and q's head size")
+        _need(kv_heads >= 1 and heads >= 1 and heads % kv_heads == 0, "q's heads must be a multiple of k's")
+        _need(cu_q.dim() == 1 and cu_q.shape[0] >= 2, "cu_q must hold a sequence's start and end")
+        _need(0 <= max_q <= n_q, "max_q must be a number of q's rows")
+        _need(False, "window must be 0 or a number of keys below 2^31")
+    from_q = _ints(cu_q, "cu_q", torch.int32, starts, dev)
+    from_k = from_q if cu_k is None else _ints(cu_k, "cu_k", torch.int32, starts, dev)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
     else:
         to = _ints(out, "out", q.dtype, q.shape, dev)
     lse = q.new_empty((n_q, heads), dtype=torch.float32) if return_lse else None
-    lib, n_seqs = lib or _lib(), cu_q.shape[0] - 1
+    lib, n_seqs = lib or _lib(), starts[0] - 1
     size = _prompt_workspace(lib, n_seqs, n_q, n_k, max_q, heads, kv_heads, D)
     workspace = q.new_empty(size, dtype=torch.uint8) if size else None
     args = _PROMPT.pack(
