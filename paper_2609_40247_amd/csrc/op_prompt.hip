@@ -857,10 +857,16 @@ static int prompt_join(PromptArgs& p) {
   return launch(k_prompt_join<TYPE, D>, dim3((unsigned)blocks), dim3(256), 0, p.a.hip_stream, p);
 }
 
+// Packed: where a quarter of the grid is left, and the sequences are found in two rounds of
+// the scan (4 heads of 64: 32 x 1 to 300 tokens 12.7 to 7.6 us, 64 x 1 to 300 13.8
+// to 8.7; 3 x 100 to 900 of 16 heads, half the grid, would take 12.0 against 11.0, 200 x
+// 1 to 60 8.0 against 7.7, 400 x 1 to 20 9.6 against 7.4).
+constexpr int PACKED_SEQS = 128;
+
 template <int TYPE, int D>
 static int prompt_few(PromptArgs& p, bool vec) {
   const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, most = p.a.n_q * p.group / 32 + p.a.n_seqs;
-  p.packed = p.a.n_seqs > 1 && p.splits == 1 && most < levels * p.a.n_seqs;
+  p.packed = p.a.n_seqs > 1 && p.a.n_seqs <= PACKED_SEQS && p.splits == 1 && 4 * most <= levels * p.a.n_seqs;
   const int64_t blocks = (p.packed ? most : levels * p.a.n_seqs) * p.a.kv_heads;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
   p.levels = (int)levels;
@@ -901,7 +907,7 @@ static int prompt_launch(PromptArgs& p, bool vec) {
 // against 49, 512 rows, 8.6e9, 57 against 51; 777 rows of 8 heads over 12000 83
 // against 64; of 64, 4096 rows of 4 heads, 4.3e9, 27 against 35).  Heads of 64 gain
 // up to 960 workgroups (16 heads: 24 x 1 to 300 tokens 9.0 us against 10.5, 100 to
-// 900 three times 12.4 against 21.0, 900 twice 16.3 against 21.2, one of 1800 20.3
+// 900 three times 11.0 against 21.0, 900 twice 16.3 against 21.2, one of 1800 20.3
 // against 36.5; 24 x 100, 1296 workgroups, 11.4 against 8.7).
 //
 // Else eight waves (256 rows) or four (128).  Eight in turns are faster where there
@@ -930,7 +936,7 @@ static PromptPlan prompt_plan(int64_t n_seqs, int64_t n_q, int64_t n_k, int64_t 
   const int64_t rows = std::max<int64_t>(1, n_q / n_seqs), keys = n_k / n_seqs;
   int64_t splits = 1;
   const int64_t few = (n_q * (q_heads / kv_heads) / 32 + n_seqs) * kv_heads;  // workgroups of 32 rows, at most
-  if ((n_q * q_heads <= 20480 || (D == 64 && few <= 960)) && n_q * q_heads * keys <= (5ll << 30) / D && max_q * (q_heads / kv_heads) < 0x7fffffe0) {
+  if ((n_q * q_heads <= 20480 || (D == 64 && few <= 960 && n_seqs <= PACKED_SEQS)) && n_q * q_heads * keys <= (5ll << 30) / D && max_q * (q_heads / kv_heads) < 0x7fffffe0) {
     plan.waves = 0;
     splits = std::min<int64_t>(512 / std::max<int64_t>(1, (n_q * q_heads + 31) / 32), keys / 512);
     if (splits < 4 && keys < 8192) splits = 1;

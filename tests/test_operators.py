@@ -476,6 +476,8 @@ RAGGED_CASES = [  # queries, keys, heads, kv heads, D, causal, window
     ([0, 0, 5, 0, 90, 1], [7, 0, 5, 0, 200, 0], 10, 2, 128, True, 40),
     ([(7 * i) % 11 for i in range(150)], None, 2, 2, 64, True, 0),             # beyond 64 sequences
     ([0] * 130 + [70] + [0] * 3 + [33], None, 3, 1, 128, False, 0),
+    ([0] * 70 + [70] + [1, 0, 9] * 16 + [33], None, 3, 1, 128, False, 0),      # the second 64
+    ([200] + [2] * 63 + [150] + [0] * 20, None, 4, 1, 64, True, 60),
 ]
 
 
