@@ -39,7 +39,7 @@
 // twice, vector instructions take half of that.
 //
 // The reference of a row's exponentials moves only when a step's sum shows that
-// one of them is large; no maximum is computed otherwise.  Rows of keys beyond
+// it does not fit (ops.hpp); no maximum is computed otherwise.  Rows of keys beyond
 // the sequence's end, or before all windows, are never read: a hidden key of a
 // step stands at a seen one's row, with the exponential 0.
 #include "ops.hpp"
@@ -60,7 +60,6 @@ constexpr int shares_of_cu(int kind, int row_blocks, int dim) {
   return dim == 64 ? (row_blocks == 1 ? 4 : quantised(kind) ? 3 : 2) : quantised(kind) && row_blocks == 1 ? 3 : 2;
 }
 constexpr float FAR_BELOW = -3.0e38f;
-constexpr float LARGE_SUM = 4096.0f;  // half's largest value is 65504
 
 struct DecodeArgs {
   herschel_decode_args a;
@@ -335,13 +334,15 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           return t;
         };
         float t = exponentials();
-        if (__ballot(!(t <= LARGE_SUM))) {
+        if (Reference<PV>::template off<4>(t)) {
           float top = FAR_BELOW;
 #pragma unroll
           for (int i = 0; i < 8; ++i) top = fmaxf(top, (seen[rb] >> i) & 1 ? sc[rb][i / 4][i % 4] * f[i] : FAR_BELOW);
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float to = fmaxf(ref[rb], top), by = shrink(ref[rb], to);
+          float total = sum[rb] + __shfl_xor(sum[rb], 16);
+          total += __shfl_xor(total, 32);
+          const float to = Reference<PV>::moved(ref[rb], top, total), by = shrink(ref[rb], to);
           ref[rb] = to;
           sum[rb] *= by;
 #pragma unroll

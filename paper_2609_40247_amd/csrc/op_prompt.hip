@@ -19,8 +19,8 @@
 //    spreads a wave's reads over all banks.  V's operand has its keys in a lane:
 //    reads that transpose blocks of four keys by 16 dimensions deliver it.
 //  - The reference of a row's exponentials stays as long as a tile's sum shows
-//    that no exponential is large; then the maximum is taken and the
-//    accumulators scaled.  No maximum is computed otherwise.
+//    that it fits (ops.hpp); else the maximum is taken and the accumulators
+//    scaled.  No maximum is computed otherwise.
 //  - Only tiles in which some row does not see some key are masked.  A hidden
 //    key's exponential is 0, which an infinite or NaN value turns into NaN: a
 //    wave whose sums are not finite at the end computes its rows again, with
@@ -37,7 +37,6 @@ namespace hop {
 
 constexpr int KT = 64;      // keys of a tile
 constexpr float NO_KEY = -3.0e38f;
-constexpr float LARGE = 4096.0f;  // a sum above this moves the reference (half's largest value is 65504)
 
 #define INLINE __attribute__((always_inline))
 
@@ -393,12 +392,13 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
     }
     float s = 0;
     if (!first) s = exponentials();
-    if (first || __ballot(!(s <= LARGE))) {
+    if (first || Reference<TYPE>::template off<2>(s)) {
       float top = sc[0][0];
 #pragma unroll
       for (int i = 1; i < 32; ++i) top = fmaxf(top, sc[i / 16][i % 16]);
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(ref, top * to_log2), by = __builtin_amdgcn_exp2f(ref - next);
+      const float next = Reference<TYPE>::moved(ref, top * to_log2, sum + __shfl_xor(sum, 32));
+      const float by = __builtin_amdgcn_exp2f(ref - next);
       ref = next;
       sum *= by;
 #pragma unroll
@@ -689,12 +689,13 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
     const bool first = k0 == begin + wave * 32;  // moves the reference in any case
     float t = 0;
     if (!first) t = exponentials();
-    if (first || __ballot(!(t <= LARGE))) {
+    if (first || Reference<TYPE>::template off<2>(t)) {
       float top = sc[0];
 #pragma unroll
       for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(ref, top * to_log2), by = __builtin_amdgcn_exp2f(ref - next);
+      const float next = Reference<TYPE>::moved(ref, top * to_log2, sum + __shfl_xor(sum, 32));
+      const float by = __builtin_amdgcn_exp2f(ref - next);
       ref = next;
       sum *= by;
 #pragma unroll

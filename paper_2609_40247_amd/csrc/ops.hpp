@@ -114,6 +114,50 @@ __device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) {
   if (status) atomicOr(status, bit);
 }
 
+// The exponentials of a row are taken against a reference that stays while their
+// sums show that it fits.  The second product takes them in TYPE, its sums and the
+// exponentials' own are 32-bit.  That rounding is a choice: the product runs at the
+// 16-bit rate, and a weight is off by half a last place of what the values
+// themselves are given in (4096 rows of 32 heads in bf16 0.0021 from 64 bits where
+// exponentials of 32 bits give 0.0016, most of it the output's own rounding).
+//
+// bf16 has the exponents of 32 bits, and the reference is the largest score that
+// called for a move.  A half has 2^-24 to 65504: weights far below the largest
+// would be lost from the product and stay in the sum, and where the largest has a
+// value of 0, they are all there is.  So a move puts the largest at 2^6, and the
+// reference moves down too, where a step's sum in a row is below 2^-12: what a key
+// loses is at most 2^-25, 2^-31 of the row's largest, and with the 32 keys of a
+// lane 2^-8 of what the step has.  Moves cost a step's exponentials twice, and
+// rows whose scores spread over 20 powers of two move often: with a tenth of the
+// heads so, prompts in half take 4 to 14% longer (4096 rows of 32 heads of 128 164
+// us against 148), without such heads under 1%.
+template <int TYPE>
+struct Reference {
+  static constexpr bool HALF = TYPE == HERSCHEL_F16;
+  static constexpr float TOP = HALF ? 6.0f : 0.0f;           // a move up puts the largest at 2^TOP
+  static constexpr float LARGE = HALF ? 65504.0f : 4096.0f;  // a lane's sum above this moves it up
+  static constexpr float SMALL = 0x1p-12f;                   // below this, in all of a row's lanes, down
+  static constexpr float LOW = -4.0f;                        // a move down puts the largest at 2^LOW
+  // A step's sums s, PARTS lanes (64 / PARTS apart) to a row: whether the reference may have to move.
+  template <int PARTS>
+  static __device__ __forceinline__ bool off(float s) {
+    if constexpr (!HALF) return __ballot(!(s <= LARGE)) != 0;
+    constexpr uint32_t FROM = __builtin_bit_cast(uint32_t, SMALL), TO = __builtin_bit_cast(uint32_t, LARGE);
+    if (__ballot(__builtin_bit_cast(uint32_t, s) - FROM > TO - FROM) == 0) return false;  // most steps; NaN is above
+    uint64_t low = __ballot(s < SMALL), some = __ballot(s > 0.0f);
+#pragma unroll
+    for (int o = 32; o >= WAVE / PARTS; o /= 2) low &= low >> o, some |= some >> o;
+    return (__ballot(!(s <= LARGE)) | (low & some & (~0ull >> (WAVE - WAVE / PARTS)))) != 0;
+  }
+  // The reference after a step whose largest score (a power of two) is top, for a row whose sum so far is
+  // total.  Down by no more than leaves that sum below 2^100: what lies 2^100 below it is nothing.
+  static __device__ __forceinline__ float moved(float ref, float top, float total) {
+    if (HALF && top < ref - 11.0f && top > -3.0e38f)
+      return fmaxf(top - LOW, ref + __builtin_amdgcn_logf(total) - 100.0f);
+    return fmaxf(ref, top - TOP);
+  }
+};
+
 // 16 bytes that may lie at any element (2 bytes).
 __device__ __forceinline__ u32x4 load_elements(const uint16_t* p) {
   u32x4 r;

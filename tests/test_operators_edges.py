@@ -1,0 +1,136 @@
+"""The reference operators where their inputs are extreme.
+
+Bounds are derived as in the operators' other tests.  For half rows one term
+joins them.  The exponentials enter the second product as halves: above 2^-14
+they are off by half a last place, below that by 2^-25 at most, where the row's
+largest stands at 2^6 or above when it is met.  So a key loses at most 2^-31 of
+the largest weight; and where a step's keys have so little that a lane's sum (of
+8 to 32 keys) would be below 2^-12, the reference moves and puts the step's
+largest at 2^-4: keys within 9 powers of two of it lose no more than half a last
+place.
+"""
+from __future__ import annotations
+
+import pytest
+import torch
+
+from paper_2609_40247_amd import operators as O
+from test_operators import DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand
+
+
+# ------------------------------------------------------------ weights far below a row's largest
+def sinking(nq, nk, hq, hk, D, at, gap, seed=0):
+    """Half rows: key `at` has the largest score of every query and the value 0; the others' scores lie gap[0] to
+    gap[1] below it (and a little noise), their values from 0.5 to 1.5."""
+    q, k = rand(nq, hq, D, seed=seed, dtype=HF, gain=0.02), rand(nk, hk, D, seed=seed + 1, dtype=HF)
+    u = torch.rand(nk, hk, generator=torch.Generator().manual_seed(seed + 2))
+    q[:, :, 0] = 8
+    k[:, :, 0] = (-(gap[0] + (gap[1] - gap[0]) * u) / 8).to(HF)
+    v = (torch.rand(nk, hk, D, generator=torch.Generator().manual_seed(seed + 3)) + 0.5).to(HF)
+    k[at, :, 0] = 0
+    v[at] = 0
+    return q, k, v
+
+
+def check_sunk(out, lse, ref, n_keys, D, gap):
+    """`check_attention` with the halves' further term; the values are at most 1.5."""
+    # from 17 on a lane's 32 keys sum to less than 32 e^-17 2^6 = 2^-13.5: of all steps but the largest key's own (64 keys
+    # at most) the reference moves, and the keys lie within 6 (8.7 powers of two) and the noise of each other
+    lost = (64 if gap[0] > 17 else n_keys) * 2.0 ** -31 * 1.5
+    o, l, A, S = ref
+    d = (D + 8) * 2.0 ** -24 * S
+    tol = (U[HF] * o.abs() + (1 + 2.0 ** -7) * ((U[HF] + 2 * d[..., None] + (n_keys + 16) * 2.0 ** -23) * A + lost) +
+           2.0 ** -25)
+    err = (out.double().cpu() - o).abs()
+    assert (err <= tol).all(), (err.max(), tol[err == err.max()])
+    if lse is not None:
+        assert ((lse.double().cpu() - l).abs() <= d + (n_keys + 16) * 2.0 ** -23 + 2.0 ** -22 * l.abs()).all()
+
+
+GAPS = [(17.4, 17.4), (10.0, 17.5), (24.0, 30.0)]
+SINK_CASES = [  # queries, keys, heads, kv heads, D, rows of another sequence that sees no key, key with the largest score
+    (20, 12_000, 4, 1, 64, 0, 0),           # parts of few rows
+    (20, 12_000, 4, 2, 128, 0, 7000),
+    (100, 2000, 2, 1, 128, 0, 0),           # few rows
+    (100, 2000, 2, 1, 64, 0, 1999),
+    (40, 3000, 4, 1, 128, 8000, 0),         # workgroups of 128 rows
+    (40, 3000, 4, 2, 64, 12_000, 1500),
+    (1400, 5000, 8, 2, 128, 0, 0),          # and in parts
+]
+
+
+@gpu
+@pytest.mark.parametrize("gap", GAPS, ids=str)
+@pytest.mark.parametrize("case", SINK_CASES, ids=str)
+def test_weights_far_below_the_largest(case, gap):
+    """One key takes nearly all the weight and has the value 0: the output is what thousands of small weights give."""
+    nq, nk, hq, hk, D, more, at = case
+    q, k, v = sinking(nq, nk, hq, hk, D, at, gap)
+    rest = torch.zeros(more, hq, D, dtype=HF)
+    cu_q, cu_k = (torch.tensor(c, dtype=torch.int32, device=DEV) for c in ([0, nq, nq + more], [0, nk, nk]))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    n = 3 if more else 2
+    out, lse = O.attn_prompt(torch.cat([q, rest]).to(DEV), k.to(DEV), v.to(DEV), cu_q[:n].contiguous(), cu_k[:n].contiguous(),
+                             max_q=max(nq, more), scale=1.0, causal=False, return_lse=True, status=status)
+    assert status.item() == 0
+    rows = [r for r in (0, 1, 31, 32, 39, 99, 127, 128, 700, 1399) if r < nq]
+    check_sunk(out[rows], lse[rows], exact_attention(q[rows], k, v, 1.0, False, 0), nk, D, gap)
+
+
+@gpu
+@pytest.mark.parametrize("gap", GAPS, ids=str)
+def test_weights_far_below_the_largest_of_long_prompts(gap):
+    """The same in workgroups of 256 rows; the largest score in the last tile of one sequence, in a middle one of the other."""
+    n, m, hq, hk, D = 1024, [1500, 2100], 128, 2, 128
+    parts = [sinking(n, x, hq, hk, D, at, gap, seed=10 * i) for i, (x, at) in enumerate(zip(m, (1499, 700)))]
+    q, k, v = (torch.cat(t) for t in zip(*parts))
+    cu_q, cu_k = (torch.tensor(c, dtype=torch.int32, device=DEV) for c in ([0, n, 2 * n], [0, m[0], sum(m)]))
+    out, lse = O.attn_prompt(q.to(DEV), k.to(DEV), v.to(DEV), cu_q, cu_k, max_q=n, scale=1.0, causal=False, return_lse=True)
+    for i, (x, (pq, pk, pv)) in enumerate(zip(m, parts)):
+        for r in (0, 33, 255, 256, 1023):
+            for h in (0, 63, 64, 127):
+                ref = exact_attention(pq[r:r + 1, h:h + 1], pk[:, h // 64:h // 64 + 1], pv[:, h // 64:h // 64 + 1], 1.0, False, 0)
+                check_sunk(out[i * n + r:i * n + r + 1, h:h + 1], lse[i * n + r:i * n + r + 1, h:h + 1], ref, x, D, gap)
+
+
+@gpu
+@pytest.mark.parametrize("gap", GAPS, ids=str)
+@pytest.mark.parametrize("lens,hq,hk,D,new,at", [([12_000], 4, 1, 64, 1, 0), ([3000, 700], 4, 2, 128, 1, 600),
+                                                 ([131_000], 2, 2, 64, 1, 5), ([5000, 200], 20, 1, 128, 2, 3)], ids=str)
+def test_decode_weights_far_below_the_largest(lens, hq, hk, D, new, at, gap):
+    page = 64
+    c = make_cache(HF, sum(-(-n // page) for n in lens) + 1, hk, page, D)
+    bt = paged(c, lens, 3)
+    q = torch.empty(len(lens), new, hq, D, dtype=HF)
+    for b, n in enumerate(lens):
+        q[b], k, v = sinking(new, n, hq, hk, D, at, gap, seed=10 * b)
+        ids = bt[b, :-(-n // page)].long()
+        for t, x in ((c.k, k), (c.v, v)):
+            whole = torch.zeros(len(ids) * page, hk, D, dtype=HF)
+            whole[:n] = x
+            t[ids.to(DEV)] = whole.view(len(ids), page, hk, D).transpose(1, 2).contiguous().to(DEV)
+    dec = O.DecodeAttention(c, batch=len(lens), heads=hq, new_tokens=new, dtype=HF)
+    out, lse = dec(q.to(DEV), bt.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), scale=1.0, return_lse=True)
+    c.check()
+    for b, (k, v) in enumerate(dense(c, bt, lens)):
+        check_sunk(out[b], lse[b], exact_attention(q[b], k, v, 1.0, True, 0), lens[b], D, gap)
+
+
+@gpu
+@pytest.mark.parametrize("gap", GAPS, ids=str)
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_weights_far_below_the_largest_of_long_shares(D, gap):
+    """So many sequences and heads that a workgroup goes through most of a sequence; all of them share one's pages."""
+    n, page, heads, B = 3000, 256, 32, 16
+    c = make_cache(HF, -(-n // page), heads, page, D)
+    q, k, v = sinking(1, n, heads, heads, D, 1, gap)
+    for t, x in ((c.k, k), (c.v, v)):
+        whole = torch.zeros(c.n_pages * page, heads, D, dtype=HF)
+        whole[:n] = x
+        t.copy_(whole.view(c.n_pages, page, heads, D).transpose(1, 2))
+    bt = torch.arange(c.n_pages, dtype=torch.int32, device=DEV).repeat(B, 1)
+    dec = O.DecodeAttention(c, batch=B, heads=heads, dtype=HF)
+    out = dec(q.expand(B, 1, heads, D).contiguous().to(DEV), bt, torch.full((B,), n, dtype=torch.int32, device=DEV), scale=1.0)
+    ref = exact_attention(q, k, v, 1.0, True, 0)
+    for b in range(B):
+        check_sunk(out[b], None, ref, n, D, gap)
