@@ -41,7 +41,10 @@
 // The reference of a row's exponentials moves only when a step's sum shows that
 // it does not fit (ops.hpp); no maximum is computed otherwise.  Rows of keys beyond
 // the sequence's end, or before all windows, are never read: a hidden key of a
-// step stands at a seen one's row, with the exponential 0.
+// step stands at a seen one's row, with the exponential 0.  An infinity or a NaN
+// times that 0 is a NaN, and so is an infinity whose weight is too small for 32
+// bits: a wave whose sums are not finite goes over its keys once more, with such
+// values taken out of the products and added to the rows that see them.
 #include "ops.hpp"
 
 namespace hop {
@@ -225,13 +228,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
     }
     f32x4 o[RB][ND];
     float ref[RB], sum[RB];
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      ref[rb] = FAR_BELOW;
-      sum[rb] = 0;
-#pragma unroll
-      for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
-    }
+    bool apart = false;  // values that are not finite are kept out of the products
     // A lane's places in a run of 16 keys: its key's row, the first of its four values' rows, their scales.
     const uint32_t koff = m * (D * CB) + 16 * g, voff = 4 * g * (D * CB) + m * (ND * CB), soff = 4 * g;
     auto load_v = [&](uint32_t* to, const char* from) INLINE {  // whole rows, read once: past the caches (32 x 4096 in bf16 102 to 93 us)
@@ -387,10 +384,8 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           vt[0][j] = __builtin_amdgcn_perm(y, x, 0x05040100);
           vt[1][j] = __builtin_amdgcn_perm(y, x, 0x07060302);
         }
-        // A value that is not finite must reach the rows that see its key and no
-        // other: where rows differ, or none sees what a bad page id stands for, it
-        // is taken out of the product, and added.
-        if (KIND != HERSCHEL_INT8 && edge && (p.a.new_tokens > 1 || !s.live[0] || !s.live[1])) {
+        // A value that is not finite must reach the rows that see its key, and no other.
+        if (KIND != HERSCHEL_INT8 && apart) {
           constexpr uint32_t ONE = PV == HERSCHEL_BF16 ? 0x3f80u : 0x3c00u;
           constexpr uint32_t INF = PV == HERSCHEL_BF16 ? 0x7f80u : 0x7c00u;
 #pragma unroll
@@ -438,10 +433,31 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
       }
     };
     Step s;
-    for (; k0 < key_end; k0 += TILE) {
-      load(s, k0, page);
-      find(k0 + TILE, page);
-      work(s, k0);
+    for (;;) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        ref[rb] = FAR_BELOW;
+        sum[rb] = 0;
+#pragma unroll
+        for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
+      }
+      for (; k0 < key_end; k0 += TILE) {
+        load(s, k0, page);
+        find(k0 + TILE, page);
+        work(s, k0);
+      }
+      if (KIND == HERSCHEL_INT8 || apart) break;  // int8's codes are finite, what their scales make is a row's own
+      float check = 0;                            // NaN if a sum is not finite
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int n = 0; n < ND; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) check = __builtin_fmaf(o[rb][n][i], 0.0f, check);
+      if (!__ballot(!(check == 0))) break;
+      apart = true;
+      k0 = key_begin + wave * 32;
+      if (k0 < key_end) find(k0, page);
     }
 
     // The four waves' parts of these rows, joined through LDS block by block.

@@ -11,11 +11,13 @@ place.
 """
 from __future__ import annotations
 
+import math
+
 import pytest
 import torch
 
 from paper_2609_40247_amd import operators as O
-from test_operators import DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand
+from test_operators import BF, DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand, run_decode
 
 
 # ------------------------------------------------------------ weights far below a row's largest
@@ -134,3 +136,40 @@ def test_decode_weights_far_below_the_largest_of_long_shares(D, gap):
     ref = exact_attention(q, k, v, 1.0, True, 0)
     for b in range(B):
         check_sunk(out[b], None, ref, n, D, gap)
+
+
+# ------------------------------------------------------------ values that are not finite
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("lens,D,window", [([37, 64, 129, 1], 128, 0), ([160, 33, 31], 64, 0), ([200, 97], 128, 50),
+                                           ([300, 4000], 64, 64)], ids=str)
+def test_decode_infinite_values_of_seen_keys(lens, D, window, dtype):
+    """One new token: infinities in the last key's value and in the first one's that is seen stay infinities, at lengths
+    that end inside a step and at its end."""
+    page = 16
+
+    def edit(c, bt):
+        for b, n in enumerate(lens):
+            first = max(0, n - window) if window else 0
+            for key, head, d, x in ((n - 1, 0, 3, math.inf), (n - 1, 1, 4, -math.inf), (first, 0, 5, -math.inf),
+                                    (first, 1, 6, math.inf), (n - 1, 1, 7, math.nan)):
+                c.v[int(bt[b, key // page]), head, key % page, d] = x
+    run_decode(lens, 4, 2, D, dtype, dtype, page, window=window, edit=edit)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("D,new", [(64, 1), (128, 1), (64, 2)])
+def test_decode_infinite_values_of_small_weights(D, new, dtype):
+    """A key hundreds below the largest score, with an infinite value: its weight is no longer a 32-bit number, but not 0."""
+    lens, page, heads = [300, 64], 32, 2
+
+    def edit(c, bt):
+        q = rand(len(lens), new, heads, D, seed=2, dtype=dtype)  # the call's own rows
+        for b, n in enumerate(lens):
+            for h in range(heads):
+                for key in (20, n - 30):
+                    at = int(bt[b, key // page]), h, key % page
+                    c.k[at] = (-16 * q[b].float().sum(0)[h] * (1.0 if new == 1 else 0.5)).to(dtype).to(DEV)
+                    c.v[at][5] = math.inf
+    run_decode(lens, heads, heads, D, dtype, dtype, page, new=new, edit=edit)
