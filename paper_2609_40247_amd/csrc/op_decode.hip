@@ -45,6 +45,8 @@
 // times that 0 is a NaN, and so is an infinity whose weight is too small for 32
 // bits: a wave whose sums are not finite goes over its keys once more, with such
 // values taken out of the products and added to the rows that see them.
+#include <type_traits>
+
 #include "ops.hpp"
 
 namespace hop {
@@ -130,9 +132,9 @@ __device__ __forceinline__ void scan_line(const DecodeArgs& p, int* s_pre, int* 
   __syncthreads();
 }
 
-// Factor of sums whose reference moves up; never 0, so that an infinite sum stays one.
-__device__ __forceinline__ float shrink(float from, float to) {
-  return fmaxf(__builtin_amdgcn_exp2f(from - to), 0x1p-126f);
+// Factor of sums whose reference moves; of none, which are 0, 1.
+__device__ __forceinline__ float factor(float from, float to) {
+  return from > FAR_BELOW ? __builtin_amdgcn_exp2f(from - to) : 1.0f;
 }
 
 // a / b of numbers that are not negative: a 64-bit division takes a microsecond.
@@ -280,6 +282,12 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
         }
       }
     };
+    // Factor of sums whose reference moves.  0 times an infinity would be a NaN: the second pass starts from the first's
+    // last reference, from which bf16's goes up by a few powers of two at most, and a half times 2^-126 is nothing.
+    auto moved_by = [](float from, float to) INLINE {
+      const float by = __builtin_amdgcn_exp2f(from - to);
+      return PV == HERSCHEL_F16 ? fmaxf(by, 0x1p-126f) : by;
+    };
     auto work = [&](Step& s, int k0) INLINE {
       // S^T = K Q^T
       f32x4 sc[RB][2];
@@ -339,7 +347,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           top = fmaxf(top, __shfl_xor(top, 32));
           float total = sum[rb] + __shfl_xor(sum[rb], 16);
           total += __shfl_xor(total, 32);
-          const float to = Reference<PV>::moved(ref[rb], top, total), by = shrink(ref[rb], to);
+          const float to = Reference<PV>::moved(ref[rb], top, total), by = moved_by(ref[rb], to);
           ref[rb] = to;
           sum[rb] *= by;
 #pragma unroll
@@ -432,11 +440,12 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           }
       }
     };
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) ref[rb] = FAR_BELOW;
     Step s;
     for (;;) {
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
-        ref[rb] = FAR_BELOW;
         sum[rb] = 0;
 #pragma unroll
         for (int n = 0; n < ND; ++n) o[rb][n] = f32x4{0, 0, 0, 0};
@@ -455,7 +464,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
 #pragma unroll
           for (int i = 0; i < 4; ++i) check = __builtin_fmaf(o[rb][n][i], 0.0f, check);
       if (!__ballot(!(check == 0))) break;
-      apart = true;
+      apart = true;  // from the reference that this pass ended with
       k0 = key_begin + wave * 32;
       if (k0 < key_end) find(k0, page);
     }
@@ -493,10 +502,15 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
         for (int n = 0; n < ND; ++n) acc[n] = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const float by = shrink(all[w * WS + D], top);
+          const float by = factor(all[w * WS + D], top);
           den += all[w * WS + D + 1] * by;
+          if (by != 0) {
 #pragma unroll
-          for (int n = 0; n < ND; ++n) acc[n] += all[w * WS + d0 + n] * by;
+            for (int n = 0; n < ND; ++n) acc[n] += all[w * WS + d0 + n] * by;
+          } else {
+#pragma unroll
+            for (int n = 0; n < ND; ++n) acc[n] += weighted(all[w * WS + d0 + n], by);
+          }
         }
         if (whole) {
           const float inv = den > 0 ? 1.0f / den : den == 0 ? 0.0f : den;  // no key seen: 0; NaN stays
@@ -504,8 +518,7 @@ __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(Decod
           uint32_t* out = (uint32_t*)((uint16_t*)p.a.out + at * D + d0);
 #pragma unroll
           for (int n = 0; n < ND; n += 2) out[n / 2] = pack2<TYPE>(acc[n] * inv, acc[n + 1] * inv);
-          if (p.a.lse && tid % 16 == 0)
-            p.a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+          if (p.a.lse && tid % 16 == 0) p.a.lse[at] = log_sum(top, den);
         } else {
           float* to = p.part + (slot * (RB * 16) + rb * 16 + tid / 16) * (D + 2);
 #pragma unroll
@@ -534,21 +547,35 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
   if (span.x < 0) return;
   const int first = span.x / 2, last = span.y;  // shares; a later share's part is its first
   const int lane = threadIdx.x % 16, group = threadIdx.x / 16;
-  float top = FAR_BELOW, den = 0, acc[ND];
-#pragma unroll
-  for (int n = 0; n < ND; ++n) acc[n] = 0;
-  auto add = [&](const float* from) INLINE {
+  float top, den, acc[ND];
+  // Sums that are not finite are joined again with infinities kept where a factor is 0.
+  auto add = [&](const float* from, auto kept) INLINE {
     const float t = from[D], to = fmaxf(top, t);
-    const float old = shrink(top, to), by = shrink(t, to);
+    const float old = factor(top, to), by = factor(t, to);
     den = den * old + from[D + 1] * by;
 #pragma unroll
-    for (int n = 0; n < ND; ++n) acc[n] = acc[n] * old + from[lane * ND + n] * by;
+    for (int n = 0; n < ND; ++n)
+      if constexpr (kept) acc[n] = weighted(acc[n], old) + weighted(from[lane * ND + n], by);
+      else acc[n] = acc[n] * old + from[lane * ND + n] * by;
     top = to;
   };
-  for (int w = first + group; w <= last; w += 16) {
-    const int64_t slot = w == first ? span.x : 2 * w;
-    add(p.part + (slot * (RB * 16) + r % (RB * 16)) * (D + 2));
-  }
+  auto finite = [&]() INLINE {
+    float check = 0;
+#pragma unroll
+    for (int n = 0; n < ND; ++n) check = __builtin_fmaf(acc[n], 0.0f, check);
+    return check == 0;
+  };
+  auto of_group = [&](auto kept) INLINE {
+    top = FAR_BELOW, den = 0;
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = 0;
+    for (int w = first + group; w <= last; w += 16) {
+      const int64_t slot = w == first ? span.x : 2 * w;
+      add(p.part + (slot * (RB * 16) + r % (RB * 16)) * (D + 2), kept);
+    }
+  };
+  of_group(std::false_type());
+  if (!finite()) of_group(std::true_type());
 #pragma unroll
   for (int n = 0; n < ND; ++n) s_part[group][lane * ND + n] = acc[n];
   if (lane == 0) {
@@ -557,14 +584,20 @@ __global__ __launch_bounds__(256) void k_decode_join(DecodeArgs p) {
   }
   __syncthreads();
   if (group) return;
-  for (int i = 1; i < 16 && i <= last - first; ++i) add(s_part[i]);
+  const float own_top = top, own_den = den;
+  for (int i = 1; i < 16 && i <= last - first; ++i) add(s_part[i], std::false_type());
+  if (!finite()) {
+    top = own_top, den = own_den;
+#pragma unroll
+    for (int n = 0; n < ND; ++n) acc[n] = s_part[0][lane * ND + n];
+    for (int i = 1; i < 16 && i <= last - first; ++i) add(s_part[i], std::true_type());
+  }
   const float inv = den > 0 ? 1.0f / den : den == 0 ? 0.0f : den;
   const int64_t at = ((int64_t)b * p.a.new_tokens + r / p.group) * p.a.q_heads + head * p.group + r % p.group;
   uint32_t* out = (uint32_t*)((uint16_t*)p.a.out + at * D + lane * ND);
 #pragma unroll
   for (int n = 0; n < ND; n += 2) out[n / 2] = pack2<TYPE>(acc[n] * inv, acc[n + 1] * inv);
-  if (p.a.lse && lane == 0)
-    p.a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+  if (p.a.lse && lane == 0) p.a.lse[at] = log_sum(top, den);
 }
 
 template <int TYPE, int KIND, int D, int RB>

@@ -30,6 +30,7 @@
 // 2001 to 8192 rows 692 us, 1036 TFLOP/s, where a matrix product of 8192 cubed
 // reaches 1200.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.hpp"
 
@@ -131,8 +132,8 @@ __device__ __forceinline__ void reads_ahead() {
 
 // A row's outputs from the keys [lo, hi) alone, by a wave: 64 keys at a time, a
 // key to a lane for the scores, then a dimension (or two) to a lane for the
-// values, 32 rows asked for at once.  Factors are never 0, so that an infinite
-// value or sum stays one.  4096 rows of 32 heads of 128 that all see a NaN: 14 ms (a key at a time 46).
+// values, 32 rows asked for at once.  An infinite value or sum stays one, also
+// where its weight is too small for 32 bits.  4096 rows of 32 heads of 128 that all see a NaN: 15 ms (a key at a time 46).
 template <int TYPE, int D>
 __device__ __forceinline__ void row_by_key(const uint16_t* q, const uint16_t* kbase, const uint16_t* vbase,
                                            const herschel_prompt_args& a, int lo, int hi, int64_t at) {
@@ -176,40 +177,44 @@ __device__ __forceinline__ void row_by_key(const uint16_t* q, const uint16_t* kb
     float next = fmaxf(top, lane < n ? x : top);
 #pragma unroll
     for (int m = 1; m < WAVE; m *= 2) next = fmaxf(next, __shfl_xor(next, m));
-    const float by = fmaxf(__builtin_amdgcn_exp2f(top - next), 0x1p-126f);
-    float e = __builtin_amdgcn_exp2f(x - next);
-    if (e == 0) e = 0x1p-126f;
-    if (lane >= n) e = 0;
+    const float by = __builtin_amdgcn_exp2f(top - next);
+    const float e = lane < n ? __builtin_amdgcn_exp2f(x - next - 30.0f) : 0.0f;  // as bf16's reference (ops.hpp)
     top = next;
     float total = e;
 #pragma unroll
     for (int m = 1; m < WAVE; m *= 2) total += __shfl_xor(total, m);
     den = den * by + total;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) acc[d] *= by;
+    for (int d = 0; d < ND; ++d) acc[d] = weighted(acc[d], by);
     const uint16_t* v = vbase + k0 * a.v_strides.row + lane;
-    for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
-      uint16_t w[AT_ONCE][ND];
+    auto values = [&](auto small) INLINE {  // small: some weights are too small for 32 bits
+      for (int i0 = 0; i0 < n; i0 += AT_ONCE) {
+        uint16_t w[AT_ONCE][ND];
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i)
+        for (int i = 0; i < AT_ONCE; ++i)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) w[i][d] = v[min(i0 + i, n - 1) * a.v_strides.row + d * WAVE];
+          for (int d = 0; d < ND; ++d) w[i][d] = v[min(i0 + i, n - 1) * a.v_strides.row + d * WAVE];
 #pragma unroll
-      for (int i = 0; i < AT_ONCE; ++i) {
-        const float f = of_lane(e, min(i0 + i, n - 1));
+        for (int i = 0; i < AT_ONCE; ++i) {
+          const float f = of_lane(e, min(i0 + i, n - 1));
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          float y;
-          unpack2<TYPE>(w[i][d], y, unused);
-          acc[d] += i0 + i < n ? f * y : 0.0f;
+          for (int d = 0; d < ND; ++d) {
+            float y;
+            unpack2<TYPE>(w[i][d], y, unused);
+            if constexpr (small) y = weighted(y, f);
+            else y *= f;
+            acc[d] += i0 + i < n ? y : 0.0f;
+          }
         }
       }
-    }
+    };
+    if (__ballot(lane < n && e == 0)) values(std::true_type());
+    else values(std::false_type());
   }
 #pragma unroll
   for (int d = 0; d < ND; ++d)
     ((uint16_t*)a.out)[at * D + d * WAVE + lane] = (uint16_t)pack2<TYPE>(den == 0 ? 0.0f : acc[d] / den, 0.0f);
-  if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+  if (a.lse && lane == 0) a.lse[at] = log_sum(top + 30.0f, den);
 }
 
 template <int TYPE, int D, int WAVES, bool VEC, bool SPLIT>
@@ -525,7 +530,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
       *(u32x2*)out = u32x2{pack2<TYPE>(o[d][4 * i] * inv, o[d][4 * i + 1] * inv),
                            pack2<TYPE>(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv)};
     }
-  if (a.lse && g == 0) a.lse[at] = sum == 0 ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * 0.69314718055994530942f;
+  if (a.lse && g == 0) a.lse[at] = log_sum(ref, sum);
 }
 
 // Few rows: 32 to a workgroup, whose four waves share the keys, 32 at a time.
@@ -784,7 +789,7 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
     uint16_t* out = (uint16_t*)a.out + at * D + 32 * (x / 16) + 8 * (x % 16 / 4) + 4 * g;
     *(u32x2*)out = u32x2{pack2<TYPE>(acc[i] * inv, acc[i + 1] * inv), pack2<TYPE>(acc[i + 2] * inv, acc[i + 3] * inv)};
   }
-  if (a.lse && g == 0 && wave == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+  if (a.lse && g == 0 && wave == 0) a.lse[at] = log_sum(top, den);
 }
 
 // Joins the parts of each row: a wave per row, four rows in turn.
@@ -847,7 +852,7 @@ __global__ __launch_bounds__(256) void k_prompt_join(PromptArgs p) {
     uint16_t* out = (uint16_t*)a.out + at * D + lane * ND;
     if constexpr (ND == 2) *(uint32_t*)out = pack2<TYPE>(acc[0] * inv, acc[1] * inv);
     else *out = (uint16_t)pack2<TYPE>(acc[0] * inv, 0.0f);
-    if (a.lse && lane == 0) a.lse[at] = den == 0 ? -INFINITY : (top + __builtin_amdgcn_logf(den)) * 0.69314718055994530942f;
+    if (a.lse && lane == 0) a.lse[at] = log_sum(top, den);
   }
 }
 

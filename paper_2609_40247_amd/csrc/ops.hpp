@@ -121,8 +121,8 @@ __device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) {
 // themselves are given in (4096 rows of 32 heads in bf16 0.0021 from 64 bits where
 // exponentials of 32 bits give 0.0016, most of it the output's own rounding).
 //
-// bf16 has the exponents of 32 bits, and the reference is the largest score that
-// called for a move.  A half has 2^-24 to 65504: weights far below the largest
+// bf16 has the exponents of 32 bits: the largest that called for a move stands at
+// 2^-30, so that sums of the largest values over a million keys stay numbers.  A half has 2^-24 to 65504: weights far below the largest
 // would be lost from the product and stay in the sum, and where the largest has a
 // value of 0, they are all there is.  So a move puts the largest at 2^6, and the
 // reference moves down too, where a step's sum in a row is below 2^-12: what a key
@@ -134,10 +134,10 @@ __device__ __forceinline__ void flag(uint32_t* status, uint32_t bit) {
 template <int TYPE>
 struct Reference {
   static constexpr bool HALF = TYPE == HERSCHEL_F16;
-  static constexpr float TOP = HALF ? 6.0f : 0.0f;           // a move up puts the largest at 2^TOP
-  static constexpr float LARGE = HALF ? 65504.0f : 4096.0f;  // a lane's sum above this moves it up
-  static constexpr float SMALL = 0x1p-12f;                   // below this, in all of a row's lanes, down
-  static constexpr float LOW = -4.0f;                        // a move down puts the largest at 2^LOW
+  static constexpr float TOP = HALF ? 6.0f : -30.0f;           // a move up puts the largest at 2^TOP
+  static constexpr float LARGE = HALF ? 65504.0f : 0x1p-18f;  // a lane's sum above this moves it up
+  static constexpr float SMALL = 0x1p-12f;                    // below this, in all of a row's lanes, down
+  static constexpr float LOW = -4.0f;                         // a move down puts the largest at 2^LOW
   // A step's sums s, PARTS lanes (64 / PARTS apart) to a row: whether the reference may have to move.
   template <int PARTS>
   static __device__ __forceinline__ bool off(float s) {
@@ -150,13 +150,23 @@ struct Reference {
     return (__ballot(!(s <= LARGE)) | (low & some & (~0ull >> (WAVE - WAVE / PARTS)))) != 0;
   }
   // The reference after a step whose largest score (a power of two) is top, for a row whose sum so far is
-  // total.  Down by no more than leaves that sum below 2^100: what lies 2^100 below it is nothing.
+  // total.  Down by no more than leaves that sum below 2^60: what lies 2^60 below it is nothing.
   static __device__ __forceinline__ float moved(float ref, float top, float total) {
     if (HALF && top < ref - 11.0f && top > -3.0e38f)
-      return fmaxf(top - LOW, ref + __builtin_amdgcn_logf(total) - 100.0f);
+      return fmaxf(top - LOW, ref + __builtin_amdgcn_logf(total) - 60.0f);
     return fmaxf(ref, top - TOP);
   }
 };
+
+// x times a weight that may be too small for 32 bits: 0 then, but an infinity or a NaN stays one.
+__device__ __forceinline__ float weighted(float x, float by) { return by != 0 ? x * by : x - x == 0 ? 0.0f : x; }
+
+// Natural log of sum times 2 to the ref.
+__device__ __forceinline__ float log_sum(float ref, float sum) {
+  if (sum == 0) return -INFINITY;
+  return (ref + (float)__builtin_amdgcn_frexp_expf(sum) + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(sum))) *
+         0.69314718055994530942f;
+}
 
 // 16 bytes that may lie at any element (2 bytes).
 __device__ __forceinline__ u32x4 load_elements(const uint16_t* p) {

@@ -17,7 +17,7 @@ import pytest
 import torch
 
 from paper_2609_40247_amd import operators as O
-from test_operators import BF, DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand, run_decode
+from test_operators import BF, DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand, run_decode, run_prompt
 
 
 # ------------------------------------------------------------ weights far below a row's largest
@@ -173,3 +173,58 @@ def test_decode_infinite_values_of_small_weights(D, new, dtype):
                     c.k[at] = (-16 * q[b].float().sum(0)[h] * (1.0 if new == 1 else 0.5)).to(dtype).to(DEV)
                     c.v[at][5] = math.inf
     run_decode(lens, heads, heads, D, dtype, dtype, page, new=new, edit=edit)
+
+
+# ------------------------------------------------------------ huge values
+@gpu
+@pytest.mark.parametrize("low", [32, 128, 1024])
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_huge_values_of_small_weights(D, low):
+    """The first keys lie hundreds below the others' scores and have values of 1e36: nothing of them is left, whether the
+    higher scores come in the same wave, in another one or in another workgroup."""
+    lens, page, heads = [4000, low + 1, low + 40], 16, 2
+
+    def edit(c, bt):
+        q = rand(len(lens), 1, heads, D, seed=2)
+        for b in range(len(lens)):
+            for key in range(low):
+                at = int(bt[b, key // page]), slice(None), key % page
+                c.k[at] = (-16 * q[b, 0]).to(DEV)
+                c.v[at] = 1e36
+    run_decode(lens, heads, heads, D, BF, BF, page, edit=edit)
+
+
+@gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("more", [0, 16_000])
+def test_prompt_huge_values_of_small_weights(D, more):
+    """The same of prompts, also in rows that see a NaN in another dimension."""
+    for bad in (False, True):
+        def edit(q, k, v):
+            q[:, :, 0] = 16
+            k[:, :, 0] = 0
+            k[:70, :, 0] = -16.0 * D ** 0.5
+            v[:70] = 1e36
+            if bad:
+                v[100, :, 5] = math.nan
+        run_prompt([40, more], [150, 0], 2, 1, D, BF, False, 0, edit=edit)
+
+
+@gpu
+@pytest.mark.parametrize("D", [64, 128])
+def test_largest_values(D):
+    """Values of 3e38 under equal scores: their mean is a number, though their sum is none."""
+    for bad in (False, True):
+        def edit(q, k, v):
+            q *= 0
+            v[:] = 3e38
+            v[:, :, 1] = -3e38
+            if bad:
+                v[7, :, 5] = math.nan
+        run_prompt([40], [3000], 2, 1, D, BF, False, 0, edit=edit)            # parts of few rows
+        run_prompt([40, 16_000], [1000, 0], 2, 1, D, BF, False, 0, edit=edit)
+
+    def fill(c, bt):
+        c.k.zero_()
+        c.v.fill_(3e38)
+    run_decode([3000, 33], 4, 2, D, BF, BF, 16, edit=fill)
