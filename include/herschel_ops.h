@@ -123,10 +123,11 @@ typedef struct {
   herschel_strides q_strides, k_strides, v_strides;
   void *out;                  /* [n_q][q_heads][head_dim] contiguous, 8-byte aligned */
   float *lse;                 /* [n_q][q_heads] or NULL: log of the sum of exp(scale q.k) over the keys seen */
-  const int32_t *cu_q, *cu_k; /* [n_seqs + 1]: first query and first key row of each sequence; cu[0] = 0 */
+  const int32_t *cu_q, *cu_k; /* [n_seqs + 1]: first query and first key row of each sequence; cu[0] = 0.  Rows of q
+                                 from cu_q[n_seqs] on are padding: out is 0 there, lse -infinity */
   int32_t n_seqs;
   int64_t n_q, n_k;           /* rows of q and of k and v */
-  int32_t max_q;              /* queries of the longest sequence: those beyond are not computed */
+  int32_t max_q;              /* queries of the longest sequence: those beyond are not computed, out is 0 there */
   int32_t q_heads, kv_heads;  /* q_heads a multiple of kv_heads */
   int32_t head_dim;           /* 64 or 128 */
   int32_t type;               /* HERSCHEL_BF16 or HERSCHEL_F16 */

@@ -94,7 +94,56 @@ __device__ __forceinline__ bool find_level(const herschel_prompt_args& a, int he
 __device__ __forceinline__ void report_lengths(const herschel_prompt_args& a) {
   for (int b = threadIdx.x; b < a.n_seqs; b += WAVE) {
     const int64_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1], k0 = a.cu_k[b], k1 = a.cu_k[b + 1];
-    if (q0 < 0 || q1 < q0 || q1 > a.n_q || q1 - q0 > a.max_q || k0 < 0 || k1 < k0 || k1 > a.n_k) flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+    if (q0 < 0 || (b == 0 && q0 > 0) || q1 < q0 || q1 > a.n_q || q1 - q0 > a.max_q || k0 < 0 || k1 < k0 || k1 > a.n_k) flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+  }
+}
+
+// Outputs [from, to) of heads h0 ... h0 + heads - 1 that no query computes: 0, log sums minus infinity.  The work of
+// workgroup `id` of `of`.
+template <int D>
+__device__ __forceinline__ void no_query(const herschel_prompt_args& a, int64_t from, int64_t to, int h0, int heads, int64_t id,
+                                         int64_t of) {
+  const int chunks = heads * (D / 4);  // of 8 bytes, in a row
+  for (int64_t x = id * blockDim.x + threadIdx.x; x < (to - from) * chunks; x += of * blockDim.x) {
+    const int64_t at = (from + x / chunks) * a.q_heads + h0;
+    ((u32x2*)((uint16_t*)a.out + at * D))[x % chunks] = u32x2{0, 0};
+    if (a.lse && x % chunks < heads) a.lse[at + x % chunks] = -INFINITY;
+  }
+}
+// The smallest and the largest start of a sequence, within the rows: what lies outside is no sequence's, and from the
+// first start to the largest every row is one's.
+__device__ __forceinline__ void start_range(const herschel_prompt_args& a, int64_t& lo, int64_t& hi) {
+  lo = a.n_q, hi = 0;
+  for (int b = threadIdx.x % WAVE; b <= a.n_seqs; b += WAVE) {
+    const int64_t x = min(max((int64_t)a.cu_q[b], (int64_t)0), a.n_q);
+    lo = min(lo, x), hi = max(hi, x);
+  }
+#pragma unroll
+  for (int o = 1; o < WAVE; o *= 2) {
+    lo = min(lo, (int64_t)__shfl_xor((int)lo, o));
+    hi = max(hi, (int64_t)__shfl_xor((int)hi, o));
+  }
+}
+// Rows without a query: beyond max_q of sequence b ([q0 + nq, q1)), before the first sequence and after the last;
+// q0w and q1w are the sequence's starts as given.
+template <int D>
+__device__ __forceinline__ void rows_without(const herschel_prompt_args& a, int b, int64_t q0w, int64_t q1w, int64_t q0, int64_t q1,
+                                             int nq, int h0, int heads, int id, int of) {
+  if (q1 - q0 > nq) no_query<D>(a, q0 + nq, q1, h0, heads, id, of);
+  const bool before = b == 0 && q0w > 0, after = b == a.n_seqs - 1 && q1w < a.n_q;
+  if (before || after) {
+    int64_t lo, hi;
+    start_range(a, lo, hi);
+    if (before) no_query<D>(a, 0, lo, h0, heads, id, of);
+    for (int64_t row = lo + id; before && row < q0; row += of) {  // starts fall below the first: is the row one's?
+      uint64_t named = 0;
+      for (int s0 = 0; s0 < a.n_seqs && !named; s0 += WAVE) {
+        const int s = s0 + threadIdx.x % WAVE;
+        named = __ballot(s < a.n_seqs && a.cu_q[min(s, a.n_seqs - 1)] <= row && row < a.cu_q[min(s, a.n_seqs - 1) + 1]);
+      }
+      if (!named) no_query<D>(a, row, row + 1, h0, heads, 0, 1);
+    }
+    if (after) no_query<D>(a, hi, a.n_q, h0, heads, id, of);
   }
 }
 
@@ -253,8 +302,10 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
   const int64_t q0 = min(max(q0w, (int64_t)0), a.n_q), q1 = min(max(q1w, q0), a.n_q);
   const int64_t kk0 = min(max(k0w, (int64_t)0), a.n_k), kk1 = min(max(k1w, kk0), a.n_k);
   const int nq = (int)min(q1 - q0, (int64_t)a.max_q), nk = (int)(kk1 - kk0);
-  if (level == 0 && qh == 0 && tid == 0 && (q0 != q0w || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
+  if (level == 0 && qh == 0 && tid == 0 &&
+      (q0 != q0w || (b == 0 && q0 > 0) || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
     flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+  if (!SPLIT || blockIdx.y == 0) rows_without<D>(a, b, q0w, q1w, q0, q1, nq, qh, 1, level, p.levels);
   const int row0 = level * QROWS;
   if (row0 >= nq) return;
   const int kh = qh / p.group;
@@ -573,6 +624,13 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   int64_t q0, q1;
   if (p.packed) {
     if (blockIdx.x == 0 && tid < WAVE) report_lengths(a);
+    if (a.cu_q[0] > 0 || a.cu_q[a.n_seqs] < a.n_q) {  // before the first sequence, after the last
+      const int64_t first = min((int64_t)max(a.cu_q[0], 0), a.n_q);
+      int64_t lo, hi;
+      start_range(a, lo, hi);
+      no_query<D>(a, 0, first, kh * p.group, p.group, id, gridDim.x / a.kv_heads);
+      no_query<D>(a, max(first, hi), a.n_q, kh * p.group, p.group, id, gridDim.x / a.kv_heads);
+    }
     if (!find_level(a, p.group, id, b, level, q0, q1)) return;
   }
   // lengths taken as the nearest valid
@@ -580,9 +638,15 @@ __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p
   if (!p.packed) q0 = min(max(q0w, (int64_t)0), a.n_q), q1 = min(max(q1w, q0), a.n_q);
   const int64_t kk0 = min(max(k0w, (int64_t)0), a.n_k), kk1 = min(max(k1w, kk0), a.n_k);
   const int nq = (int)min(q1 - q0, (int64_t)a.max_q), nk = (int)(kk1 - kk0);
-  if (level == 0 && kh == 0 && tid == 0 && (q0 != q0w || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
-    flag(a.status, HERSCHEL_OP_BAD_LENGTH);
   const int row0 = level * 32, rows = nq * p.group;
+  if (p.packed) {
+    if (q1 - q0 > nq) no_query<D>(a, q0 + nq, q1, kh * p.group, p.group, level, (rows + 31) / 32);
+  } else {
+    if (level == 0 && kh == 0 && tid == 0 &&
+        (q0 != q0w || (b == 0 && q0 > 0) || q1 != q1w || kk0 != k0w || kk1 != k1w || q1 - q0 != nq))
+      flag(a.status, HERSCHEL_OP_BAD_LENGTH);
+    if (!SPLIT || blockIdx.y == 0) rows_without<D>(a, b, q0w, q1w, q0, q1, nq, kh * p.group, p.group, level, p.levels);
+  }
   if (row0 >= rows) return;
   const int shift = nk - (int)(q1 - q0);  // causal: token i sees keys up to i + shift
 
@@ -871,8 +935,8 @@ constexpr int PACKED_SEQS = 128;
 
 template <int TYPE, int D>
 static int prompt_few(PromptArgs& p, bool vec) {
-  const int64_t levels = ((int64_t)p.a.max_q * p.group + 31) / 32, most = p.a.n_q * p.group / 32 + p.a.n_seqs;
-  p.packed = p.a.n_seqs > 1 && p.a.n_seqs <= PACKED_SEQS && p.splits == 1 && 4 * most <= levels * p.a.n_seqs;
+  const int64_t levels = std::max<int64_t>(1, ((int64_t)p.a.max_q * p.group + 31) / 32), most = p.a.n_q * p.group / 32 + p.a.n_seqs;
+  p.packed = p.a.max_q > 0 && p.a.n_seqs > 1 && p.a.n_seqs <= PACKED_SEQS && p.splits == 1 && 4 * most <= levels * p.a.n_seqs;
   const int64_t blocks = (p.packed ? most : levels * p.a.n_seqs) * p.a.kv_heads;
   if (blocks > 0x7fffffff) return HERSCHEL_EINVAL;
   p.levels = (int)levels;
@@ -884,7 +948,7 @@ static int prompt_few(PromptArgs& p, bool vec) {
 
 template <int TYPE, int D, int WAVES>
 static int prompt_launch(PromptArgs& p, bool vec) {
-  p.levels = (p.a.max_q + 32 * WAVES - 1) / (32 * WAVES);
+  p.levels = std::max(1, (p.a.max_q + 32 * WAVES - 1) / (32 * WAVES));
   // XCDs that share a key head: only where key heads and XCDs divide evenly
   const int G = p.a.kv_heads;
   p.spread = G >= 8 ? (G % 8 == 0 ? 1 : 0) : (8 % G == 0 ? 8 / G : 0);
@@ -998,9 +1062,9 @@ extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
   if ((a.n_q && (!a.q || !a.out || !aligned(a.q, 2) || !aligned(a.out, 8))) ||
       (a.n_k && (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2))))
     return HERSCHEL_EINVAL;
-  if (a.n_q == 0 || a.max_q == 0) return HERSCHEL_OK;
+  if (a.n_q == 0) return HERSCHEL_OK;
   PromptPlan plan = prompt_plan(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim);
-  if (!a.workspace || a.workspace_bytes < plan.bytes) plan.splits = 1;
+  if (!a.workspace || a.workspace_bytes < plan.bytes || a.max_q == 0) plan.splits = 1;
   PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0, plan.splits, 0};
   // 16-byte loads, and a tile's rows within 31 bits of bytes
   const bool vec = a.k_strides.row < (1 << 23) && a.v_strides.row < (1 << 23) && chunks_aligned(a.q, a.q_strides) && chunks_aligned(a.k, a.k_strides) && chunks_aligned(a.v, a.v_strides);

@@ -377,6 +377,8 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
 
     Query i of nq sees key j of nk iff, causal, j <= i + nk - nq and, with a window, j > i + nk - nq - window.
     ``max_q`` is the longest sequence's number of queries, ``scale`` the scores' (dim ** -0.5 if not given).
+    Rows of q from cu_q[-1] on are padding: their outputs are 0.  So are those of queries beyond ``max_q``, which
+    ``status`` reports, like every other fault of the lengths; without it nothing tells of them.
     Returns the outputs, with ``return_lse`` also the log of each row's sum of exponentials [queries, heads]."""
     sq, sk, sv = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
     _like(k, q, "k")

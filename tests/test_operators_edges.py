@@ -228,3 +228,61 @@ def test_largest_values(D):
         c.k.zero_()
         c.v.fill_(3e38)
     run_decode([3000, 33], 4, 2, D, BF, BF, 16, edit=fill)
+
+
+# ------------------------------------------------------------ rows without a query
+NO_QUERY_CASES = [  # queries, rows before, rows after, heads, kv heads, D, keys beyond the queries
+    ([5, 40, 1], 0, 17, 4, 2, 64, 0),                        # few rows
+    ([1, 300] + [1, 2] * 15, 0, 9, 8, 2, 64, 0),             # packed
+    ([1, 300] + [1, 2] * 15, 3, 0, 4, 4, 128, 0),
+    ([0, 0], 0, 33, 4, 2, 128, 0),                           # padding alone
+    ([30], 0, 3, 8, 2, 128, 4000),                           # parts of few rows
+    ([700, 300], 0, 200, 20, 4, 128, 0),                     # workgroups of 128 rows
+    ([900, 0, 500], 4, 200, 16, 16, 64, 0),
+    ([1400], 0, 10, 8, 2, 128, 4000),                        # and in parts
+    ([1030, 1026], 0, 300, 64, 16, 128, 0),                  # of 256 rows
+]
+
+
+@gpu
+@pytest.mark.parametrize("case", NO_QUERY_CASES, ids=lambda c: f"{len(c[0])}-{sum(c[0])}-{c[1]}-{c[2]}-{c[5]}")
+def test_prompt_rows_without_a_query(case):
+    """Rows before the first sequence, after the last and beyond max_q are 0 with a log sum of minus infinity; the others
+    are as without them."""
+    nq, before, after, hq, hk, D, more = case
+    n, nk = sum(nq), [x + more for x in nq]
+    q, k, v = rand(n, hq, D, seed=1), rand(sum(nk), hk, D, seed=2), rand(sum(nk), hk, D, seed=3)
+    padded = torch.cat([rand(before, hq, D, seed=4), q, rand(after, hq, D, seed=5)]).to(DEV)
+    k, v, q = k.to(DEV), v.to(DEV), q.to(DEV)
+    cu_q, cu_k = (torch.tensor([0] + x).cumsum(0).int().to(DEV) for x in (nq, nk))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for most in (max(nq), max(nq) // 2):
+        out = torch.full_like(padded, math.nan)
+        status.zero_()
+        got, lse = O.attn_prompt(padded, k, v, cu_q + before, cu_k, max_q=most, return_lse=True, out=out, status=status)
+        assert got is out and status.item() == (O.BAD_LENGTH if before or most < max(nq) else 0)
+        want, want_lse = O.attn_prompt(q, k, v, cu_q, cu_k, max_q=max(nq), return_lse=True)
+        named = torch.zeros(before + n + after, dtype=torch.bool, device=DEV)
+        named[before:before + n] = torch.cat([torch.arange(x, device=DEV) < most for x in nq])
+        assert (out[~named] == 0).all() and (lse[~named] == -math.inf).all()
+        rows = named[before:before + n]
+        # another grid may add parts in another order
+        assert torch.allclose(out[named].float(), want[rows].float(), rtol=2 ** -7, atol=2 ** -9)
+        assert torch.allclose(lse[named], want_lse[rows], rtol=1e-5, atol=1e-5)
+
+
+@gpu
+def test_prompt_starts_that_fall_leave_no_row_unwritten():
+    q = rand(300, 4, 64).to(DEV)
+    k = rand(300, 2, 64, seed=1).to(DEV)
+    for heads in (4, 1):
+        for cu in ([5, 0, 10, 200], [0, 200, 50, 60], [40, 90, 20, 20], [-3, 10, 5, 290], [300, 300, 300, 300], [7, 7, 7, 7]):
+            cu = torch.tensor(cu, dtype=torch.int32, device=DEV)
+            for n in (1, 40):  # with empty ones that make the call a packed one
+                starts = torch.cat([cu, cu[-1:].repeat(n)])
+                status = torch.zeros(1, dtype=torch.int32, device=DEV)
+                x = q[:, :heads]
+                out = torch.full(x.shape, math.nan, dtype=BF, device=DEV)
+                kv = k if heads == 4 else k[:, :1]
+                O.attn_prompt(x, kv, kv, starts, starts.clamp(0, 300), max_q=300, out=out, status=status)
+                assert status.item() == O.BAD_LENGTH and torch.isfinite(out).all(), (heads, cu.tolist(), n)
