@@ -86,7 +86,7 @@ typedef struct {
   int64_t n_positions;
   const int64_t *slots;      /* [n_tokens]: page * page_size + row in the page, negative for a token that is not
                                 cached; with a cache only.  No two tokens share a slot. */
-  int64_t n_tokens;          /* >= 0 */
+  int64_t n_tokens;          /* >= 0; 0: nothing is done, and the rows', positions' and slots' addresses may be NULL */
   int32_t q_heads, kv_heads, head_dim; /* kv_heads and head_dim equal the cache's */
   int32_t rotary_dim;        /* even, 0 <= rotary_dim <= head_dim: the rest of a head passes unchanged */
   int32_t layout;            /* HERSCHEL_ROPE_* */

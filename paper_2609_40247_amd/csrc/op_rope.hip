@@ -294,17 +294,17 @@ extern "C" int herschel_rope_write(const herschel_rope_args* args, const hersche
   if (a.n_tokens < 0 || a.head_dim < 2 || a.head_dim > 256 || (a.head_dim & 1) || !type_ok(a.type)) return HERSCHEL_EINVAL;
   if (a.rotary_dim < 0 || a.rotary_dim > a.head_dim || (a.rotary_dim & 1)) return HERSCHEL_EINVAL;
   if (a.layout != HERSCHEL_ROPE_HALF && a.layout != HERSCHEL_ROPE_INTERLEAVED) return HERSCHEL_EINVAL;
-  if ((!a.q && !a.k) || (a.q && a.q_heads < 1) || (a.k && a.kv_heads < 1)) return HERSCHEL_EINVAL;
-  if ((a.q_out && !a.q) || (a.k_out && !a.k) || (cache && (!a.k || !a.v || !a.slots))) return HERSCHEL_EINVAL;
-  if ((a.q && a.q_heads > (1 << 16)) || (a.k && a.kv_heads > (1 << 16))) return HERSCHEL_EINVAL;
-  if (!a.positions || a.n_positions < 1 || (a.rotary_dim && (!a.table || !aligned(a.table, 8)))) return HERSCHEL_EINVAL;
   if (!strides_ok(a.q_strides) || !strides_ok(a.k_strides) || !strides_ok(a.v_strides) ||
       !strides_ok(a.q_out_strides) || !strides_ok(a.k_out_strides))
     return HERSCHEL_EINVAL;
   if (cache && (!cache_ok(cache) || cache->head_dim != a.head_dim || cache->n_heads != a.kv_heads ||
                 (!quantised(cache->kind) && cache->kind != a.type)))
     return HERSCHEL_EINVAL;
-  if (a.n_tokens == 0) return HERSCHEL_OK;
+  if (a.n_tokens == 0) return HERSCHEL_OK;  // nothing to point at
+  if ((!a.q && !a.k) || (a.q && a.q_heads < 1) || (a.k && a.kv_heads < 1)) return HERSCHEL_EINVAL;
+  if ((a.q_out && !a.q) || (a.k_out && !a.k) || (cache && (!a.k || !a.v || !a.slots))) return HERSCHEL_EINVAL;
+  if ((a.q && a.q_heads > (1 << 16)) || (a.k && a.kv_heads > (1 << 16))) return HERSCHEL_EINVAL;
+  if (!a.positions || a.n_positions < 1 || (a.rotary_dim && (!a.table || !aligned(a.table, 8)))) return HERSCHEL_EINVAL;
   RopeArgs p{};
   p.a = a;
   if (cache) {

@@ -11,13 +11,16 @@ place.
 """
 from __future__ import annotations
 
+import ctypes
 import math
 
 import pytest
 import torch
 
+from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
-from test_operators import BF, DEV, HF, U, dense, exact_attention, gpu, make_cache, paged, rand, run_decode, run_prompt
+from test_operators import (BF, DEV, F8, HF, U, dense, exact_attention, fake_cache, gpu, lib, make_cache, paged, rand, rope_args,
+                            run_decode, run_prompt)
 
 
 # ------------------------------------------------------------ weights far below a row's largest
@@ -286,3 +289,29 @@ def test_prompt_starts_that_fall_leave_no_row_unwritten():
                 kv = k if heads == 4 else k[:, :1]
                 O.attn_prompt(x, kv, kv, starts, starts.clamp(0, 300), max_q=300, out=out, status=status)
                 assert status.item() == O.BAD_LENGTH and torch.isfinite(out).all(), (heads, cu.tolist(), n)
+
+
+# ------------------------------------------------------------ empty calls
+def test_rotary_write_of_no_tokens_needs_no_addresses():
+    """Empty tensors have the address 0."""
+    none = dict(q=None, k=None, v=None, q_out=None, positions=None, slots=None, n_tokens=0)
+    L = lib()
+    assert L.herschel_rope_write(ctypes.byref(rope_args(**none)), ctypes.byref(fake_cache())) == H.OK
+    assert L.herschel_rope_write(ctypes.byref(rope_args(**none)), None) == H.OK
+    for bad in (dict(head_dim=63), dict(rotary_dim=66), dict(layout=2), dict(type=O.FP8), dict(q_strides=O._Strides(-1, 64))):
+        assert L.herschel_rope_write(ctypes.byref(rope_args(**{**none, **bad})), None) == H.EINVAL
+    assert L.herschel_rope_write(ctypes.byref(rope_args(**none)), ctypes.byref(fake_cache(n_pages=0))) == H.EINVAL
+
+
+@gpu
+@pytest.mark.parametrize("kind", [None, BF, F8], ids=str)
+def test_rotary_write_of_no_tokens(kind):
+    x = torch.empty(0, 8, 64, dtype=BF, device=DEV)
+    none = torch.empty(0, dtype=torch.int64, device=DEV)
+    table = O.rotary_table(10, 64, device=DEV)
+    cache = make_cache(kind, 2, 2, 16, 64, fill=0x11) if kind else None
+    q, k = O.rope_write(x[:, :4], x[:, 4:6], x[:, 6:], none, table, cache, none if kind else None, keep_keys=True)
+    assert q.shape == (0, 4, 64) and k.shape == (0, 2, 64)
+    if cache:
+        cache.check()
+        assert (cache.k.view(torch.uint8) == 0x11).all()
