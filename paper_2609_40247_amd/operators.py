@@ -447,7 +447,7 @@ class DecodeAttention:
         B = shape[0]
         _need(q.dtype == self.dtype, "q must have the type that DecodeAttention was made for")
         c._fits(q)
-        _need(1 <= B <= self.batch and shape == (B, self.new_tokens, self.heads, c.head_dim),
+        _need(B <= self.batch and shape == (B, self.new_tokens, self.heads, c.head_dim),
               "q must have the sizes that the workspace is for")
         table, lens = _table(block_table, B, dev), _ints(seq_lens, "seq_lens", torch.int32, (B,), dev)
         _need(0 <= window < 2 ** 31, "window must be 0 or a number of keys below 2^31")
@@ -457,6 +457,8 @@ class DecodeAttention:
         else:
             to = _ints(out, "out", q.dtype, shape, dev)
         lse = q.new_empty(shape[:3], dtype=torch.float32) if return_lse else None
+        if B == 0:  # a step in which no sequence takes part
+            return (out, lse) if return_lse else out
         stream = _stream(dev)
         ws = self._workspaces.get(stream)
         if ws is None:

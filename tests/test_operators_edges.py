@@ -315,3 +315,14 @@ def test_rotary_write_of_no_tokens(kind):
     if cache:
         cache.check()
         assert (cache.k.view(torch.uint8) == 0x11).all()
+
+
+@gpu
+def test_decode_of_no_sequences():
+    c = make_cache(BF, 2, 2, 16, 64)
+    dec = O.DecodeAttention(c, batch=3, heads=4, new_tokens=2)
+    none = torch.empty(0, 4, dtype=torch.int32, device=DEV)
+    out, lse = dec(torch.empty(0, 2, 4, 64, dtype=BF, device=DEV), none, none[:, 0].contiguous(), return_lse=True)
+    assert out.shape == (0, 2, 4, 64) and lse.shape == (0, 2, 4) and out.dtype == BF
+    with pytest.raises(ValueError):
+        dec(torch.empty(0, 2, 3, 64, dtype=BF, device=DEV), none, none[:, 0].contiguous())
