@@ -5,7 +5,8 @@ reference, the SOL that the same op reaches elsewhere.  This module provides
 that reference for the ops of a served model's attention layer: it runs them
 (``operators``) at given sizes, a prompt and then decode steps, records the
 calls as a trace of CPU ops, launches and kernels with their operation counts
-and logical bytes, and has the analyzer rate them (HERSCHEL_OUT_SOL).
+and logical bytes, and has the analyzer rate them (HERSCHEL_OUT_SOL).  An op's
+time is the analyzer's, from its first kernel's start to its last one's end.
 
     python -m paper_2609_40247_amd.reference --prompt 4096 --batch 32 --cache fp8
 
@@ -15,10 +16,15 @@ is the ``ref_sol_ppm`` of traces of the same ops at the same sizes.
 from __future__ import annotations
 
 import argparse
-import time
+import bisect
+import json
+import os
+import tempfile
+from decimal import Decimal
 
 import numpy as np
 import torch
+from torch.profiler import ProfilerActivity, profile, record_function
 
 from . import herschel as H
 from . import operators as O
@@ -92,43 +98,58 @@ def counts(layer: AttentionLayer, op: str, lengths: list) -> tuple:
 
 
 class Recorder:
-    """Records calls as a trace: a CPU op and a launch on the host's clock, a kernel between two events."""
-
-    def __init__(self):
-        self.rows, self.events, self.host0 = [], [], 0
+    """Records calls as a trace, from torch's profiler: each call a CPU op, its launches and its kernels with the times
+    that the device reports for them.  (Between events around a call there would be the host's time too.)"""
 
     def begin(self) -> None:
         torch.cuda.synchronize()
-        self.rows, self.events = [], []
-        self.base = torch.cuda.Event(enable_timing=True)
-        self.base.record()
-        torch.cuda.synchronize()
-        self.host0 = time.perf_counter_ns()
+        self.profile = profile(activities=[ProfilerActivity.CPU, ProfilerActivity.CUDA], acc_events=True)
+        self.profile.start()
 
     def __call__(self, name: str, call):
-        first, last = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-        t0 = time.perf_counter_ns()
-        first.record()
-        out = call()
-        last.record()
-        self.rows.append((name, t0, time.perf_counter_ns()))
-        self.events.append((first, last))
-        return out
+        with record_function(name):
+            return call()
 
     def columns(self, work: list) -> dict:
-        """The trace's columns; ``work``: (operations, bytes) of each call in order."""
+        """The trace's columns; ``work``: (operations, bytes) of each call in order.  ``kernels`` holds their names."""
         torch.cuda.synchronize()
-        c = {k: [] for k in ("ts", "te", "corr", "pid", "lane", "name", "kind", "flops", "bytes")}
+        self.profile.stop()
+        with tempfile.TemporaryDirectory() as folder:
+            path = os.path.join(folder, "trace.json")
+            self.profile.export_chrome_trace(path)
+            with open(path) as f:
+                events = [e for e in json.load(f, parse_float=Decimal)["traceEvents"] if e.get("ph") == "X"]
 
-        def row(kind, ts, te, corr, name, f=0, b=0):
-            for k, x in zip(c, (ts, max(ts, te), corr, 0, 0, name, kind, f, b)):
+        def span(e):  # microseconds with three decimals: ns
+            begin = int(Decimal(e["ts"]) * 1000)
+            return begin, begin + max(1, int(Decimal(e["dur"]) * 1000))
+        ops = sorted((e for e in events if e.get("cat") == "user_annotation" and e["name"] in OPS), key=span)
+        launches = {e["args"].get("correlation"): e for e in events if e.get("cat") == "cuda_runtime"}
+        kernels = sorted((e for e in events if e.get("cat") == "kernel"), key=span)
+        if len(ops) != len(work) or not kernels:
+            raise RuntimeError(f"the profiler recorded {len(ops)} of {len(work)} calls and {len(kernels)} kernels")
+        base = span(ops[0])[0]
+        c = {k: [] for k in ("ts", "te", "corr", "pid", "lane", "name", "kind", "flops", "bytes")}
+        self.kernels = []
+
+        def row(kind, e, corr, name, f=0, b=0):
+            begin, end = span(e)
+            for k, x in zip(c, (begin - base, end - base, corr, 0, 0, name, kind, f, b)):
                 c[k].append(x)
-        for i, ((name, t0, t1), (first, last), (f, b)) in enumerate(zip(self.rows, self.events, work)):
-            t0, t1 = t0 - self.host0, t1 - self.host0
-            row(H.CPU_OP, t0, t1, 0, OPS.index(name), f, b)
-            row(H.LAUNCH, t0 + (t1 - t0) // 2, t1, i, 0)
-            at = int(self.base.elapsed_time(first) * 1e6)
-            row(H.KERNEL, at, at + max(1, int(first.elapsed_time(last) * 1e6)), i, OPS.index(name))
+        for op, (f, b) in zip(ops, work):
+            row(H.CPU_OP, op, 0, OPS.index(op["name"]), f, b)
+        begins = [span(op)[0] for op in ops]
+        for i, kernel in enumerate(kernels):
+            launch = launches.get(kernel["args"].get("correlation"))
+            if launch is None:
+                continue
+            at = bisect.bisect_right(begins, span(launch)[0]) - 1
+            if at < 0 or span(launch)[1] > span(ops[at])[1]:
+                continue  # of no recorded call
+            if kernel["name"] not in self.kernels:
+                self.kernels.append(kernel["name"])
+            row(H.LAUNCH, launch, i, 0)
+            row(H.KERNEL, kernel, i, self.kernels.index(kernel["name"]))
         types = dict(ts=np.int64, te=np.int64, corr=np.int64, pid=np.int32, lane=np.int32, name=np.int32,
                      kind=np.uint8, flops=np.int64, bytes=np.int64)
         return {k: np.array(v, dtype=types[k]) for k, v in c.items()}
@@ -155,10 +176,11 @@ def reference_sol(heads: int = 32, kv_heads: int = 8, head_dim: int = 128, promp
     then.lengths.fill_(prompt)
     tokens = [qkv(batch) for _ in range(steps + 2)]
     rec, work = Recorder(), []
-    for _ in range(2):  # warm up
+    for warm in range(2):  # once without and once under the profiler, whose first records take longer
+        if warm:
+            rec.begin()
         first.prompt(rows, lengths)
         then.step(tokens.pop())
-    rec.begin()
     for _ in range(max(1, steps // 4)):
         first.prompt(rows, lengths, rec)
         work += [counts(first, op, lengths) for op in OPS[:2]]
@@ -169,7 +191,7 @@ def reference_sol(heads: int = 32, kv_heads: int = 8, head_dim: int = 128, promp
     first.cache.check()
     then.cache.check()
     params = dict(window_begin=int(columns["ts"].min()), window_end=int(columns["te"].max()) + 1, gap_threshold=0,
-                  n_procs=1, n_streams=1, n_threads=1, n_names=len(OPS), n_op_names=len(OPS),
+                  n_procs=1, n_streams=1, n_threads=1, n_names=max(1, len(rec.kernels)), n_op_names=len(OPS),
                   flags=H.OUT_CONTAIN | H.OUT_SOL, peak_flops=peak_flops, peak_bytes=peak_bytes)
     code, out = H.analyze(columns, params, variant=variant)
     if code != H.OK:

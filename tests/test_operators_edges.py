@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import time
 
 import pytest
 import torch
@@ -326,3 +327,37 @@ def test_decode_of_no_sequences():
     assert out.shape == (0, 2, 4, 64) and lse.shape == (0, 2, 4) and out.dtype == BF
     with pytest.raises(ValueError):
         dec(torch.empty(0, 2, 3, 64, dtype=BF, device=DEV), none, none[:, 0].contiguous())
+
+
+# ------------------------------------------------------------ the recorded trace
+@gpu
+def test_recorded_kernels_have_their_own_times():
+    """A call that keeps the host busy before and between its launches takes no longer on the device: a trace's kernels
+    are the kernels, each with its launch inside its op."""
+    from paper_2609_40247_amd import reference as R
+    layer = R.AttentionLayer(8, 2, 64, 3, 400, 32, "fp8")
+    qkv = rand(3, 12, 64).to(DEV)
+    layer.lengths.fill_(300)
+    layer.step(qkv)
+    rec = R.Recorder()
+    rec.begin()
+
+    def slow(name, call):
+        def late():
+            time.sleep(0.003)
+            return call()
+        return rec(name, late)
+    for _ in range(3):
+        layer.step(qkv, slow)
+    c = rec.columns([(1, 1)] * 6)
+    ops, kernels, launches = (c["kind"] == x for x in (R.H.CPU_OP, R.H.KERNEL, R.H.LAUNCH))
+    assert [R.OPS[i] for i in c["name"][ops]] == ["rope_write_step", "attn_decode"] * 3
+    assert kernels.sum() == launches.sum() == 9  # one of a write, two of an attention
+    names = [rec.kernels[i] for i in c["name"][kernels]]
+    assert ["k_rope" in n for n in names] == [True, False, False] * 3 and sum("k_decode_join" in n for n in names) == 3
+    spans = list(zip(c["ts"], c["te"]))
+    host, device = [s for s, x in zip(spans, ops) if x], [s for s, x in zip(spans, kernels) if x]
+    assert all(b - a > 3_000_000 for a, b in host) and all(0 < b - a < 1_000_000 for a, b in device)
+    for i, (a, b) in enumerate(s for s, x in zip(spans, launches) if x):
+        op = host[2 * (i // 3) + (i % 3 > 0)]
+        assert op[0] <= a and b <= op[1] and device[i][0] >= a
