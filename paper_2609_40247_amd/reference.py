@@ -39,11 +39,13 @@ class AttentionLayer:
     """Rotary positions, cache and attention of one layer, for ``batch`` sequences of up to ``room`` tokens.
 
     ``prompt`` takes the QKV product's rows of whole prompts, ``step`` those of one new token a sequence; both
-    return the attention's output rows.  Pages are given out in a fixed shuffled order."""
+    return the attention's output rows.  Pages are given out in a fixed shuffled order.  A prompt longer than ``room``
+    is refused; a step's token beyond it is not cached and its output no number, which ``cache.check`` reports."""
 
     def __init__(self, heads: int = 32, kv_heads: int = 8, head_dim: int = 128, batch: int = 1, room: int = 8192,
                  page_size: int = 64, cache="bf16", dtype=torch.bfloat16, stretch: float = 1.0, device="cuda", seed: int = 0):
         self.heads, self.kv_heads, self.head_dim, self.batch, self.page_size = heads, kv_heads, head_dim, batch, page_size
+        self.room = room
         pages = -(-room // page_size)
         self.cache = O.PagedCache.allocate(batch * pages, kv_heads, page_size, head_dim,
                                            CACHES[cache] if isinstance(cache, str) else cache, device)
@@ -58,11 +60,16 @@ class AttentionLayer:
         return qkv[:, :h], qkv[:, h:h + g], qkv[:, h + g:]
 
     def _slots(self, seq: torch.Tensor, pos: torch.Tensor) -> torch.Tensor:
-        return self.block_table[seq, pos // self.page_size].long() * self.page_size + pos % self.page_size
+        pages = self.block_table.shape[1]
+        slots = self.block_table[seq, (pos // self.page_size).clamp(0, pages - 1)].long() * self.page_size + pos % self.page_size
+        # beyond a sequence's pages: beyond the cache, which the write reports
+        return torch.where((pos >= 0) & (pos < pages * self.page_size), slots, self.block_table.numel() * self.page_size)
 
     def prompt(self, qkv: torch.Tensor, lengths: list, timed=lambda name, call: call()) -> torch.Tensor:
         """qkv [sum of lengths, heads + 2 kv heads, dim]: all sequences' prompts, one after the other."""
         dev = qkv.device
+        if len(lengths) != self.batch or sum(lengths) != qkv.shape[0] or not all(0 <= n <= self.room for n in lengths):
+            raise ValueError(f"lengths must be {self.batch} of at most {self.room} tokens, qkv's rows in all")
         n = torch.tensor(lengths, device=dev)
         seq = torch.repeat_interleave(torch.arange(self.batch, device=dev), n)
         cu = torch.cat([n.new_zeros(1), n.cumsum(0)])

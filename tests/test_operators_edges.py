@@ -361,3 +361,34 @@ def test_recorded_kernels_have_their_own_times():
     for i, (a, b) in enumerate(s for s, x in zip(spans, launches) if x):
         op = host[2 * (i // 3) + (i % 3 > 0)]
         assert op[0] <= a and b <= op[1] and device[i][0] >= a
+
+
+# ------------------------------------------------------------ a layer's room
+def test_layer_refuses_prompts_beyond_its_room():
+    """What would index the block table beyond its end, which on a GPU ends the process, is refused or kept inside."""
+    from paper_2609_40247_amd import reference as R
+    layer = R.AttentionLayer.__new__(R.AttentionLayer)
+    layer.batch, layer.room, layer.page_size = 2, 40, 16
+    layer.block_table = torch.tensor([[4, 1, 0], [2, 5, 3]], dtype=torch.int32)
+    x = torch.zeros(50, 6, 64)
+    for lengths in ([41, 9], [50], [25, 24], [25, 26], [51, -1], [10, 20, 20]):
+        with pytest.raises(ValueError, match="lengths"):
+            layer.prompt(x, lengths)
+    seq, pos = torch.tensor([0, 0, 1, 1, 0, 1]), torch.tensor([0, 47, 16, 48, 1 << 40, -1])
+    assert layer._slots(seq, pos).tolist() == [64, 15, 80, 96, 96, 96]  # 96: beyond the cache
+
+
+@gpu
+def test_layer_reports_steps_beyond_its_room():
+    from paper_2609_40247_amd import reference as R
+    layer = R.AttentionLayer(4, 2, 64, 2, 32, 16, "bf16")
+    x = rand(62, 8, 64).to(DEV)
+    layer.prompt(x, [31, 31])
+    layer.step(x[:2])
+    layer.cache.check()
+    before = layer.cache.k.clone(), layer.cache.v.clone()
+    for _ in range(20):  # across the last page's end
+        layer.step(x[:2])
+        with pytest.raises(ValueError, match="position"):
+            layer.cache.check()
+    assert torch.equal(layer.cache.k, before[0]) and torch.equal(layer.cache.v, before[1])
