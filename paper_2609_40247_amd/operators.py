@@ -170,6 +170,17 @@ _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None) or torch.cuda.is_current_stream_capturing
+
+
+def _captured(device: int) -> bool:
+    """Whether the device's current stream is being captured into a graph."""
+    if _device() == device:
+        return _capturing()
+    with torch.cuda.device(device):
+        return _capturing()
+
+
 def _status(status: torch.Tensor | None, device: int) -> int:
     if status is None:
         return 0
@@ -418,7 +429,8 @@ class DecodeAttention:
     """Causal attention of the last ``new_tokens`` tokens of up to ``batch`` sequences over a cache.
 
     Keeps the workspace, one for each stream it is called on; calls allocate nothing but an output that is
-    not given.  A graph captured from a call uses the workspace of the stream it was captured on."""
+    not given.  A call that is captured (``torch.cuda.graph``) takes a workspace from the graph's own memory:
+    graphs may be replayed beside each other and beside other calls."""
 
     def __init__(self, cache: PagedCache, *, batch: int, heads: int, new_tokens: int = 1, dtype=None, lib=None):
         dtype = dtype or (torch.bfloat16 if cache.quantised else cache.k.dtype)
@@ -461,8 +473,10 @@ class DecodeAttention:
             return (out, lse) if return_lse else out
         stream = _stream(dev)
         ws = self._workspaces.get(stream)
-        if ws is None:
-            ws = self._workspaces[stream] = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device)
+        if ws is None or (stream and _captured(dev)):  # the default stream, 0, is never captured
+            ws = torch.empty(self.workspace_bytes, dtype=torch.uint8, device=q.device)
+            if not (stream and _captured(dev)):
+                self._workspaces[stream] = ws
         args = _DECODE.pack(
             q.data_ptr(), sq[0], sq[1], sq[2], to,
             lse.data_ptr() if return_lse else 0, table, block_table.shape[1], lens, B, self.new_tokens, self.heads,

@@ -20,8 +20,8 @@ import torch
 
 from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
-from test_operators import (BF, DEV, F8, HF, U, dense, exact_attention, fake_cache, gpu, lib, make_cache, paged, rand, rope_args,
-                            run_decode, run_prompt)
+from test_operators import (BF, DEV, F8, HF, U, dense, exact_attention, fake_cache, fill_cache, gpu, lib, make_cache, paged,
+                            rand, rope_args, run_decode, run_prompt)
 
 
 # ------------------------------------------------------------ weights far below a row's largest
@@ -392,3 +392,71 @@ def test_layer_reports_steps_beyond_its_room():
         with pytest.raises(ValueError, match="position"):
             layer.cache.check()
     assert torch.equal(layer.cache.k, before[0]) and torch.equal(layer.cache.v, before[1])
+
+
+# ------------------------------------------------------------ graphs of one handle
+class Seen:
+    """The library, with the workspaces that decode calls were given."""
+
+    def __init__(self):
+        self.lib, self.workspaces = lib(), []
+        self.herschel_attn_decode_workspace = self.lib.herschel_attn_decode_workspace
+
+    def herschel_attn_decode(self, args, cache):
+        fields = [f for f, _ in O.HerschelDecodeArgs._fields_]
+        flat = O._DECODE.unpack(args)  # q_strides are two values
+        self.workspaces.append(flat[fields.index("workspace") + 1])
+        return self.lib.herschel_attn_decode(args, cache)
+
+
+@gpu
+def test_graphs_of_one_handle_have_workspaces_of_their_own():
+    seen = Seen()
+    c = make_cache(BF, 200, 2, 16, 64)
+    fill_cache(c, 1)
+    dec = O.DecodeAttention(c, batch=2, heads=8, lib=seen)
+    q = rand(2, 1, 8, 64, seed=2).to(DEV)
+    bt, lens = torch.arange(200, dtype=torch.int32, device=DEV).view(2, 100), torch.tensor([1500, 900], dtype=torch.int32, device=DEV)
+    want = dec(q, bt, lens)
+    torch.cuda.synchronize()
+    stream, graphs = torch.cuda.Stream(), []
+    for _ in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            graphs.append((graph, dec(q, bt, lens)))
+    with torch.cuda.stream(stream):
+        late = dec(q, bt, lens)  # on the stream that was captured
+    torch.cuda.synchronize()
+    assert len(seen.workspaces) == len(set(seen.workspaces)) == 4
+    for graph, out in graphs:
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(late, want)
+
+
+@gpu
+def test_graphs_of_one_handle_replayed_beside_each_other():
+    c = make_cache(F8, 400, 2, 16, 128)
+    fill_cache(c, 3)
+    dec = O.DecodeAttention(c, batch=2, heads=16)
+    bt = torch.arange(400, dtype=torch.int32, device=DEV).view(2, 200)
+    calls = [(rand(2, 1, 16, 128, seed=4 + i).to(DEV), torch.tensor(n, dtype=torch.int32, device=DEV))
+             for i, n in enumerate(([3100, 40], [900, 2000], [17, 3000]))]
+    want = [dec(q, bt, n) for q, n in calls]
+    torch.cuda.synchronize()
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    for q, n in calls[:2]:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(dec(q, bt, n))
+    for _ in range(20):
+        for out in outs:
+            out.zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        eager = dec(calls[2][0], bt, calls[2][1])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs + [eager], want))
+    c.check()
