@@ -190,10 +190,13 @@ def _status(status: torch.Tensor | None, device: int) -> int:
 
 
 def raise_faults(status: torch.Tensor) -> None:
-    """Waits for the device, clears ``status`` and raises what it reported."""
+    """Waits for the device, all its streams, takes what calls reported out of ``status`` and raises it.  What calls
+    report meanwhile, enqueued by another thread, stays for the next time."""
+    torch.cuda.synchronize(status.device)
     bits = int(status.item())
     if bits:
-        status.zero_()
+        # bits are only ever set, so an addition clears them; it is atomic, like the kernels' setting of others
+        status.view(1).index_add_(0, torch.zeros(1, dtype=torch.int32, device=status.device), torch.full_like(status.view(1), -bits))
         raise ValueError("; ".join(text for bit, text in _FAULTS.items() if bits & bit))
 
 
@@ -235,7 +238,7 @@ class PagedCache:
         return cls(k.view(dtype), v.view(dtype), *(torch.zeros(shape[:3], device=device) for _ in range(2)))
 
     def check(self) -> None:
-        """Waits for the device and raises what calls with this cache reported since the last check."""
+        """Waits for the device, all its streams, and raises what calls with this cache reported since the last check."""
         raise_faults(self.status)
 
     def _fits(self, t: torch.Tensor) -> None:

@@ -460,3 +460,37 @@ def test_graphs_of_one_handle_replayed_beside_each_other():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs + [eager], want))
     c.check()
+
+
+# ------------------------------------------------------------ reports
+@gpu
+def test_check_waits_for_every_stream():
+    c = make_cache(BF, 2, 2, 16, 64)
+    dec = O.DecodeAttention(c, batch=1, heads=2)
+    q = rand(1, 1, 2, 64).to(DEV)
+    bt, n = torch.full((1, 2), 9, dtype=torch.int32, device=DEV), torch.full((1,), 5, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        dec(q, bt, n)
+    with pytest.raises(ValueError, match="block table"):
+        c.check()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)  # tens of milliseconds
+        dec(q, bt, n)
+    with pytest.raises(ValueError, match="block table"):
+        c.check()
+    c.check()
+
+
+@gpu
+def test_reports_that_come_while_others_are_taken_stay():
+    class Late(torch.Tensor):
+        def item(self):
+            bits = super().item()
+            self.bitwise_or_(O.BAD_SLOT)  # as by a call that another thread enqueued
+            return bits
+    status = torch.full((1,), O.BAD_PAGE | O.BAD_LENGTH, dtype=torch.int32, device=DEV).as_subclass(Late)
+    with pytest.raises(ValueError, match="block table.*lengths"):
+        O.raise_faults(status)
+    assert torch.Tensor.item(status) == O.BAD_SLOT
+    O.raise_faults(torch.zeros((), dtype=torch.int32, device=DEV))
