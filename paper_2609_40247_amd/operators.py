@@ -13,7 +13,8 @@ structures and calls the HIP library:
 Every call is enqueued on torch's current stream and returns at once.  What
 only the device can see to be wrong (a page id, a length, a position, a slot)
 is reported by ``PagedCache.check`` or, without a cache, through ``status``.
-There is no CPU fallback: without the built library or a GPU the calls raise.
+There is no backward pass: rows that require gradients are refused in grad
+mode.  There is no CPU fallback: without the built library or a GPU the calls raise.
 """
 from __future__ import annotations
 
@@ -152,6 +153,12 @@ def _table(t: torch.Tensor, n_seqs: int, device: int) -> int:
     return t.data_ptr()
 
 
+def _no_gradients(name: str) -> None:
+    """For a call with tensors that require gradients: its results would be cut off from them without a word."""
+    if torch.is_grad_enabled():
+        raise ValueError(f"{name} has no backward pass: call it under torch.no_grad() or with detached tensors")
+
+
 def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> None:
     """Calls an entry point with the tensors' device current."""
     if _device() == device:
@@ -215,6 +222,7 @@ class PagedCache:
         _need(k.shape[2] in (16, 32, 64, 128, 256), "the page size must be 16, 32, 64, 128 or 256")
         _need(2 <= k.shape[3] <= 256 and k.shape[3] % 2 == 0, "the head dimension must be even, at most 256")
         _need(k.shape[0] >= 1 and k.shape[1] >= 1, "the cache must have a page and a head")
+        _need(not (k.requires_grad or v.requires_grad), "k and v must not require gradients")
         self.quantised = KINDS[k.dtype] in (FP8, INT8)
         for s, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
             _need((s is not None) == self.quantised, f"{name} goes with an 8-bit cache, and with no other")
@@ -301,6 +309,8 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
             _rows(t, name)
             _like(t, first, name)
             _need(False, f"{name} must have the tokens, heads and head size of the rows it goes with")
+        if t.requires_grad:
+            _no_gradients("rope_write")
         return t.data_ptr(), row, head, heads
 
     qa = rows(q, "q") if q is not None else _NO_ROWS
@@ -359,16 +369,20 @@ def cache_read(cache: PagedCache, block_table: torch.Tensor, cu: torch.Tensor, *
     shape = (total, cache.n_heads, cache.head_dim)
     if not (cache.quantised or dtype is cache.k.dtype):
         raise ValueError("a 16-bit cache has the type of the rows")
+    given = ()
     if k_out is None:
         k_out = cache.k.new_empty(shape, dtype=dtype)
         to_k = k_out.data_ptr()
     else:
-        to_k = _ints(k_out, "k_out", dtype, shape, dev)
+        to_k, given = _ints(k_out, "k_out", dtype, shape, dev), (k_out,)
     if v_out is None:
         v_out = torch.empty_like(k_out)
         to_v = v_out.data_ptr()
     else:
-        to_v = _ints(v_out, "v_out", dtype, shape, dev)
+        to_v, given = _ints(v_out, "v_out", dtype, shape, dev), given + (v_out,)
+    for t in given:
+        if t.requires_grad:
+            _no_gradients("cache_read")
     args = _READ.pack(table, block_table.shape[1], starts, n, total, to_k, to_v, TYPES[dtype], cache._status,
                       _stream(dev))
     _call((lib or _lib()).herschel_cache_read, dev, "cache_read", args, cache._at)
@@ -397,6 +411,8 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
     sq, sk, sv = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
     _like(k, q, "k")
     _like(v, q, "v")
+    if q.requires_grad or k.requires_grad or v.requires_grad or out is not None and out.requires_grad:
+        _no_gradients("attn_prompt")
     dev, (n_q, heads, D), (n_k, kv_heads, _) = q.get_device(), q.shape, k.shape
     starts = cu_q.shape
     if not ((D == 64 or D == 128) and k.shape == v.shape == (n_k, kv_heads, D) and kv_heads >= 1 and heads >= 1 and
@@ -460,6 +476,8 @@ class DecodeAttention:
         c = self.cache
         sq, shape, dev = _rows(q, "q", 4), q.shape, q.get_device()
         B = shape[0]
+        if q.requires_grad or out is not None and out.requires_grad:
+            _no_gradients("DecodeAttention")
         _need(q.dtype == self.dtype, "q must have the type that DecodeAttention was made for")
         c._fits(q)
         _need(B <= self.batch and shape == (B, self.new_tokens, self.heads, c.head_dim),

@@ -494,3 +494,31 @@ def test_reports_that_come_while_others_are_taken_stay():
         O.raise_faults(status)
     assert torch.Tensor.item(status) == O.BAD_SLOT
     O.raise_faults(torch.zeros((), dtype=torch.int32, device=DEV))
+
+
+# ------------------------------------------------------------ autograd
+@gpu
+def test_rows_that_require_gradients_are_refused():
+    x = rand(4, 2, 64).to(DEV)
+    g = x.clone().requires_grad_()
+    cu = torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    c = make_cache(BF, 2, 2, 16, 64)
+    pos, table = torch.arange(4, device=DEV), O.rotary_table(5, 64, device=DEV)
+    dec = O.DecodeAttention(c, batch=1, heads=2)
+    bt, n = torch.zeros(1, 2, dtype=torch.int32, device=DEV), torch.full((1,), 4, dtype=torch.int32, device=DEV)
+    calls = [lambda a, t=t: O.attn_prompt(*(a if i == t else x for i in range(3)), cu, max_q=4) for t in range(3)]
+    calls += [lambda a, t=t: O.rope_write(*(a if i == t else x for i in range(3)), pos, table, c, pos, keep_keys=True)
+              for t in range(3)]
+    calls += [lambda a: dec(a[None, :1], bt, n), lambda a: O.attn_prompt(x, x, x, cu, max_q=4, out=a),
+              lambda a: O.rope_write(x, None, None, pos, table, q_out=a), lambda a: dec(x[None, :1], bt, n, out=a[None, :1]),
+              lambda a: O.cache_read(c, bt, cu, total=4, v_out=a)]
+    for call in calls:
+        with pytest.raises(ValueError, match="backward"):
+            call(g)
+        with torch.no_grad():
+            got = call(g)
+        want = call(x.clone())
+        for a, b in zip(got if isinstance(got, tuple) else [got], want if isinstance(want, tuple) else [want]):
+            assert a is None and b is None or torch.equal(a, b)
+    with pytest.raises(ValueError, match="gradients"):
+        O.PagedCache(c.k.clone().requires_grad_(), c.v)
