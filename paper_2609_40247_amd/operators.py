@@ -159,6 +159,10 @@ def _no_gradients(name: str) -> None:
         raise ValueError(f"{name} has no backward pass: call it under torch.no_grad() or with detached tensors")
 
 
+# Tells autograd that tensors were written, so that a backward pass that needs their old values raises.
+_written = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
+
+
 def _call(fn, device: int, name: str, args: bytes, cache: int | None = None) -> None:
     """Calls an entry point with the tensors' device current."""
     if _device() == device:
@@ -233,6 +237,7 @@ class PagedCache:
         self.status = torch.zeros(1, dtype=torch.int32, device=k.device)
         self.struct = HerschelCache(k.data_ptr(), v.data_ptr(), None if k_scale is None else k_scale.data_ptr(),
                                     None if v_scale is None else v_scale.data_ptr(), *k.shape, KINDS[k.dtype])
+        self._tensors = tuple(t for t in (k, v, k_scale, v_scale) if t is not None)
         self._at, self._status, self._device = ctypes.addressof(self.struct), self.status.data_ptr(), k.get_device()
 
     @classmethod
@@ -330,9 +335,10 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
             raise ValueError("the cache has another number of heads or head size")
         cache._fits(k)
         slot = _ints(slots, "slots", torch.int64, (T,), dev)
+    given = ()
     if q_out is not None:
         _need(q is not None, "q_out needs q")
-        qo = rows(q_out, "q_out", qa[3])
+        qo, given = rows(q_out, "q_out", qa[3]), (q_out,)
     elif q is not None:
         q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
         qo = q_out.data_ptr(), qa[3] * D, D
@@ -340,7 +346,7 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
         qo = _NO_ROWS
     if k_out is not None:
         _need(k is not None, "k_out needs k")
-        ko = rows(k_out, "k_out", ka[3])
+        ko, given = rows(k_out, "k_out", ka[3]), given + (k_out,)
     elif k is not None and (keep_keys or cache is None):
         k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
         ko = k_out.data_ptr(), ka[3] * D, D
@@ -351,6 +357,10 @@ def rope_write(q: torch.Tensor | None, k: torch.Tensor | None, v: torch.Tensor |
                       ko[2], pos, table.data_ptr(), pairs[0], slot, T, qa[3], ka[3], D, 2 * pairs[1],
                       LAYOUTS[layout], TYPES[dtype], reported, _stream(dev))
     _call((lib or _lib()).herschel_rope_write, dev, "rope_write", args, 0 if cache is None else cache._at)
+    if cache is not None:
+        given += cache._tensors
+    if given:
+        _written(given)
     return q_out, k_out
 
 
@@ -386,6 +396,8 @@ def cache_read(cache: PagedCache, block_table: torch.Tensor, cu: torch.Tensor, *
     args = _READ.pack(table, block_table.shape[1], starts, n, total, to_k, to_v, TYPES[dtype], cache._status,
                       _stream(dev))
     _call((lib or _lib()).herschel_cache_read, dev, "cache_read", args, cache._at)
+    if given:
+        _written(given)
     return k_out, v_out
 
 
@@ -425,6 +437,7 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
         _need(False, "window must be 0 or a number of keys below 2^31")
     from_q = _ints(cu_q, "cu_q", torch.int32, starts, dev)
     from_k = from_q if cu_k is None else _ints(cu_k, "cu_k", torch.int32, starts, dev)
+    given = out
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         to = out.data_ptr()
@@ -441,6 +454,8 @@ def attn_prompt(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.T
         D ** -0.5 if scale is None else scale, workspace.data_ptr() if size else 0, size,
         0 if status is None else _status(status, dev), _stream(dev))
     _call(lib.herschel_attn_prompt, dev, "attn_prompt", args)
+    if given is not None:
+        _written((given,))
     return (out, lse) if return_lse else out
 
 
@@ -484,6 +499,7 @@ class DecodeAttention:
               "q must have the sizes that the workspace is for")
         table, lens = _table(block_table, B, dev), _ints(seq_lens, "seq_lens", torch.int32, (B,), dev)
         _need(0 <= window < 2 ** 31, "window must be 0 or a number of keys below 2^31")
+        given = out
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
             to = out.data_ptr()
@@ -504,4 +520,6 @@ class DecodeAttention:
             TYPES[q.dtype], window, c.head_dim ** -0.5 if scale is None else scale, ws.data_ptr(),
             self.workspace_bytes, c._status, stream)
         _call(self.lib.herschel_attn_decode, dev, "DecodeAttention", args, c._at)
+        if given is not None:
+            _written((given,))
         return (out, lse) if return_lse else out

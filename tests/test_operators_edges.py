@@ -522,3 +522,33 @@ def test_rows_that_require_gradients_are_refused():
             assert a is None and b is None or torch.equal(a, b)
     with pytest.raises(ValueError, match="gradients"):
         O.PagedCache(c.k.clone().requires_grad_(), c.v)
+
+
+@gpu
+def test_written_tensors_count_as_changed():
+    """A backward pass that needs what a call has overwritten raises, as after torch's own in-place operations."""
+    x = rand(4, 2, 64).to(DEV)
+    cu = torch.tensor([0, 4], dtype=torch.int32, device=DEV)
+    pos, table = torch.arange(4, device=DEV), O.rotary_table(5, 64, device=DEV)
+    bt, n = torch.zeros(1, 2, dtype=torch.int32, device=DEV), torch.full((1,), 4, dtype=torch.int32, device=DEV)
+    for kind in (BF, F8):
+        c = make_cache(kind, 2, 2, 16, 64)
+        dec, written = O.DecodeAttention(c, batch=1, heads=2, dtype=BF), [t for t in (c.k, c.v, c.k_scale, c.v_scale) if t is not None]
+        out = x.clone()
+        for call, changed in ((lambda: O.rope_write(x, x, x, pos, table, c, pos), written),
+                              (lambda: O.rope_write(x, x, None, pos, table, q_out=out), [out]),
+                              (lambda: O.rope_write(x, x, None, pos, table, k_out=out), [out]),
+                              (lambda: O.cache_read(c, bt, cu, total=4, dtype=BF, k_out=out), [out]),
+                              (lambda: O.cache_read(c, bt, cu, total=4, dtype=BF, v_out=out), [out]),
+                              (lambda: O.attn_prompt(x, x, x, cu, max_q=4, out=out), [out]),
+                              (lambda: dec(x[None, :1], bt, n, out=out[None, :1]), [out])):
+            before = {id(t): t._version for t in (*written, out, x)}
+            call()
+            for t in (*written, out, x):
+                assert (t._version > before[id(t)]) == any(t is s for s in changed)
+    w = torch.ones(2, 2, 16, 64, dtype=BF, device=DEV, requires_grad=True)
+    c = make_cache(BF, 2, 2, 16, 64)
+    loss = (w * c.k).sum()
+    O.rope_write(x, x, x, pos, table, c, pos)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
