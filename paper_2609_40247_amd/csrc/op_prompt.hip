@@ -481,10 +481,14 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  // Copies asked for before this are asked for before those after it: `meet` counts by their order, which nothing else
+  // in the source holds (they go to different buffers).
+  auto in_order = []() INLINE { asm volatile("" ::: "memory"); };
   if (tiles > 0) {
     if constexpr (WAVES == 4) {
       load_k(0, s_k);
       load_v(0, s_v);
+      in_order();
       if (tiles > 1) load_k(1, s_k + KBYTES);
       meet(tiles > 1 ? KL : 0);
       bool first = true;
@@ -493,6 +497,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
       auto work = [&](int t, const char* __restrict kc, const char* __restrict vc, char* __restrict kn,
                       char* __restrict vn) INLINE {
         if (t + 1 < tiles) load_v(t + 1, vn);
+        in_order();  // the newest KL copies are K's: those that may be under way when the waves meet
         if (t + 2 < tiles) load_k(t + 2, kn);
         if (!hidden(t)) {
           scores(kc);
