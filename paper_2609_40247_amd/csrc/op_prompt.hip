@@ -1051,14 +1051,14 @@ extern "C" int herschel_attn_prompt_workspace(int32_t n_seqs, int64_t n_q, int64
                                               int32_t kv_heads, int32_t head_dim, size_t* bytes) {
   using namespace hop;
   if (!bytes || !prompt_sizes_ok(n_seqs, n_q, n_k, max_q, q_heads, kv_heads, head_dim)) return HERSCHEL_EINVAL;
-  *bytes = prompt_plan(n_seqs, n_q, n_k, max_q, q_heads, kv_heads, head_dim).bytes;
+  *bytes = prompt_plan(n_seqs, n_q, n_k, std::min<int64_t>(max_q, n_q), q_heads, kv_heads, head_dim).bytes;
   return HERSCHEL_OK;
 }
 
 extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
   using namespace hop;
   if (!args) return HERSCHEL_EINVAL;
-  const herschel_prompt_args& a = *args;
+  herschel_prompt_args a = *args;
   if (!prompt_sizes_ok(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim) || !type_ok(a.type))
     return HERSCHEL_EINVAL;
   if (a.workspace && !aligned(a.workspace, 16)) return HERSCHEL_EWORKSPACE;
@@ -1068,6 +1068,7 @@ extern "C" int herschel_attn_prompt(const herschel_prompt_args* args) {
       (a.n_k && (!a.k || !a.v || !aligned(a.k, 2) || !aligned(a.v, 2))))
     return HERSCHEL_EINVAL;
   if (a.n_q == 0) return HERSCHEL_OK;
+  a.max_q = (int32_t)std::min<int64_t>(a.max_q, a.n_q);  // no sequence has more: grids and their arithmetic go by it
   PromptPlan plan = prompt_plan(a.n_seqs, a.n_q, a.n_k, a.max_q, a.q_heads, a.kv_heads, a.head_dim);
   if (!a.workspace || a.workspace_bytes < plan.bytes || a.max_q == 0) plan.splits = 1;
   PromptArgs p{a, a.q_heads / a.kv_heads, 0, 0, plan.splits, 0};

@@ -20,6 +20,7 @@ import torch
 
 from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
+from test_host_calls import child, fake, launches  # noqa: F401 (a fixture)
 from test_operators import (BF, DEV, F8, HF, U, dense, exact_attention, fake_cache, fill_cache, gpu, lib, make_cache, paged,
                             rand, rope_args, run_decode, run_prompt)
 
@@ -552,3 +553,32 @@ def test_written_tensors_count_as_changed():
     O.rope_write(x, x, x, pos, table, c, pos)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+# ------------------------------------------------------------ grids
+def test_longest_sequence_beyond_the_rows(fake):
+    """max_q may be any bound: grids are those of at most all rows, also where the bound is the type's largest."""
+    res = child(fake, """
+        import struct
+        PROMPT = struct.Struct("@3P6q4Pi2q7ifPN2P")
+
+        def prompt(n_q, n_k, max_q, heads, kv_heads, dim, n_seqs=1, workspace=0):
+            device()
+            a = 1 << 44
+            args = PROMPT.pack(a, a, a, heads * dim, dim, kv_heads * dim, dim, kv_heads * dim, dim, a, 0, a, a, n_seqs, n_q, n_k,
+                               max_q, heads, kv_heads, dim, 0, 1, 0, 1.0, workspace, 1 << 40, 0, 0)
+            lib.herschel_attn_prompt.argtypes = [ctypes.c_void_p]
+            return lib.herschel_attn_prompt(args), log()
+        for sizes in ((50, 50, 8, 2, 64), (4096, 4096, 32, 8, 128), (3000, 3000, 16, 16, 64), (700, 9000, 8, 2, 128),
+                      (2000, 9000, 16, 2, 128)):
+            n_q, n_k, heads, kv_heads, dim = sizes
+            for most in (n_q, n_q + 1, 2**31 - 1, 2**31 - 100):
+                for w in (0, 1 << 44):
+                    out.append((n_q, most, prompt(n_q, n_k, most, heads, kv_heads, dim, workspace=w)))
+    """)
+    for i in range(0, len(res), 8):
+        for w in (0, 1):
+            want = res[i + w][2]
+            assert want[0] == H.OK and launches(want[1])
+            for n_q, most, got in res[i + w:i + 8:2]:
+                assert got == want, (n_q, most, got, want)
