@@ -21,7 +21,7 @@ import torch
 from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
 from test_host_calls import child, fake, launches  # noqa: F401 (a fixture)
-from test_operators import (BF, DEV, F8, HF, U, dense, exact_attention, fake_cache, fill_cache, gpu, lib, make_cache, paged,
+from test_operators import (BF, DEV, F8, HF, I8, U, dense, exact_attention, fake_cache, fill_cache, gpu, lib, make_cache, paged,
                             rand, rope_args, run_decode, run_prompt)
 
 
@@ -582,3 +582,34 @@ def test_longest_sequence_beyond_the_rows(fake):
             assert want[0] == H.OK and launches(want[1])
             for n_q, most, got in res[i + w:i + 8:2]:
                 assert got == want, (n_q, most, got, want)
+
+
+# ------------------------------------------------------------ small values
+@gpu
+@pytest.mark.parametrize("power", [-60, -80, -88])
+def test_small_values_scale(power):
+    """Values times a power of two give outputs times it, down to near bf16's smallest: exponentials that leave room for
+    sums of the largest values leave it below too.  The values are from 2^-10 on: with 2^-88, and 2^-30 for the largest
+    weight, what a weight of 2^-8 of it adds is above 2^-140, a number with 9 places, and lesser ones make up less than
+    2^-8 of an output."""
+    by = 2.0 ** power
+    q, k, v = rand(40, 4, 64, seed=1).to(DEV), rand(700, 2, 64, seed=2).to(DEV), (rand(700, 2, 64, seed=3).abs() + 0.5).to(DEV)
+    for more in (0, 8000):
+        qq = torch.cat([q, q.new_zeros(more, 4, 64)])
+        starts = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([0, 40, 40 + more], [0, 700, 700]))
+        starts = tuple(starts)
+        a, b = (O.attn_prompt(qq, k, x, *starts, max_q=max(40, more))[:40].double() for x in (v, v * by))
+        assert ((b / by - a).abs() <= 2.0 ** -7 * a).all()
+    for kind in (BF, F8, I8):
+        c = make_cache(kind, 64, 2, 16, 64)
+        fill_cache(c, 1)
+        dec = O.DecodeAttention(c, batch=1, heads=4, dtype=BF)
+        bt, n = torch.arange(64, dtype=torch.int32, device=DEV)[None], torch.tensor([1000], dtype=torch.int32, device=DEV)
+        if kind == BF:
+            c.v.copy_(c.v.abs() + 0.5)
+        else:  # magnitudes
+            c.v.view(torch.uint8).bitwise_and_(0x7f)
+        a = dec(q[:1][None], bt, n).double()
+        (c.v if kind == BF else c.v_scale).mul_(by)
+        b = dec(q[:1][None], bt, n).double()
+        assert ((b / by - a).abs() <= 2.0 ** -7 * a).all(), kind
