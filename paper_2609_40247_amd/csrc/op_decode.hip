@@ -22,18 +22,18 @@
 //    inside a sequence's head the parts are joined by a second small kernel.
 //
 //  - A step's 16 KB (8 with codes) a wave are asked for at once; the waits are
-//    filled by the other waves of the SIMD.  (Loading the next step's rows before
-//    this one is worked on costs registers, and with them waves: 105 us became
-//    110 for 32 requests of 4096 tokens in bf16, 92 became 102 for 64 in fp8.  Its
-//    keys once the scores are there and its values after the second product spill
-//    with fp8, 79 became 136 us, and gain nothing with int8, 52 became 54.)
-//  - The second kernel costs 5 to 7 us.  Joining in the first, by the workgroup
-//    whose part is the last one there, costs more: parts written through the
+//    filled by the other waves of the SIMD.  (When tried, loading the next step's
+//    rows before this one was worked on cost registers, and with them waves: 105 us
+//    became 110 for 32 requests of 4096 tokens in bf16, 92 became 102 for 64 in fp8.
+//    Its keys once the scores are there and its values after the second product spilled
+//    with fp8, 79 became 136 us, and gained nothing with int8, 52 became 54.)
+//  - The second kernel costs 4 to 7 us.  Joining in the first, by the workgroup
+//    whose part is the last one there, cost more when tried: parts written through the
 //    caches to where all XCDs see them 14.0 us against 12.9 for one request of 4000
 //    tokens, 140 against 121 for three long contexts.
 //
-// 64 requests of 512 to 8704 tokens in fp8, 396 MB: 78 us, 5.1 TB/s, a copy's rate.
-// One of 4000 tokens in bf16, 16 MB: 12.8 us, two kernels' latency.  Four drafted
+// 64 requests of 512 to 8704 tokens in fp8, 396 MB: 79 us, 5.0 TB/s, a copy's rate.
+// One of 4000 tokens in bf16, 16 MB: 13.0 us, two kernels' latency.  Four drafted
 // tokens of three long contexts in int8, 473 MB: 107 us, 4.4 TB/s; with 20 rows of
 // 32 in use, codes that become halves and every product of the second kind done
 // twice, vector instructions take half of that.
@@ -55,11 +55,12 @@ namespace hop {
 
 constexpr int TILE = 128;         // keys of a workgroup's step: 32 a wave
 // Shares of the line: as many workgroups as the CUs hold, by registers.  Of heads
-// of 128 three a CU with codes and one row block (64 requests 92 us against 105
-// with two), else two (bf16 102 and 104 us; more with two blocks spill: 126 us
-// become 141).  A step of heads of 64 has half the bytes to wait for and fewer
-// registers: four (64 requests in fp8 56 us against 61 with three), with two row
-// blocks of codes three (three long contexts 86 against 92 with two).
+// of 128 three a CU with codes and one row block (64 requests in fp8 80 us against
+// 83 with two), else two (bf16 73 and 73 us; more with two blocks spill: 120 us
+// become 257).  A step of heads of 64 has half the bytes to wait for and fewer
+// registers: four (64 requests in int8 52 us against 54 with three, in fp8 53
+// against 52), with two row blocks of codes three (three long contexts 72 against
+// 79 with two and 109 with four).
 constexpr int MAX_SHARES = 1024;
 constexpr int shares_of_cu(int kind, int row_blocks, int dim) {
   return dim == 64 ? (row_blocks == 1 ? 4 : quantised(kind) ? 3 : 2) : quantised(kind) && row_blocks == 1 ? 3 : 2;

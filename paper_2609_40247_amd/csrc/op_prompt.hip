@@ -26,8 +26,8 @@
 //    wave whose sums are not finite at the end computes its rows again, with
 //    nothing but the keys that each row sees.
 //
-// 32 heads of 128, causal, bf16: 4096 rows 140 us, 980 TFLOP/s; three prompts of
-// 2001 to 8192 rows 692 us, 1036 TFLOP/s, where a matrix product of 8192 cubed
+// 32 heads of 128, causal, bf16: 4096 rows 141 us, 975 TFLOP/s; three prompts of
+// 2001 to 8192 rows 675 us, 1061 TFLOP/s, where a matrix product of 8192 cubed
 // reaches 1200.
 #include <algorithm>
 #include <type_traits>
@@ -593,22 +593,22 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void k_prompt(PromptArgs p) {
 //
 // Where workgroups of 128 rows would leave most of the card idle, what counts is
 // the chain of tiles that one wave goes through: here it is four times shorter
-// (with 32 heads of 128, 128 rows 6.7 us against 9.3, 512 rows 12.2 against 16.7,
-// 16 rows over 2048 keys 22.6 against 53.7).  The rows are a token's query heads
+// (with 32 heads of 128, 128 rows 6.8 us against 9.0, 512 rows 13.1 against 17.1,
+// 16 rows over 2048 keys 24 against 49).  The rows are a token's query heads
 // of one key head, then the next token's, so that a call with fewer than 32
 // tokens fills its workgroups too.  A key goes to one wave only, through LDS that
 // is the wave's own (loads in the products' layout touch a row per lane: 2048
-// keys take 25.8 us), so no wave waits for another before the parts are joined.
+// keys took 25.8 us where this took 22.6), so no wave waits for another before the parts are joined.
 // The next step's keys are asked for once the scores are there, its values after
 // the second product.
 //
 // Packed sequences of different lengths would leave most workgroups of a grid of
 // levels by sequences without rows, and one waits for the lengths to find that
 // out: here the grid has the levels that the rows allow and one a sequence (8
-// sequences of 1 to 600 tokens, 16 heads of 64: 23.5 to 10.2 us).  Workgroups of
-// 128 rows have fewer levels, and the search costs them as much (24 x 1 to 300
-// tokens 10.5 against 11.8 us).
-constexpr int FEW_WAVES = 4;  // eight: 2048 keys 20 us against 23, but 512 rows 16.7 against 12.2
+// sequences of 1 to 600 tokens, 16 heads of 64: 25.4 to 10.5 us).  Workgroups of
+// 128 rows have fewer levels, and the search cost them as much when tried (24 x 1
+// to 300 tokens 10.5 against 11.8 us).
+constexpr int FEW_WAVES = 4;  // eight: 16 rows over 2048 keys 17.9 us against 17.5, 512 rows 18.3 against 13.1
 template <int TYPE, int D, bool VEC, bool SPLIT>
 __global__ __launch_bounds__(FEW_WAVES * WAVE, 2) void k_prompt_few(PromptArgs p) {
   const herschel_prompt_args& a = p.a;
@@ -933,9 +933,9 @@ static int prompt_join(PromptArgs& p) {
 }
 
 // Packed: where a quarter of the grid is left, and the sequences are found in two rounds of
-// the scan (4 heads of 64: 32 x 1 to 300 tokens 12.7 to 7.6 us, 64 x 1 to 300 13.8
-// to 8.7; 3 x 100 to 900 of 16 heads, half the grid, would take 12.0 against 11.0, 200 x
-// 1 to 60 8.0 against 7.7, 400 x 1 to 20 9.6 against 7.4).
+// the scan (4 heads of 64: 32 x 1 to 300 tokens 12.5 to 7.6 us, 64 x 1 to 300 14.0
+// to 8.8; 3 x 100 to 900 of 16 heads, half the grid, would take 12.4 against 11.6, 200 x
+// 1 to 60 8.3 against 8.0, 400 x 1 to 20 9.9 against 7.2).
 constexpr int PACKED_SEQS = 128;
 
 template <int TYPE, int D>
@@ -971,36 +971,37 @@ static int prompt_launch(PromptArgs& p, bool vec) {
 }
 
 // What a call runs as, from its sizes and types alone (lengths are on the device:
-// sequences count as their mean).
+// sequences count as their mean).  Times are of calls in a graph, causal, key heads
+// a quarter of the heads; heads of 64 in half.
 //
 // Few rows: as long as 32 of them (of one key head) a workgroup make no more
 // workgroups than the card holds at once, about 20,000 rows in all (24 x 16 rows
-// of 16 heads of 64 4.7 us against 5.7, 24 x 64 6.2 against 6.6; 24 x 128 11.6
-// against 9.3, 1024 rows of 32 heads of 128 27.0 against 26.4).  Over many keys
-// workgroups of 128 rows read them fewer times, so rows times keys times dimensions
-// have a limit too (of 128, 4 x 64 rows of 32 heads over 4096 keys, 4.3e9, 44
-// against 49, 512 rows, 8.6e9, 57 against 51; 777 rows of 8 heads over 12000 83
-// against 64; of 64, 4096 rows of 4 heads, 4.3e9, 27 against 35).  Heads of 64 gain
-// up to 960 workgroups (16 heads: 24 x 1 to 300 tokens 9.0 us against 10.5, 100 to
-// 900 three times 11.0 against 21.0, 900 twice 16.3 against 21.2, one of 1800 20.3
-// against 36.5; 24 x 100, 1296 workgroups, 11.4 against 8.7).
+// of 16 heads of 64 5.2 us against 6.0, 512 rows of 32 heads of 128 13.1 against
+// 17.1; 1024 rows of 32 heads of 128 28.8 against 26.5).  Over many keys workgroups
+// of 128 rows read them fewer times, so rows times keys times dimensions have a
+// limit too (of 128, 4 x 64 rows of 32 heads over 4096 keys, 4.3e9, 46 against 50,
+// 512 rows, 8.6e9, 59 against 59; 777 rows of 8 heads over 12000 89 against 64; of
+// 64, 4096 rows of 4 heads, 4.3e9, 30 against 42).  Heads of 64 gain up to 960
+// workgroups (16 heads: 24 x 1 to 300 tokens 9.3 us against 11.2, 100 to 900 three
+// times 11.6 against 21.9, 900 twice 16.5 against 22.1, one of 1800 21.7 against
+// 38.8, though 24 x 64 7.0 against 6.4; 24 x 100, 1296 workgroups, 11.5 against 8.7).
 //
 // Else eight waves (256 rows) or four (128).  Eight in turns are faster where there
-// is enough for every CU twice over: 4096 rows of 32 heads of 128 145 us against
-// 156, 8192 983 against 1080; below, what counts is more and smaller workgroups:
-// 512 rows 23 against 18 us, 8 heads of 4096 95 against 83.  With heads of 64
-// the exponentials take longer than the products and turns lose (4096 rows
-// twice: 186 against 175 us).
+// is enough for every CU twice over: 4096 rows of 32 heads of 128 139 us against
+// 151, 8192 twice 985 against 1063; below, what counts is more and smaller
+// workgroups: 512 rows 21.5 against 17.1 us, 8 heads of 4096 95 against 81.  With
+// heads of 64 the exponentials take longer than the products and turns lost when
+// tried (4096 rows twice: 186 against 175 us).
 //
 // Parts: where the workgroups would not fill the card and keys are many, each
 // workgroup's keys go to several.  The second launch and the parts' way through
 // memory take 5 to 10 us.  Of few rows, four parts or more unless keys are very
-// many: 16 rows of 32 heads over 2048 keys 15.4 us against 22.5, over 8192 21.6
-// against 77; in two parts 2048 rows of 4 heads would take 27 against 23.  Of many,
+// many: 16 rows of 32 heads over 2048 keys 17.5 us against 23.9, over 8192 24
+// against 80; in two parts 2048 rows of 4 heads would take 30 against 24.  Of many,
 // from 4096 keys on, to fill the card's places for workgroups once, or twice in up
-// to four parts: 8192 rows of 4 heads 108 against 153, 4096 of 8 71 against 80, 512
-// of 32 over 8192 keys 82 against 153 (in eight parts 93); 2048 rows of 16 heads
-// would take 53 against 44.
+// to four parts: 8192 rows of 4 heads 121 against 157, 4096 of 8 81 against 82, 512
+// of 32 over 8192 keys 92 against 159 (in eight parts 103); 2048 rows of 16 heads
+// would take 62 against 45.
 struct PromptPlan {
   int waves;  // 0: few rows
   int splits;
