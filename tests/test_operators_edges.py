@@ -21,8 +21,8 @@ import torch
 from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
 from test_host_calls import child, fake, launches  # noqa: F401 (a fixture)
-from test_operators import (BF, DEV, F8, HF, I8, U, dense, exact_attention, fake_cache, fill_cache, gpu, lib, make_cache, paged,
-                            rand, rope_args, run_decode, run_prompt)
+from test_operators import (BF, DEV, F8, HF, I8, U, check_attention, dense, exact_attention, fake_cache, fill_cache, gpu, lib,
+                            make_cache, paged, rand, rope_args, run_decode, run_prompt)
 
 
 # ------------------------------------------------------------ weights far below a row's largest
@@ -613,3 +613,22 @@ def test_small_values_scale(power):
         (c.v if kind == BF else c.v_scale).mul_(by)
         b = dec(q[:1][None], bt, n).double()
         assert ((b / by - a).abs() <= 2.0 ** -7 * a).all(), kind
+
+
+# ------------------------------------------------------------ weights over 8-bit caches
+@gpu
+@pytest.mark.parametrize("kind", [F8, I8], ids=str)
+@pytest.mark.parametrize("lens,hq,hk,D,new", [([700, 3], 16, 1, 128, 1), ([4000], 8, 2, 64, 1), ([90, 200], 8, 2, 128, 4)], ids=str)
+def test_decode_weights_over_codes_keep_two_parts(lens, hq, hk, D, new, kind):
+    """Up to 16 rows of a key head, bf16 rows as well: a weight is rounded to 16 bits' worth of two parts, 2^-16, and
+    the output once."""
+    page = 16
+    c = make_cache(kind, sum(-(-n // page) for n in lens) + 1, hk, page, D)
+    fill_cache(c, 7)
+    bt = paged(c, lens, 8)
+    q = rand(len(lens), new, hq, D, seed=9)
+    dec = O.DecodeAttention(c, batch=len(lens), heads=hq, new_tokens=new, dtype=BF)
+    out, lse = dec(q.to(DEV), bt.to(DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), return_lse=True)
+    c.check()
+    for b, (k, v) in enumerate(dense(c, bt, lens)):
+        check_attention(out[b], lse[b], exact_attention(q[b], k, v, D ** -0.5, True, 0), BF, 2.0 ** -16, lens[b], D)
