@@ -26,9 +26,10 @@
  *
  * Numbers: inputs and outputs are bfloat16 or IEEE half; products are summed,
  * and maxima, sums and scales held, in 32 bits.  The attention operators round a
- * weight (over an 8-bit cache, the weight times its value's scale) to 16 bits
- * before it meets its value: to the rows' type, over an 8-bit cache to two
- * bfloat16 (one for bfloat16 rows of more than 16 to a key head).  A weight too small for 32 bits counts
+ * weight (over an 8-bit cache, the weight times its value's scale) before it
+ * meets its value: prompts to the rows' type; decode to two parts of 16 bits, or
+ * to one where more than 16 rows share a key head and are not half rows over an
+ * 8-bit cache.  A weight too small for 32 bits counts
  * as not 0 where its value is an infinity.
  */
 #ifndef HERSCHEL_OPS_H

@@ -151,13 +151,15 @@ template <int TYPE, int KIND, int D, int RB>
 __global__ __launch_bounds__(256, shares_of_cu(KIND, RB, D)) void k_decode(DecodeArgs p) {
   // With codes the second product runs in bf16, whose range holds exponential
   // times scale for any scale.  It runs twice, on the rounded value and on what the
-  // rounding left, so that the result keeps the rows' precision (64 requests of
-  // bf16 rows in fp8 0.0017 from 64 bits instead of 0.0023); with one row block that
-  // is hidden behind the reads (80.5 against 81.2 us).  With two it takes 8% (three
-  // long contexts in fp8 99 against 107 us): there bf16 rows, whose own rounding is as
-  // large, take the rounded value alone.
+  // rounding left, so that the result keeps the rows' precision: with one row block
+  // that is hidden behind the reads (64 requests of bf16 rows in fp8 80.5 against
+  // 81.2 us and 0.0017 from 64 bits instead of 0.0023, 32 in a bf16 cache 72.6
+  // against 73.2).  With two it takes 8% (three long contexts in fp8 99 against 107
+  // us): there rows of the cache's type and bf16 rows, whose own rounding is as large,
+  // take the rounded value alone; half rows over codes, whose rounding is finer than
+  // bf16's, do not.
   constexpr int PV = quantised(KIND) ? HERSCHEL_BF16 : TYPE;
-  constexpr bool SPLIT = quantised(KIND) && (TYPE == HERSCHEL_F16 || RB == 1);
+  constexpr bool SPLIT = RB == 1 || (quantised(KIND) && TYPE == HERSCHEL_F16);
   constexpr int NS = D / 32;       // steps of the first product
   constexpr int ND = D / 16;       // blocks of dimensions of the second; dimensions of a lane's chunk
   constexpr int CB = code_bytes(KIND);

@@ -632,3 +632,9 @@ def test_decode_weights_over_codes_keep_two_parts(lens, hq, hk, D, new, kind):
     c.check()
     for b, (k, v) in enumerate(dense(c, bt, lens)):
         check_attention(out[b], lse[b], exact_attention(q[b], k, v, D ** -0.5, True, 0), BF, 2.0 ** -16, lens[b], D)
+
+
+@gpu
+@pytest.mark.parametrize("lens,hq,hk,D,new", [([700, 3], 16, 1, 128, 1), ([4000], 8, 2, 64, 1), ([90, 200], 8, 2, 128, 4)], ids=str)
+def test_decode_weights_over_bf16_caches_keep_two_parts(lens, hq, hk, D, new):
+    test_decode_weights_over_codes_keep_two_parts(lens, hq, hk, D, new, BF)
