@@ -34,7 +34,7 @@
 //
 // 64 requests of 512 to 8704 tokens in fp8, 396 MB: 79 us, 5.0 TB/s, a copy's rate.
 // One of 4000 tokens in bf16, 16 MB: 13.0 us, two kernels' latency.  Four drafted
-// tokens of three long contexts in int8, 473 MB: 107 us, 4.4 TB/s; with 20 rows of
+// tokens of three long contexts in int8, 473 MB: 107 to 110 us, 4.4 TB/s; with 20 rows of
 // 32 in use, codes that become halves and every product of the second kind done
 // twice, vector instructions take half of that.
 //

@@ -26,9 +26,9 @@
 //    wave whose sums are not finite at the end computes its rows again, with
 //    nothing but the keys that each row sees.
 //
-// 32 heads of 128, causal, bf16: 4096 rows 141 us, 975 TFLOP/s; three prompts of
-// 2001 to 8192 rows 675 us, 1061 TFLOP/s, where a matrix product of 8192 cubed
-// reaches 1200.
+// 32 heads of 128, causal, bf16, by the card: 4096 rows 141 to 146 us, 940 to 976
+// TFLOP/s; three prompts of 2001 to 8192 rows 675 to 702 us, 1021 to 1061 TFLOP/s,
+// where a matrix product of 8192 cubed reaches 1173 to 1201.
 #include <algorithm>
 #include <type_traits>
 

@@ -1,6 +1,6 @@
 // The paged cache read back as dense rows: every code and scale read once,
 // every element written once, nothing computed but the scaling.  Bound by the
-// traffic: 717 MB of int8 rows to half in 143 us, 5.0 TB/s, the rate of a copy (on
+// traffic: 717 MB of int8 rows to half in 142 us, 5.1 TB/s, the rate of a copy (on
 // some cards 132 us).
 #include "ops.hpp"
 
@@ -103,7 +103,7 @@ static int read_launch(ReadArgs& p) {
                                  : k_cache_read<TYPE, KIND, 16>;
   // Large reads run with five workgroups a CU at most, by LDS that nobody uses:
   // fewer rows under way at once, in longer runs, suit the memory better (717 MB
-  // 143 against 162 us, 497 MB 111 against 117); small ones want all there are
+  // 142 against 162 us, 497 MB 111 against 117); small ones want all there are
   // (34 MB 10.2 against 11.0 us).
   const bool large = p.a.n_rows * p.c.n_heads * p.c.head_dim >= (16 << 20);
   return launch(k, dim3((unsigned)(tiles * p.parts)), dim3(256), large ? 32768 : 0, p.a.hip_stream, p);

@@ -638,3 +638,22 @@ def test_decode_weights_over_codes_keep_two_parts(lens, hq, hk, D, new, kind):
 @pytest.mark.parametrize("lens,hq,hk,D,new", [([700, 3], 16, 1, 128, 1), ([4000], 8, 2, 64, 1), ([90, 200], 8, 2, 128, 4)], ids=str)
 def test_decode_weights_over_bf16_caches_keep_two_parts(lens, hq, hk, D, new):
     test_decode_weights_over_codes_keep_two_parts(lens, hq, hk, D, new, BF)
+
+
+@gpu
+def test_no_keys_at_all():
+    """Rows without any key, over empty tensors and a block table without entries: 0, with a log sum of minus infinity."""
+    none = torch.empty(0, 2, 64, dtype=BF, device=DEV)
+    for n, heads in ((5, 4), (6000, 4), (1100, 64)):
+        q = rand(n, heads, 64 if heads == 4 else 128).to(DEV)
+        kv = none if heads == 4 else torch.empty(0, 2, 128, dtype=BF, device=DEV)
+        cu_q, cu_k = (torch.tensor([0, x], dtype=torch.int32, device=DEV) for x in (n, 0))
+        for causal in (True, False):
+            out, lse = O.attn_prompt(q, kv, kv, cu_q, cu_k, max_q=n, causal=causal, return_lse=True)
+            assert (out == 0).all() and (lse == -math.inf).all()
+    c = make_cache(BF, 2, 2, 16, 64)
+    dec = O.DecodeAttention(c, batch=3, heads=4)
+    q = rand(3, 1, 4, 64).to(DEV)
+    out, lse = dec(q, torch.empty(3, 0, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV), return_lse=True)
+    c.check()
+    assert (out == 0).all() and (lse == -math.inf).all()
