@@ -1,6 +1,7 @@
 /*
  * herschel_ops.h -- C ABI of the reference operators: the attention layer of a
- * served model, from the rows of the QKV product to the attention's output.
+ * served model, from the rows of the QKV product to the attention's output, and
+ * what a decoder layer has around it.
  *
  * The trace analyzer (herschel.h) rates an op by SOL = max(MFU, MBU) and sums
  * what its name would save at a reference SOL, "the SOL the same op reaches
@@ -13,7 +14,12 @@
  *    into a paged cache, quantised on the way (one launch);
  *  - herschel_cache_read: rows of the cache back in 16 bits;
  *  - herschel_attn_prompt: attention over packed prompts;
- *  - herschel_attn_decode: attention of one or a few new tokens over the cache.
+ *  - herschel_attn_decode: attention of one or a few new tokens over the cache;
+ *  - herschel_norm_rows: root-mean-square norm with the residual's addition, to
+ *    16 bits or to 8 with scales;
+ *  - herschel_product4: rows, of 16 or 8 bits, times 4-bit weights with a scale
+ *    for each group of a weight row;
+ *  - herschel_verify_drafts: drafted tokens against the target's probabilities.
  *
  * Conventions, those of herschel.h where they apply: every array is a DEVICE
  * pointer, the caller owns every buffer, return codes are HERSCHEL_*.  Unlike
@@ -42,8 +48,9 @@ extern "C" {
 #endif
 
 /* Element types.  FP8 (4 exponent bits, 3 fraction bits, largest value 448) and
- * INT8 are cache codes only. */
-enum { HERSCHEL_BF16 = 0, HERSCHEL_F16 = 1, HERSCHEL_FP8 = 2, HERSCHEL_INT8 = 3 };
+ * INT8 are codes, of caches and of rows; F32 is for what stays in 32 bits where
+ * an operator says so. */
+enum { HERSCHEL_BF16 = 0, HERSCHEL_F16 = 1, HERSCHEL_FP8 = 2, HERSCHEL_INT8 = 3, HERSCHEL_F32 = 4 };
 
 /* Rotary layouts: element i is paired with i + rotary_dim / 2, or 2 i with 2 i + 1. */
 enum { HERSCHEL_ROPE_HALF = 0, HERSCHEL_ROPE_INTERLEAVED = 1 };
@@ -53,7 +60,9 @@ enum {
   HERSCHEL_OP_BAD_PAGE = 1,     /* a block table entry outside [0, n_pages): its keys are not seen, its rows read as 0 */
   HERSCHEL_OP_BAD_LENGTH = 2,   /* lengths that fall, are negative or exceed the buffers: taken as the nearest valid */
   HERSCHEL_OP_BAD_POSITION = 4, /* a position outside the table: the token's rotated rows are NaN, nothing is cached */
-  HERSCHEL_OP_BAD_SLOT = 8      /* a slot at or beyond the cache's end: the token is not cached */
+  HERSCHEL_OP_BAD_SLOT = 8,     /* a slot at or beyond the cache's end: the token is not cached */
+  HERSCHEL_OP_BAD_TOKEN = 16,   /* a drafted token outside the vocabulary: not accepted */
+  HERSCHEL_OP_BAD_ROW = 32      /* a row of probabilities without one above 0: the token drawn from it is -1 */
 };
 
 /* A paged cache of keys and values: page p holds, for each head, page_size
@@ -184,6 +193,108 @@ int herschel_attn_decode_workspace(int32_t n_seqs, int32_t new_tokens, int32_t q
 /* Causal attention of each sequence's last new_tokens tokens over its cached
  * tokens.  Keys not seen have no effect, whatever the pages hold. */
 int herschel_attn_decode(const herschel_decode_args *args, const herschel_cache *cache);
+
+typedef struct {
+  const void *x;              /* [n_rows][dim] of type */
+  int64_t x_row;              /* elements from one row to the next, >= 0 */
+  const void *residual;       /* [n_rows][dim] of residual_type, or NULL */
+  int64_t residual_row;
+  void *residual_out;         /* [n_rows][dim] of residual_type, or NULL; may be residual with the same stride */
+  int64_t residual_out_row;   /* >= dim */
+  const void *weight;         /* [dim] of weight_type */
+  void *out;                  /* [n_rows][dim] of out_kind, contiguous; of the rows' type it may be a contiguous x */
+  float *scale;               /* 8 bits: [n_rows][dim / group], or [n_rows] with group 0 */
+  int64_t n_rows;             /* >= 0; 0: nothing is done */
+  int32_t dim;                /* 1 ... HERSCHEL_MAX_NORM_DIM */
+  int32_t group;              /* 8 bits: columns that share a scale, 32, 64 or 128 and a divisor of dim; 0: a row's */
+  int32_t type;               /* HERSCHEL_BF16 or HERSCHEL_F16 */
+  int32_t residual_type;      /* type or HERSCHEL_F32 */
+  int32_t weight_type;        /* type or HERSCHEL_F32 */
+  int32_t out_kind;           /* type, HERSCHEL_FP8 or HERSCHEL_INT8 */
+  float eps;                  /* finite, >= 0 */
+  void *hip_stream;
+} herschel_norm_args;
+
+#define HERSCHEL_MAX_NORM_DIM 32768
+
+/* For each row, in 32 bits: h = x + residual, residual_out = h rounded to its
+ * type, y = h / sqrt(mean(h^2) + eps) * weight, from the h that is not rounded.
+ * Squares of rows whose sum would leave 32 bits are summed scaled by a power of
+ * two.  out = y rounded, or codes with the scale of the row or of each group of
+ * columns, by the rule of a cache row. */
+int herschel_norm_rows(const herschel_norm_args *args);
+
+/* A matrix [n][k] of 4-bit codes c, each worth (c - zero) * scale with the zero
+ * and scale of its row's group of `group` columns.  Rows are held in tiles of 16,
+ * columns in tiles of 128, both filled up with codes, scales and zeros of 0:
+ *   codes[n / 16][k / 128][(k / 8) % 4 * 16 + n % 16][(k / 32) % 4][k % 4], bytes,
+ *     column k in the low half of its byte if k % 8 < 4, else in the high half;
+ *   scales and zeros[n / 16][groups, those of the filled columns][n % 16]. */
+typedef struct {
+  const void *codes;          /* 16-byte aligned */
+  const void *scales;         /* of scale_type, 16-byte aligned */
+  const uint8_t *zeros;       /* each 0 ... 15, 16-byte aligned; NULL: every zero is 8 */
+  int32_t n, k;               /* >= 1 */
+  int32_t group;              /* 32, 64 or 128; the last of a row may be shorter */
+  int32_t scale_type;         /* HERSCHEL_BF16 or HERSCHEL_F16 */
+} herschel_weights4;
+
+typedef struct {
+  const void *x;              /* [n_rows][k] of kind */
+  int64_t x_row;              /* elements from one row to the next, >= 0 */
+  const float *x_scale;       /* 8 bits: [n_rows][ceil(k / group)] with x_group, else [n_rows] */
+  void *out;                  /* [n_rows][n], gated [n_rows][n / 2], of type, contiguous */
+  int64_t n_rows;             /* >= 0; 0: nothing is done */
+  int32_t kind;               /* HERSCHEL_BF16 ... HERSCHEL_INT8 */
+  int32_t x_group;            /* 8 bits: 0 or the weights' group */
+  int32_t type;               /* HERSCHEL_BF16 or HERSCHEL_F16; that of rows of 16 bits */
+  int32_t gated;              /* n a multiple of 32: y = silu(a) b, a the first n / 2 columns of the product, b the others */
+  void *hip_stream;
+} herschel_product_args;
+
+/* out[m] = sum over k of x[m][k] * weight[n][k], codes summed within a group
+ * before they meet its scale, in 32 bits (int8 rows: whole numbers), rounded
+ * once.  A row that holds an infinity or a NaN comes out as NaN. */
+int herschel_product4(const herschel_product_args *args, const herschel_weights4 *weights);
+
+typedef struct {
+  const void *target;         /* [n_seqs][n_drafts + 1][vocab] of type: the target's probabilities at each draft and
+                                 behind the last */
+  int64_t target_seq, target_row; /* elements from one sequence, and one row, to the next, >= 0 */
+  const void *draft;          /* [n_seqs][n_drafts][vocab] of type: those that the drafts were drawn from; or NULL: each
+                                 draft had probability 1 */
+  int64_t draft_seq, draft_row;
+  const int64_t *tokens;      /* [n_seqs][n_drafts]: the drafted tokens */
+  const int32_t *counts;      /* [n_seqs]: drafts of each sequence, 0 ... n_drafts; NULL: n_drafts */
+  const float *accept_u;      /* [n_seqs][n_drafts]: a random number in [0, 1) for each draft */
+  const float *final_u;       /* [n_seqs]: and one for the token behind the accepted ones */
+  int64_t *out;               /* [n_seqs][n_drafts + 1]: the accepted drafts, the token drawn, -1 */
+  int32_t *accepted;          /* [n_seqs] */
+  int32_t n_seqs;             /* 0 ... 65535; 0: nothing is done */
+  int32_t n_drafts;           /* 0 ... HERSCHEL_MAX_DRAFTS */
+  int32_t vocab;              /* >= 1 */
+  int32_t type;               /* HERSCHEL_F32, HERSCHEL_BF16 or HERSCHEL_F16 */
+  void *workspace;            /* herschel_verify_workspace() bytes, 16-byte aligned; no two calls at once */
+  size_t workspace_bytes;
+  uint32_t *status;
+  void *hip_stream;
+} herschel_verify_args;
+
+#define HERSCHEL_MAX_DRAFTS 1024
+
+/* Bytes of workspace for calls of at most these sizes. */
+int herschel_verify_workspace(int32_t n_seqs, int32_t vocab, size_t *bytes);
+
+/* Draft t of a sequence, token x, is accepted iff those before it are and
+ * accept_u[t] * draft[t][x] < target[t][x].  Behind the accepted ones one token is
+ * drawn: from target - draft, where that is above 0, of the first draft that is
+ * not accepted; behind the last draft from the target.  Where nothing is above 0,
+ * from the target alone.  The token drawn is the lowest whose cumulative sum is
+ * above final_u times the sum of all (with a final_u not below 1, the last whose
+ * part is above 0).  Products, differences and sums are in 64 bits; what is not
+ * above 0, a NaN among it, counts as 0.  A count out of range is taken as the
+ * nearest valid one (HERSCHEL_OP_BAD_LENGTH). */
+int herschel_verify_drafts(const herschel_verify_args *args);
 
 #ifdef __cplusplus
 }

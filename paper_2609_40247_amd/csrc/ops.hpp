@@ -1,5 +1,5 @@
 // Shared pieces of the reference operators (rotary write, cache read, prompt
-// and decode attention): element types, conversions, the cache's addressing
+// and decode attention, norm, products with 4-bit weights, verification): element types, conversions, the cache's addressing
 // and the host's launch helper.  Sums, maxima and scales are 32-bit floats;
 // elements are bf16 or half, cache codes 8 bits.
 #pragma once
@@ -31,6 +31,39 @@ constexpr float SCALE_MIN = 0x1p-100f;
 
 __host__ __device__ constexpr bool quantised(int kind) { return kind == HERSCHEL_FP8 || kind == HERSCHEL_INT8; }
 __host__ __device__ constexpr int code_bytes(int kind) { return quantised(kind) ? 1 : 2; }
+
+// The codes' scale of a row whose largest magnitude has these bits, and its
+// inverse; NaN and 0 if the row holds an infinity or a NaN.
+template <int KIND>
+__device__ __forceinline__ float row_scale(uint32_t amax_bits, float& inv) {
+  if (amax_bits >= 0x7f800000u) {
+    inv = 0.0f;
+    return __builtin_nanf("");
+  }
+  const float s = fmaxf(__builtin_bit_cast(float, amax_bits) * (1.0f / code_max(KIND)), SCALE_MIN);
+  inv = 1.0f / s;
+  return s;
+}
+template <int KIND>
+__device__ __forceinline__ uint32_t encode4(const float* x, float inv) {
+  constexpr float M = code_max(KIND);
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // 0 * NaN in a row without a scale: the code is 0 there
+    const float z = inv == 0.0f ? 0.0f : x[i] * inv;
+    y[i] = __builtin_amdgcn_fmed3f(z, -M, M);
+  }
+  if constexpr (KIND == HERSCHEL_FP8) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  } else {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= ((uint32_t)(int)__builtin_rintf(y[i]) & 0xffu) << (8 * i);
+    return w;
+  }
+}
 
 // Two floats rounded to nearest even into a word of TYPE, the first in the low half, and back.
 template <int TYPE>

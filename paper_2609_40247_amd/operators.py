@@ -1,4 +1,4 @@
-"""Reference operators: the attention layer of a served model on MI355X.
+"""Reference operators: the attention layer of a served model on MI355X, and what a decoder layer has around it.
 
 The C ABI is ``include/herschel_ops.h``; this module checks tensors, fills its
 structures and calls the HIP library:
@@ -9,6 +9,10 @@ structures and calls the HIP library:
 ``cache_read``       rows of the cache back in 16 bits
 ``attn_prompt``      attention over packed prompts
 ``DecodeAttention``  attention of new tokens over the cache (keeps the workspace)
+``norm_rows``        root-mean-square norm with the residual's addition, to 16 bits or 8 (``Rows8``)
+``Weights4``         a matrix of 4-bit weights with a scale for each group of a row
+``product4``         rows, 16-bit or 8-bit, times such a matrix, gated where asked for
+``verify_drafts``    drafted tokens against the target's probabilities
 
 Every call is enqueued on torch's current stream and returns at once.  What
 only the device can see to be wrong (a page id, a length, a position, a slot)
@@ -22,19 +26,22 @@ import ctypes
 import functools
 import math
 import struct
+from typing import NamedTuple
 
 import torch
 
 from . import herschel as H
 
-BF16, F16, FP8, INT8 = 0, 1, 2, 3
+BF16, F16, FP8, INT8, F32 = 0, 1, 2, 3, 4
 TYPES = {torch.bfloat16: BF16, torch.float16: F16}
 KINDS = {**TYPES, torch.float8_e4m3fn: FP8, torch.int8: INT8}
 LAYOUTS = {"half": 0, "interleaved": 1}
-BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT = 1, 2, 4, 8
-MAX_DECODE_SEQS = 4096
+CODES = {torch.float8_e4m3fn: FP8, torch.int8: INT8}
+BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, BAD_TOKEN, BAD_ROW = 1, 2, 4, 8, 16, 32
+MAX_DECODE_SEQS, MAX_NORM_DIM, MAX_DRAFTS = 4096, 32768, 1024
 _FAULTS = {BAD_PAGE: "a block table entry outside the cache", BAD_LENGTH: "lengths that do not fit the buffers",
-           BAD_POSITION: "a position outside the rotary table", BAD_SLOT: "a slot beyond the cache's end"}
+           BAD_POSITION: "a position outside the rotary table", BAD_SLOT: "a slot beyond the cache's end",
+           BAD_TOKEN: "a drafted token outside the vocabulary", BAD_ROW: "probabilities of which none is above 0"}
 
 _P = ctypes.c_void_p
 _I64, _I32 = ctypes.c_int64, ctypes.c_int32
@@ -77,12 +84,39 @@ class HerschelDecodeArgs(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_size_t), ("status", _P), ("hip_stream", _P)]
 
 
+class HerschelNormArgs(ctypes.Structure):
+    _fields_ = [("x", _P), ("x_row", _I64), ("residual", _P), ("residual_row", _I64), ("residual_out", _P),
+                ("residual_out_row", _I64), ("weight", _P), ("out", _P), ("scale", _P), ("n_rows", _I64), ("dim", _I32),
+                ("group", _I32), ("type", _I32), ("residual_type", _I32), ("weight_type", _I32), ("out_kind", _I32),
+                ("eps", ctypes.c_float), ("hip_stream", _P)]
+
+
+class HerschelWeights4(ctypes.Structure):
+    _fields_ = [("codes", _P), ("scales", _P), ("zeros", _P), ("n", _I32), ("k", _I32), ("group", _I32),
+                ("scale_type", _I32)]
+
+
+class HerschelProductArgs(ctypes.Structure):
+    _fields_ = [("x", _P), ("x_row", _I64), ("x_scale", _P), ("out", _P), ("n_rows", _I64), ("kind", _I32),
+                ("x_group", _I32), ("type", _I32), ("gated", _I32), ("hip_stream", _P)]
+
+
+class HerschelVerifyArgs(ctypes.Structure):
+    _fields_ = [("target", _P), ("target_seq", _I64), ("target_row", _I64), ("draft", _P), ("draft_seq", _I64),
+                ("draft_row", _I64), ("tokens", _P), ("counts", _P), ("accept_u", _P), ("final_u", _P), ("out", _P),
+                ("accepted", _P), ("n_seqs", _I32), ("n_drafts", _I32), ("vocab", _I32), ("type", _I32),
+                ("workspace", _P), ("workspace_bytes", ctypes.c_size_t), ("status", _P), ("hip_stream", _P)]
+
+
 # The same structures as struct formats: filling one this way takes 0.2 us
 # instead of 1 to 2, and a decode step's calls are as short as their host time.
 _ROPE = struct.Struct("@3P6q2P4q2PqPq6i2P")
 _READ = struct.Struct("@PqPiq2Pi2P")
 _PROMPT = struct.Struct("@3P6q4Pi2q7ifPN2P")
 _DECODE = struct.Struct("@P3q3PqP5ifPN2P")
+_NORM = struct.Struct("@PqPqPq3Pq6ifP")
+_PRODUCT = struct.Struct("@Pq2Pq4iP")
+_VERIFY = struct.Struct("@P2qP2q6P4iPN2P")
 
 _ready = {}
 
@@ -93,7 +127,8 @@ def load(variant: str | None = None) -> ctypes.CDLL:
     if lib is None:
         lib = H.load(variant)
         for name, n in (("herschel_rope_write", 2), ("herschel_cache_read", 2), ("herschel_attn_prompt", 1),
-                        ("herschel_attn_decode", 2)):
+                        ("herschel_attn_decode", 2), ("herschel_norm_rows", 1), ("herschel_product4", 2),
+                        ("herschel_verify_drafts", 1)):
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = ctypes.c_int, [_P] * n
         lib.herschel_attn_prompt_workspace.restype = ctypes.c_int
@@ -101,6 +136,8 @@ def load(variant: str | None = None) -> ctypes.CDLL:
                                                        ctypes.POINTER(ctypes.c_size_t)]
         lib.herschel_attn_decode_workspace.restype = ctypes.c_int
         lib.herschel_attn_decode_workspace.argtypes = [_I32, _I32, _I32, _P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.herschel_verify_workspace.restype = ctypes.c_int
+        lib.herschel_verify_workspace.argtypes = [_I32, _I32, ctypes.POINTER(ctypes.c_size_t)]
         if variant:
             _ready[variant] = lib
     return lib
@@ -523,3 +560,294 @@ class DecodeAttention:
         if given is not None:
             _written((given,))
         return (out, lse) if return_lse else out
+
+
+# ------------------------------------------------------------ around the attention
+class Rows8(NamedTuple):
+    """Rows of 8-bit codes [rows, columns], float8_e4m3fn or int8, each worth itself times its scale, float32
+    [rows, 1] or [rows, groups of columns]."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+    def values(self) -> torch.Tensor:
+        """The rows in 32 bits."""
+        rows, columns = self.codes.shape
+        groups = self.scale.shape[1]
+        return (self.codes.float().view(rows, groups, columns // groups) * self.scale[..., None]).view(rows, columns)
+
+
+def _row(t: torch.Tensor, name: str, shape: tuple, dtype, device: int) -> int:
+    """The row stride of a tensor [rows, columns] of this type on this GPU, columns contiguous."""
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or t.stride(1) != 1 and shape[1] > 1:
+        _need(t.dtype == dtype, f"{name} must be {dtype}")
+        _need(t.get_device() == device, f"{name} must be on GPU {device}")
+        _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
+        _need(False, f"{name}'s last dimension must be contiguous")
+    return t.stride(0)
+
+
+def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, *, eps: float = 1e-6,
+              kind: torch.dtype | None = None, group: int = 0, residual_out: torch.Tensor | None = None,
+              out: torch.Tensor | Rows8 | None = None, lib=None):
+    """h / sqrt(mean(h^2) + eps) * weight for each row h of x [rows, columns], with a residual of h = x + residual.
+
+    ``residual`` has x's type or is float32; the sums go to ``residual_out``, without it back into ``residual``.
+    The norm is that of the sums in 32 bits, before they are rounded.  ``weight`` [columns] has x's type or is
+    float32.  ``kind`` float8_e4m3fn or int8 asks for ``Rows8``, with a scale for each row, or for each ``group``
+    (32, 64 or 128) of its columns; without it the result has x's type.  ``out`` is written where given."""
+    if not (x.is_cuda and x.dim() == 2 and x.dtype in TYPES and (x.stride(1) == 1 or x.shape[1] < 2)):
+        _need(x.dim() == 2, "x must have 2 dimensions")
+        _rows(x, "x", 2)
+    dev, dtype, shape = x.get_device(), x.dtype, x.shape
+    n, dim = shape
+    if not 1 <= dim <= MAX_NORM_DIM:
+        raise ValueError(f"rows must have 1 to {MAX_NORM_DIM} columns")
+    if not (0 <= eps < math.inf):
+        raise ValueError("eps must be finite and not negative")
+    if weight.dtype is not dtype and weight.dtype is not torch.float32:
+        raise ValueError("weight must have x's type or be float32")
+    w = _ints(weight, "weight", weight.dtype, (dim,), dev)
+    needs, given = x.requires_grad or weight.requires_grad, ()
+    rp = rs = op = os = 0
+    if residual is not None:
+        if residual.dtype is not dtype and residual.dtype is not torch.float32:
+            raise ValueError("residual must have x's type or be float32")
+        rp, rs = residual.data_ptr(), _row(residual, "residual", shape, residual.dtype, dev)
+        if residual_out is None:
+            residual_out = residual
+        op, os = residual_out.data_ptr(), _row(residual_out, "residual_out", shape, residual.dtype, dev)
+        if os < dim:
+            if n > 1:
+                raise ValueError("residual_out's rows must not overlap")
+            os = dim
+        needs, given = needs or residual.requires_grad or residual_out.requires_grad, (residual_out,)
+    elif residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    scale = 0
+    if kind is None:
+        if group:
+            raise ValueError("group goes with rows of 8 bits")
+        if out is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+            to = out.data_ptr()
+        else:
+            to, given = _ints(out, "out", dtype, shape, dev), given + (out,)
+            needs = needs or out.requires_grad
+        code = TYPES[dtype]
+    else:
+        if kind not in CODES:
+            raise ValueError("kind must be float8_e4m3fn or int8")
+        if group not in (0, 32, 64, 128) or group and dim % group:
+            raise ValueError("group must be 0, or 32, 64 or 128 and a divisor of the columns")
+        code, groups = CODES[kind], (n, dim // group if group else 1)
+        if out is None:
+            out = Rows8(x.new_empty(shape, dtype=kind), x.new_empty(groups, dtype=torch.float32))
+        else:
+            given += (out[0], out[1])
+        to, scale = _ints(out[0], "out's codes", kind, shape, dev), _ints(out[1], "out's scale", torch.float32, groups, dev)
+    if needs:
+        _no_gradients("norm_rows")
+    args = _NORM.pack(x.data_ptr(), x.stride(0), rp, rs, op, os, w, to, scale, n, dim, group, TYPES[dtype],
+                      F32 if residual is not None and residual.dtype is torch.float32 else TYPES[dtype],
+                      F32 if weight.dtype is torch.float32 else TYPES[dtype], code, eps, _stream(dev))
+    _call((lib or _lib()).herschel_norm_rows, dev, "norm_rows", args)
+    if given:
+        _written(given)
+    return out
+
+
+class Weights4:
+    """A matrix [n, k] of 4-bit weights, each (code - zero) * scale with the zero and scale of its row's group of
+    32, 64 or 128 columns, laid out once in the tiles that ``product4`` reads.
+
+    ``codes`` uint8 [n, k / 2 rounded up], the even column in the low four bits (and the last bits of an odd k of no
+    effect); ``scales`` [n, groups] bfloat16 or float16; ``zeros`` uint8 [n, groups] of 0 to 15, 8 everywhere
+    without them.  The group is the one of which a row of k has as many as there are scales."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, zeros: torch.Tensor | None = None, *, k: int | None = None):
+        _need(codes.dtype == torch.uint8 and codes.dim() == 2 and codes.numel() > 0, "codes must be uint8 [n, k / 2]")
+        n, half = codes.shape
+        k = 2 * half if k is None else k
+        _need(k >= 1 and (k + 1) // 2 == half, "codes must have k / 2 bytes a row, rounded up")
+        _need(scales.dtype in TYPES, "scales must be bfloat16 or float16")
+        _need(scales.dim() == 2 and scales.shape[0] == n and scales.device == codes.device,
+              "scales must be [n, groups], on the codes' device")
+        group = next((g for g in (128, 64, 32) if -(-k // g) == scales.shape[1]), 0)
+        _need(group > 0, "scales must be one for each 32, 64 or 128 columns")
+        if zeros is not None:
+            _need(zeros.dtype == torch.uint8 and zeros.shape == scales.shape and zeros.device == codes.device,
+                  "zeros must be uint8, like scales")
+            _need(int(zeros.max()) <= 15, "zeros must be 0 to 15")
+        self.n, self.k, self.group, self.groups, self.device = n, k, group, scales.shape[1], codes.device
+        tiles_n, tiles_k = -(-n // 16), -(-k // 128)
+        self.codes = codes.new_empty((tiles_n, tiles_k, 4, 16, 4, 4))
+        for at in range(0, tiles_n, 256):  # 4096 rows at a time, so that no copy of a byte a weight is made of them all
+            part = codes[at * 16:(at + 256) * 16]
+            wide = codes.new_zeros((-(-part.shape[0] // 16) * 16, tiles_k * 128))
+            wide[:part.shape[0], 0:k:2] = part & 15
+            wide[:part.shape[0], 1:k:2] = part[:, :k // 2] >> 4
+            # rows of a tile, its columns as 4 words' 4 lanes' halves of 4 bytes
+            wide = wide.view(-1, 16, tiles_k, 4, 4, 2, 4)
+            packed = wide[..., 0, :] | (wide[..., 1, :] << 4)
+            self.codes[at:at + 256] = packed.permute(0, 2, 4, 1, 3, 5)
+        self.scales, self.zeros = self._tile(scales), None if zeros is None else self._tile(zeros)
+        self.struct = HerschelWeights4(self.codes.data_ptr(), self.scales.data_ptr(),
+                                       None if zeros is None else self.zeros.data_ptr(), n, k, group, TYPES[scales.dtype])
+        self._at, self._device = ctypes.addressof(self.struct), codes.get_device()
+
+    def _tile(self, t: torch.Tensor) -> torch.Tensor:
+        """[n, groups] as [tiles of 16 rows, groups of the filled up columns, 16]."""
+        tiles, groups = -(-self.n // 16), -(-self.k // 128) * (128 // self.group)
+        wide = t.new_zeros((tiles * 16, groups))
+        wide[:self.n, :self.groups] = t
+        return wide.view(tiles, 16, groups).transpose(1, 2).contiguous()
+
+    @classmethod
+    def quantise(cls, weights: torch.Tensor, group: int = 128, *, zeros: bool = False, scale_dtype=None):
+        """To the nearest codes: -7 to 7 times a group's scale, or with ``zeros`` 16 steps from its smallest weight
+        (or 0) to its largest (or 0).  ``scale_dtype``: that of 16-bit weights, else bfloat16."""
+        _need(weights.dim() == 2 and weights.numel() > 0 and weights.is_floating_point(), "weights must be [n, k] of numbers")
+        _need(group in (32, 64, 128), "group must be 32, 64 or 128")
+        scale_dtype = scale_dtype or (weights.dtype if weights.dtype in TYPES else torch.bfloat16)
+        _need(scale_dtype in TYPES, "scale_dtype must be bfloat16 or float16")
+        n, k = weights.shape
+        groups = -(-k // group)
+        codes = torch.empty((n, (k + 1) // 2), dtype=torch.uint8, device=weights.device)
+        scales = torch.empty((n, groups), dtype=scale_dtype, device=weights.device)
+        zero = torch.empty((n, groups), dtype=torch.uint8, device=weights.device) if zeros else None
+        for at in range(0, n, 4096):
+            w = weights[at:at + 4096].float()
+            w = torch.nn.functional.pad(w, (0, groups * group - k)).view(-1, groups, group)
+            if zeros:
+                low, high = w.amin(-1).clamp_max(0), w.amax(-1).clamp_min(0)
+                s = (high / 15 - low / 15).to(scale_dtype)
+            else:
+                s = (w.abs().amax(-1) / 7).to(scale_dtype)
+            inv = torch.where(s > 0, 1 / s.float(), 0.0)
+            z = (-low * inv).round().clamp(0, 15) if zeros else torch.full_like(inv, 8.0)
+            c = (w * inv[..., None] + z[..., None]).round().clamp(0 if zeros else 1, 15).to(torch.uint8).view(-1, groups * group)
+            c = torch.nn.functional.pad(c[:, :k], (0, k % 2))
+            codes[at:at + 4096] = c[:, ::2] | (c[:, 1::2] << 4)
+            scales[at:at + 4096] = s
+            if zeros:
+                zero[at:at + 4096] = z.to(torch.uint8)
+        return cls(codes, scales, zero, k=k)
+
+    def dense(self) -> torch.Tensor:
+        """The weights [n, k] in 32 bits."""
+        tiles_n, tiles_k = self.codes.shape[:2]
+        b = self.codes.permute(0, 3, 1, 4, 2, 5)  # row, tile, word, lane, byte
+        c = torch.stack([b & 15, b >> 4], -2).reshape(tiles_n * 16, tiles_k, 128 // self.group, self.group).float()
+
+        def wide(t):
+            return t.transpose(1, 2).reshape(tiles_n * 16, tiles_k, -1, 1).float()
+        c = (c - (8.0 if self.zeros is None else wide(self.zeros))) * wide(self.scales)
+        return c.view(tiles_n * 16, -1)[:self.n, :self.k].contiguous()
+
+
+def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False, dtype: torch.dtype | None = None,
+             out: torch.Tensor | None = None, lib=None) -> torch.Tensor:
+    """Rows x [rows, k], or 8-bit ones with a scale a row or for each of the weights' groups, times ``weights``
+    [n, k]: [rows, n].  Gated, the first half of the weights' rows gates the second: silu(a) * b, [rows, n / 2].
+
+    ``dtype`` is the result's: the type of 16-bit rows, else bfloat16 or float16 (bfloat16 if not given).  A row
+    that holds an infinity or a NaN comes out as NaN."""
+    if isinstance(x, Rows8):
+        t, scale = x
+        if t.dtype not in CODES:
+            raise ValueError("rows of 8 bits must be float8_e4m3fn or int8")
+        kind, dtype = CODES[t.dtype], dtype or torch.bfloat16
+        if dtype not in TYPES:
+            raise ValueError("dtype must be bfloat16 or float16")
+    else:
+        t, scale = x, None
+        if t.dtype not in TYPES or dtype is not None and dtype != t.dtype:
+            _need(t.dtype in TYPES, "x must be bfloat16, float16 or Rows8")
+            _need(False, "dtype must be that of rows of 16 bits")
+        kind, dtype = TYPES[t.dtype], t.dtype
+    dev, shape = t.get_device(), t.shape
+    if dev < 0 or len(shape) != 2 or weights._device != dev:
+        _need(len(shape) == 2, "x must have 2 dimensions")
+        _need(dev >= 0, "x must be on a GPU")
+        _need(False, "the weights are on another device")
+    n, k = shape
+    stride, x_group, scales = _row(t, "x", (n, weights.k), t.dtype, dev), 0, 0
+    if scale is not None:
+        groups = scale.shape[1] if scale.dim() == 2 else 0
+        if groups != 1 and groups != weights.groups:
+            raise ValueError("rows of 8 bits have a scale a row, [rows, 1], or one for each of the weights' groups")
+        scales = _ints(scale, "scale", torch.float32, (n, groups), dev)
+        x_group = weights.group if groups > 1 else 0
+    if gated and weights.n % 32:
+        raise ValueError("a gated product needs a multiple of 32 weight rows")
+    if t.requires_grad or scale is not None and scale.requires_grad or out is not None and out.requires_grad:
+        _no_gradients("product4")
+    given, shape = out, (n, weights.n // 2 if gated else weights.n)
+    if out is None:
+        out = t.new_empty(shape, dtype=dtype)
+        to = out.data_ptr()
+    else:
+        to = _ints(out, "out", dtype, shape, dev)
+    args = _PRODUCT.pack(t.data_ptr(), stride, scales, to, n, kind, x_group, TYPES[dtype], bool(gated), _stream(dev))
+    _call((lib or _lib()).herschel_product4, dev, "product4", args, weights._at)
+    if given is not None:
+        _written((given,))
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def _verify_workspace(lib, *sizes) -> int:
+    """Bytes of workspace for a call of these sizes."""
+    size = ctypes.c_size_t(0)
+    lib.herschel_verify_workspace(*sizes, ctypes.byref(size))
+    return int(size.value)
+
+
+_PROBABILITIES = {torch.float32: F32, **TYPES}
+
+
+def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, accept: torch.Tensor, final: torch.Tensor, *,
+                  draft: torch.Tensor | None = None, counts: torch.Tensor | None = None,
+                  status: torch.Tensor | None = None, lib=None) -> tuple:
+    """Drafted tokens [sequences, drafts] (int64) against the target's probabilities [sequences, drafts + 1, vocab],
+    float32, bfloat16 or float16, at each draft and behind the last.
+
+    Draft t of a sequence is accepted iff those before it are and accept[t] * draft[t, token] < target[t, token],
+    with ``draft`` [sequences, drafts, vocab] the probabilities that the drafts were drawn from (None: each was the
+    one choice, of probability 1).  Behind the accepted ones one token is drawn, from max(target - draft, 0) at the
+    first that is not accepted or from the target behind the last (or where nothing of the difference is left): the
+    lowest whose cumulative sum is above final times the whole sum.  ``accept`` [sequences, drafts] and ``final``
+    [sequences] are random numbers in [0, 1), float32; ``counts`` (int32) the drafts of each sequence where some
+    have fewer.  Returns the tokens [sequences, drafts + 1], -1 behind the drawn one, and the numbers of accepted
+    drafts (int32)."""
+    shape, dev = target.shape, target.get_device()
+    if dev < 0 or len(shape) != 3 or target.dtype not in _PROBABILITIES or shape[2] < 1 or target.stride(2) != 1 and shape[2] > 1:
+        _need(dev >= 0, "target must be on a GPU")
+        _need(len(shape) == 3 and shape[2] >= 1, "target must be [sequences, drafts + 1, vocab]")
+        _need(target.dtype in _PROBABILITIES, "target must be float32, bfloat16 or float16")
+        _need(False, "target's last dimension must be contiguous")
+    B, S, V = shape[0], shape[1] - 1, shape[2]
+    if not (0 <= S <= MAX_DRAFTS and B <= 65535 and V <= 2 ** 30):
+        raise ValueError(f"at most 65535 sequences, 0 to {MAX_DRAFTS} drafts and a vocabulary of at most 2^30")
+    drafted = _ints(tokens, "tokens", torch.int64, (B, S), dev)
+    u, last = _ints(accept, "accept", torch.float32, (B, S), dev), _ints(final, "final", torch.float32, (B,), dev)
+    dp = ds = dr = 0
+    if draft is not None:
+        if draft.dtype is not target.dtype or draft.get_device() != dev or draft.shape != (B, S, V) or (
+                draft.stride(2) != 1 and V > 1):
+            _like(draft, target, "draft")
+            _need(tuple(draft.shape) == (B, S, V), f"draft must have shape {(B, S, V)}")
+            _need(False, "draft's last dimension must be contiguous")
+        dp, ds, dr = draft.data_ptr(), draft.stride(0), draft.stride(1)
+    if target.requires_grad or draft is not None and draft.requires_grad:
+        _no_gradients("verify_drafts")
+    n = 0 if counts is None else _ints(counts, "counts", torch.int32, (B,), dev)
+    out, accepted = tokens.new_empty((B, S + 1)), tokens.new_empty((B,), dtype=torch.int32)
+    lib = lib or _lib()
+    size = _verify_workspace(lib, B, V)
+    workspace = target.new_empty(size, dtype=torch.uint8)
+    args = _VERIFY.pack(target.data_ptr(), target.stride(0), target.stride(1), dp, ds, dr, drafted, n, u, last,
+                        out.data_ptr(), accepted.data_ptr(), B, S, V, _PROBABILITIES[target.dtype], workspace.data_ptr(),
+                        size, 0 if status is None else _status(status, dev), _stream(dev))
+    _call(lib.herschel_verify_drafts, dev, "verify_drafts", args)
+    return out, accepted

@@ -1,0 +1,766 @@
+"""The reference operators around the attention (norm of rows, products with
+4-bit weights, verification of drafted tokens) against plain 64-bit
+implementations, and their refusals.
+
+Tolerances are bounds, derived here and not fitted; u is the unit roundoff of
+the output's type (bfloat16 2^-8, half 2^-11).
+
+Norm.  h = x + residual is rounded once, 2^-24 of itself.  The sum of its
+squares, all positive, is off by the longest chain of additions times 2^-24: 32
+of a thread, 6 across a wave, 16 waves, under 2^-18 of itself; the root halves
+that, and mean, root, quotient and three products add a few 2^-24 each.  So
+y is off by less than 2^-17 |y|, and rounded once.  A code is off by half a step:
+2^-4 of itself in fp8, or 2^-10 of a scale below its normal numbers, half a scale
+in int8; with the 2^-17 of y, of the row's largest and of the scale on top.
+
+Product.  A group's sums have at most 128 products of a whole number below 16
+with an element, exact, and 128 additions, each off by at most 2^-23 (whatever
+the matrix cores' rounding) of the sum of magnitudes so far; the zero's part
+likewise; then a sum over the groups and the waves' parts.  With A = sum over k of
+(c + z) s |x| the error is below (140 + groups) 2^-23 A, and y is rounded once.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+
+import pytest
+import torch
+
+from paper_2609_40247_amd import herschel as H
+from paper_2609_40247_amd import operators as O
+from test_operators import BF, DEV, F8, FAKE, HF, I8, U, gpu, lib, named, rand
+
+F32 = torch.float32
+TOP = {F8: 448.0, I8: 127.0}
+TINY = {BF: 2.0 ** -134, HF: 2.0 ** -25, F32: 2.0 ** -150}  # half the smallest step
+
+
+# ------------------------------------------------------------ norm
+def exact_norm(x, w, residual, eps):
+    h = x.double() + (0 if residual is None else residual.double())
+    return h, h / torch.sqrt((h * h).mean(1, keepdim=True) + eps) * w.double()
+
+
+def check_norm(y, e, dtype, kind, group):
+    if kind is None:
+        assert y.dtype == dtype
+        bound = U[dtype] * e.abs() + 2.0 ** -17 * (1 + U[dtype]) * e.abs() + TINY[dtype]
+        assert ((y.double().cpu() - e).abs() <= bound).all()
+        return
+    n, dim = e.shape
+    s = (e.view(n, -1, group or dim).abs().amax(-1) / TOP[kind]).clamp_min(2.0 ** -100)
+    assert y.codes.dtype == kind and y.codes.shape == e.shape and y.scale.shape == s.shape
+    assert ((y.scale.double().cpu() - s).abs() <= 2.0 ** -16 * s).all()
+    wide = s.repeat_interleave(group or dim, 1)
+    step = torch.maximum(2.0 ** -4 * e.abs(), 2.0 ** -10 * wide) if kind == F8 else 0.5 * wide
+    values = y.codes.double().cpu() * y.scale.double().cpu().repeat_interleave(group or dim, 1)
+    assert ((values - e).abs() <= step * (1 + 2.0 ** -14) + 2.0 ** -16 * (e.abs() + wide)).all()
+    assert torch.equal(y.values().cpu(), values.float())
+
+
+@gpu
+@pytest.mark.parametrize("kind", [None, F8, I8], ids=str)
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("rows,dim,residual,wide", [
+    (1, 1, None, False), (3, 5, "same", True), (7, 8, "f32", False), (2, 63, "f32", True), (5, 512, "same", False),
+    (4, 1000, None, True), (33, 2051, "f32", False), (1, 4096, "same", False), (19, 5120, "same", True),
+    (2050, 136, "same", False), (2049, 2560, "f32", False), (2048, 4097, None, False), (3, 8200, "same", False),
+    (2, 16_392, "f32", True), (2, 32_768, "same", False), (1, 32_767, "same", False)])
+def test_norm_rows(rows, dim, residual, wide, dtype, kind):
+    x, w = rand(rows, dim, seed=1, dtype=dtype), rand(dim, seed=2, dtype=F32 if wide else dtype)
+    x[0] *= 30
+    r = None if residual is None else rand(rows, dim, seed=3, dtype=F32 if residual == "f32" else dtype, gain=3.0)
+    h, e = exact_norm(x, w, r, 1e-6)
+    kept = None if r is None else r.to(DEV)
+    y = O.norm_rows(x.to(DEV), w.to(DEV), kept, kind=kind)
+    check_norm(y, e, dtype, kind, 0)
+    if r is not None:  # in place
+        u = 0 if residual == "f32" else U[dtype]
+        assert ((kept.double().cpu() - h).abs() <= u * h.abs() + 2.0 ** -23 * h.abs() + TINY[r.dtype]).all()
+
+
+@gpu
+@pytest.mark.parametrize("kind", [F8, I8], ids=str)
+@pytest.mark.parametrize("dim,group", [(32, 32), (4096, 128), (5120, 64), (96, 32), (2176, 128), (8320, 64)])
+@pytest.mark.parametrize("odd", [False, True])
+def test_norm_rows_of_groups(dim, group, kind, odd):
+    """A scale for each group of columns; groups of very different magnitudes, one of zeros."""
+    x = rand(9, dim, seed=4, gain=2.0)
+    x *= (2.0 ** torch.arange(dim // group).remainder(11)).repeat_interleave(group).to(BF)
+    x[2, :group] = 0
+    w = rand(dim, seed=5)
+    given = x.to(DEV)
+    if odd:  # rows that start at odd elements
+        given = torch.cat([x[:, :1], x], 1).to(DEV)[:, 1:]
+    y = O.norm_rows(given, w.to(DEV), kind=kind, group=group)
+    check_norm(y, exact_norm(x, w, None, 1e-6)[1], BF, kind, group)
+    assert (y.scale[2, 0] == 2.0 ** -100) and (y.codes[2, :group].float() == 0).all()
+
+
+@gpu
+@pytest.mark.parametrize("residual", [None, "same", "f32"])
+def test_norm_rows_strides_and_outputs(residual):
+    """Rows inside wider ones, a row for all, given outputs, a separate residual; the rest of the buffers stays."""
+    dtype, n, dim = HF, 21, 264
+    r_type = F32 if residual == "f32" else dtype
+    big = rand(n, 3 * dim, seed=6, dtype=dtype).to(DEV)
+    w = rand(dim, seed=7, dtype=dtype).to(DEV)
+    for from_, x in ((0, big[:, dim:2 * dim]), (1, big[:, dim + 1:2 * dim + 1]), (2, big[:1, :dim].expand(n, dim))):
+        r = r_in = None
+        if residual:
+            r = rand(n, 2 * dim, seed=8, dtype=r_type).to(DEV)
+            r_in = r[:, from_:from_ + dim]
+        h, e = exact_norm(x.cpu(), w.cpu(), None if r_in is None else r_in.cpu(), 1e-5)
+        before = None if r is None else r.clone()
+        out = torch.full((n, dim), 7.0, dtype=dtype, device=DEV)
+        wide = torch.full((n, dim + 16), 7.0, dtype=r_type, device=DEV)
+        y = O.norm_rows(x, w, r_in, eps=1e-5, out=out, residual_out=wide[:, 8:8 + dim] if residual else None)
+        assert y is out
+        check_norm(y, e, dtype, None, 0)
+        if residual:
+            assert torch.equal(r, before)
+            assert (wide[:, :8] == 7).all() and (wide[:, 8 + dim:] == 7).all()
+            assert ((wide[:, 8:8 + dim].double().cpu() - h).abs() <= U[HF] * h.abs() + TINY[dtype]).all()
+            O.norm_rows(x, w, r_in, eps=1e-5, out=out)
+            assert torch.equal(r_in, wide[:, 8:8 + dim]) and torch.equal(r[:, from_ + dim:], before[:, from_ + dim:])
+    x = rand(n, dim, seed=9, dtype=dtype).to(DEV)
+    want = O.norm_rows(x, w)
+    assert torch.equal(O.norm_rows(x, w, out=x), want) and torch.equal(x, want)  # over its own input
+    rows8 = O.Rows8(torch.zeros(n, dim, dtype=I8, device=DEV), torch.zeros(n, 1, device=DEV))
+    got = O.norm_rows(want, w, kind=I8, out=rows8)
+    assert got is rows8 and torch.equal(got.values(), O.norm_rows(want, w, kind=I8).values())
+
+
+@gpu
+@pytest.mark.parametrize("dim", [64, 777, 4096])
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+def test_norm_rows_far_magnitudes(dim, dtype):
+    """Rows whose squares leave 32 bits, above and below, with eps and without."""
+    base = rand(6, dim, seed=10, dtype=F32)
+    gain = torch.tensor([1.0, 2.0 ** 120, 2.0 ** 70, 2.0 ** -70, 2.0 ** -110, 2.0 ** -120] if dtype == BF else
+                        [1.0, 2.0 ** 12, 2.0 ** 10, 2.0 ** -10, 2.0 ** -13, 2.0 ** -14])
+    x = (base * gain[:, None]).to(dtype)
+    w = rand(dim, seed=11, dtype=dtype)
+    for eps in (0.0, 1e-30, 1e-6):
+        for r in (None, (base * gain[:, None] * 0.5).float()):
+            _, e = exact_norm(x, w, r, eps)
+            y = O.norm_rows(x.to(DEV), w.to(DEV), None if r is None else r.to(DEV), eps=eps)
+            check_norm(y, e, dtype, None, 0)
+
+
+@gpu
+@pytest.mark.parametrize("kind", [None, F8, I8], ids=str)
+@pytest.mark.parametrize("dim", [136, 99])
+def test_norm_rows_that_are_not_finite(kind, dim):
+    """An infinity or a NaN has its row's effect alone: an infinity leaves zeros around a NaN, 8-bit rows have no scale."""
+    x = rand(8, dim, seed=12)
+    clean = O.norm_rows(x.to(DEV), torch.ones(dim, dtype=BF, device=DEV), kind=kind)
+    x[2, 5], x[5, 77], x[6, 0] = math.inf, math.nan, -math.inf
+    y = O.norm_rows(x.to(DEV), torch.ones(dim, dtype=BF, device=DEV), kind=kind)
+    good = [0, 1, 3, 4, 7]
+    if kind is None:
+        assert torch.equal(y[good], clean[good])
+        assert y[5].isnan().all() and y[2, 5].isnan() and y[6, 0].isnan() and y[2].isnan().sum() == 1
+        return
+    assert torch.equal(y.codes[good].view(torch.uint8), clean.codes[good].view(torch.uint8))
+    assert torch.equal(y.scale[good], clean.scale[good]) and y.scale[[2, 5, 6]].isnan().all()
+    assert (y.codes.view(torch.uint8)[[2, 5, 6]] == 0).all()
+
+
+@gpu
+def test_norm_rows_of_none_and_zeros():
+    w = torch.ones(40, dtype=BF, device=DEV)
+    assert O.norm_rows(torch.empty(0, 40, dtype=BF, device=DEV), w).shape == (0, 40)
+    assert O.norm_rows(torch.empty(0, 40, dtype=BF, device=DEV), w, torch.empty(0, 40, device=DEV), kind=F8).scale.shape == (0, 1)
+    assert (O.norm_rows(torch.zeros(3, 40, dtype=BF, device=DEV), w) == 0).all()
+    assert O.norm_rows(torch.zeros(3, 40, dtype=BF, device=DEV), w, eps=0.0).isnan().all()  # 0 / 0
+
+
+# ------------------------------------------------------------ products with 4-bit weights
+def make_weights(n, k, group, zeros, dtype=BF, seed=0):
+    """Raw codes, scales and zeros on the CPU, and the weights with the magnitudes (c + z) s, in 64 bits."""
+    g = torch.Generator().manual_seed(seed)
+    groups = -(-k // group)
+    codes = torch.randint(0, 256, (n, (k + 1) // 2), generator=g).to(torch.uint8)
+    scales = ((torch.rand(n, groups, generator=g) + 0.2) * torch.sign(torch.randn(n, groups, generator=g)) * 0.05).to(dtype)
+    zero = torch.randint(0, 16, (n, groups), generator=g).to(torch.uint8) if zeros else None
+    c = torch.stack([codes & 15, codes >> 4], -1).view(n, -1)[:, :k].double()
+    at = torch.arange(k) // group
+    z = zero.double()[:, at] if zeros else 8.0
+    return codes, scales, zero, (c - z) * scales.double()[:, at], (c + z) * scales.double()[:, at].abs()
+
+
+def device_weights(codes, scales, zero, k):
+    return O.Weights4(codes.to(DEV), scales.to(DEV), None if zero is None else zero.to(DEV), k=k)
+
+
+def make_rows8(x, kind, group):
+    m, k = x.shape
+    parts = x.float().view(m, -1, group or k)
+    scale = parts.abs().amax(-1).clamp_min(1e-20) / TOP[kind]
+    codes = (parts / scale[..., None]).clamp(-TOP[kind], TOP[kind])
+    return O.Rows8((codes if kind == F8 else codes.round()).to(kind).view(m, k), scale)
+
+
+def product_bound(x, size, group):
+    return (140 + -(-size.shape[1] // group)) * 2.0 ** -23 * (x.abs() @ size.t())
+
+
+def check_product(y, x, w, size, group, dtype, gated=False):
+    """x, w and size (magnitudes) in 64 bits."""
+    e, d = x @ w.t(), product_bound(x, size, group)
+    if gated:
+        (a, b), (da, db) = e.chunk(2, 1), d.chunk(2, 1)
+        silu = a * torch.sigmoid(a)
+        e, d = silu * b, 1.1 * da * (b.abs() + db) + silu.abs() * db + 2.0 ** -20 * (silu * b).abs() + 2.0 ** -120 * b.abs()
+    assert y.dtype == dtype and y.shape == e.shape
+    off = (y.double().cpu() - e).abs()
+    bound = U[dtype] * e.abs() + (1 + U[dtype]) * d + TINY[dtype]
+    assert (off <= bound).all(), (off / bound).max()
+
+
+PRODUCTS = [  # rows, n, k, group, zeros
+    (1, 16, 128, 128, False), (1, 1, 1, 32, True), (2, 17, 31, 32, True), (5, 48, 129, 64, False), (16, 130, 640, 32, True),
+    (17, 64, 1000, 64, True), (3, 33, 2059, 128, True), (32, 96, 384, 128, False), (33, 80, 511, 64, True),
+    (64, 35, 1152, 32, False), (65, 50, 260, 64, True), (200, 112, 896, 128, True), (1, 4096, 2048, 128, False),
+    (9, 256, 9000, 64, True)]
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["rows", F8, I8], ids=str)
+@pytest.mark.parametrize("dtype", [BF, HF], ids=str)
+@pytest.mark.parametrize("case", PRODUCTS, ids=str)
+def test_product4(case, dtype, kind):
+    rows, n, k, group, zeros = case
+    codes, scales, zero, w, size = make_weights(n, k, group, zeros, HF if dtype == BF and n % 2 else dtype, seed=n)
+    W = device_weights(codes, scales, zero, k)
+    # groups of one column set: the largest that fits is what the scales' number says
+    x = rand(rows, k, seed=k, dtype=dtype)
+    x[0] *= 20
+    if kind == "rows":
+        y = O.product4(x.to(DEV), W)
+        check_product(y, x.double(), w, size, group, dtype)
+        return
+    for by_group in (False, True) if k % group == 0 else (False,):
+        r = make_rows8(x, kind, group if by_group else 0)
+        wide = r.codes.double() * r.scale.double().repeat_interleave(k // r.scale.shape[1], 1)
+        y = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W, dtype=dtype)
+        check_product(y, wide, w, size, group, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["rows", F8, I8], ids=str)
+@pytest.mark.parametrize("rows,n,k,group", [(1, 32, 128, 128), (4, 96, 300, 32), (19, 160, 640, 64), (40, 2080, 512, 128),
+                                            (70, 64, 200, 128)])
+def test_product4_gated(rows, n, k, group, kind):
+    codes, scales, zero, w, size = make_weights(n, k, group, True, seed=rows)
+    W = device_weights(codes, scales, zero, k)
+    x = rand(rows, k, seed=3)
+    x[:1] *= 100  # gates far from 0
+    if kind == "rows":
+        check_product(O.product4(x.to(DEV), W, gated=True), x.double(), w, size, group, BF, True)
+        return
+    r = make_rows8(x, kind, 0)
+    y = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W, gated=True)
+    check_product(y, r.codes.double() * r.scale.double(), w, size, group, BF, True)
+
+
+@gpu
+def test_product4_strides_and_outputs():
+    """Rows inside wider ones, at odd elements, one row for all; a given output and what lies behind it."""
+    codes, scales, zero, w, size = make_weights(50, 260, 64, True)
+    W = device_weights(codes, scales, zero, 260)
+    big = rand(21, 600, seed=4)
+    for x in (big[:, :260], big[:, 100:360], big[:, 101:361], big[:1, :260].expand(21, 260)):
+        given = big.to(DEV)[:, x.storage_offset():x.storage_offset() + 260] if x.stride(0) else x[:1].to(DEV).expand(21, 260)
+        buffer = torch.full((22 * 50,), 3.0, dtype=BF, device=DEV)
+        out = buffer[:21 * 50].view(21, 50)
+        assert O.product4(given, W, out=out) is out
+        check_product(out, x.double(), w, size, 64, BF)
+        assert (buffer[21 * 50:] == 3).all()
+        codes8 = make_rows8(x, I8, 0)
+        held = torch.zeros(21, 301, dtype=I8)
+        held[:, 3:263] = codes8.codes
+        y = O.product4(O.Rows8(held.to(DEV)[:, 3:263], codes8.scale.to(DEV)), W, dtype=HF)
+        check_product(y, codes8.codes.double() * codes8.scale.double(), w, size, 64, HF)
+    assert O.product4(torch.empty(0, 260, dtype=BF, device=DEV), W).shape == (0, 50)
+    codes, scales, zero, w, size = make_weights(40, 260, 64, True)  # half a tile of rows at the end
+    buffer = torch.full((22 * 40,), 3.0, dtype=BF, device=DEV)
+    O.product4(big[:, :260].to(DEV), device_weights(codes, scales, zero, 260), out=buffer[:21 * 40].view(21, 40))
+    check_product(buffer[:21 * 40].view(21, 40), big[:, :260].double(), w, size, 64, BF)
+    assert (buffer[21 * 40:] == 3).all()
+    odd = torch.full((21 * 64 + 1,), 3.0, dtype=BF, device=DEV)[1:].view(21, 64)  # an output at an odd element
+    codes, scales, zero, w, size = make_weights(64, 260, 64, True)
+    check_product(O.product4(big[:, :260].to(DEV), device_weights(codes, scales, zero, 260), out=odd), big[:, :260].double(),
+                  w, size, 64, BF)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["rows", F8, I8], ids=str)
+@pytest.mark.parametrize("zeros", [False, True])
+def test_product4_rows_that_are_not_finite(kind, zeros):
+    codes, scales, zero, w, size = make_weights(40, 300, 64, zeros)
+    W = device_weights(codes, scales, zero, 300)
+    x = rand(20, 300, seed=5)
+    if kind != "rows":
+        r = make_rows8(x, kind, 0)
+        clean = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W)
+        r.scale[[3, 17]] = torch.tensor([[math.nan], [math.inf]])
+        y = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W)
+        bad = [3]
+    else:
+        clean = O.product4(x.to(DEV), W)
+        x[3, 299], x[17, 0], x[11, 128] = math.inf, math.nan, -math.inf
+        y = O.product4(x.to(DEV), W)
+        bad = [3, 11, 17]
+    assert y[bad].isnan().all()
+    good = [i for i in range(20) if i not in (3, 11, 17)]
+    assert torch.equal(y[good], clean[good])
+
+
+@gpu
+def test_product4_far_magnitudes():
+    """bf16 rows near the type's largest under small scales, and near its smallest under large ones."""
+    codes, scales, zero, w, size = make_weights(32, 256, 128, True)
+    for x_gain, s_gain in ((2.0 ** 124, 2.0 ** -20), (2.0 ** -120, 2.0 ** 100)):
+        s = (scales.float() * s_gain).to(BF)
+        x = (rand(4, 256, seed=6).clamp(-4, 4).float() * x_gain).to(BF)
+        y = O.product4(x.to(DEV), device_weights(codes, s, zero, 256))
+        check_product(y, x.double(), w * s_gain, size * s_gain, 128, BF)
+
+
+def test_weights4_layout_and_quantise():
+    """Every code where the layout says, the dense weights, and the quantiser's error: half a scale, on the CPU."""
+    for n, k, group, zeros in ((40, 256, 128, True), (33, 301, 32, True), (5, 7, 128, False), (4100, 129, 64, True)):
+        codes, scales, zero, w, _ = make_weights(n, k, group, zeros)
+        W = O.Weights4(codes, scales, zero, k=k)
+        assert torch.equal(W.dense().double(), w)
+        flat = W.codes.view(W.codes.shape[0], W.codes.shape[1], 64, 4, 4)
+        for i, j in ((0, 0), (n - 1, k - 1), (n // 2, k // 2), (n - 1, k // 3), (n // 3, 5)):
+            byte = int(flat[i // 16, j // 128, (j // 8) % 4 * 16 + i % 16, (j // 32) % 4, j % 4])
+            assert (byte >> (0 if j % 8 < 4 else 4)) & 15 == (int(codes[i, j // 2]) >> (4 * (j % 2))) & 15
+            g = j // group if k > group else 0
+            assert W.scales[i // 16, g, i % 16] == scales[i, g]
+    for zeros in (False, True):
+        x = rand(50, 200, seed=7, dtype=F32) + (1.0 if zeros else 0.0)
+        x[3, 64:128] = 0
+        W = O.Weights4.quantise(x, 64, zeros=zeros, scale_dtype=HF)
+        s = W.scales.transpose(1, 2).reshape(64, -1)[:50, :4].double().repeat_interleave(64, 1)[:, :200]
+        # half a step; at the ends the scale's rounding on top: 7 or 15 steps of 2^-11, and the zero's half step
+        assert ((W.dense().double() - x.double()).abs() <= s * (0.5 + 15 * 2.0 ** -11 + (0.5 if zeros else 0)) + 1e-12).all()
+        assert (W.dense()[3, 64:128] == 0).all()
+
+
+# ------------------------------------------------------------ verification of drafted tokens
+def plain_verify(target, tokens, accept, final, draft=None, counts=None):
+    B, S = tokens.shape
+    V = target.shape[2]
+    out, accepted = torch.full((B, S + 1), -1, dtype=torch.int64), torch.zeros(B, dtype=torch.int32)
+    for b in range(B):
+        n, t = S if counts is None else int(counts[b]), 0
+        while t < n:
+            x = int(tokens[b, t])
+            if not 0 <= x < V:
+                break
+            q = 1.0 if draft is None else float(draft[b, t, x])
+            if not float(accept[b, t]) * q < float(target[b, t, x]):
+                break
+            out[b, t] = x
+            t += 1
+        p = target[b, t].double()
+        p = torch.where(p > 0, p, 0.0)
+        if t < n:
+            q = torch.zeros_like(p)
+            if draft is not None:
+                q = draft[b, t].double()
+            elif 0 <= tokens[b, t] < V:
+                q[tokens[b, t]] = 1
+            d = target[b, t].double() - q
+            d = torch.where(d > 0, d, 0.0)
+            p = d if (d > 0).any() else p
+        total = p.cumsum(0)
+        above = (total > float(final[b]) * total[-1]) & (p > 0)
+        some = above if above.any() else (p > 0)
+        if some.any():
+            out[b, t] = int(some.nonzero()[0 if above.any() else -1])
+        accepted[b] = t
+    return out, accepted
+
+
+def draws(B, S, V, dtype, drafted, seed, spread=2.0):
+    g = torch.Generator().manual_seed(seed)
+    logits = torch.randn(B, S + 1, V, generator=g) * spread
+    target = torch.softmax(logits, -1).to(dtype)
+    draft = torch.softmax(logits[:, :S] + 0.4 * torch.randn(B, S, V, generator=g), -1).to(dtype) if drafted else None
+    from_ = draft if drafted else target[:, :S]
+    tokens = torch.multinomial(from_.float().reshape(-1, V), 1, generator=g).view(B, S) if S else torch.zeros(B, 0, dtype=torch.int64)
+    return target, tokens, torch.rand(B, S, generator=g), torch.rand(B, generator=g), draft
+
+
+def run_verify(target, tokens, accept, final, draft=None, counts=None, status=None):
+    to = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    return O.verify_drafts(to(target), to(tokens), to(accept), to(final), draft=to(draft), counts=to(counts), status=status)
+
+
+def check_verify(*args):
+    tokens, accepted = run_verify(*args)
+    want, count = plain_verify(*args)
+    assert torch.equal(accepted.cpu(), count)
+    assert torch.equal(tokens.cpu(), want)
+    return count
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF, HF], ids=str)
+@pytest.mark.parametrize("drafted", [True, False])
+@pytest.mark.parametrize("B,S,V", [(1, 1, 1), (3, 4, 7), (1, 0, 100), (5, 2, 2047), (4, 3, 2049), (2, 70, 300), (7, 5, 32_001),
+                                   (200, 3, 5000), (1, 2, 151_936)])
+def test_verify_drafts(B, S, V, drafted, dtype):
+    counts = set()
+    for seed in range(3):
+        a = draws(B, S, V, dtype, drafted, seed, 6.0 if not drafted else 2.0)
+        counts |= set(check_verify(*a).tolist())
+        if S:
+            n = torch.randint(0, S + 1, (B,), generator=torch.Generator().manual_seed(seed), dtype=torch.int32)
+            check_verify(*a, n)
+    assert len(counts) > 1 or B < 4 or S == 0
+
+
+@gpu
+def test_verify_drafts_at_the_borders():
+    """Whole cumulative sums: random numbers at a border go to the next token that has a part; an acceptance test at
+    equality is none; a probability of 0 is never accepted, and one above the draft's always."""
+    V = 4096
+    target = torch.zeros(6, 2, V)
+    target[:, :, 1000], target[:, :, 3000], target[:, :, 4095] = 0.25, 0.25, 0.5
+    draft = torch.zeros(6, 1, V)
+    draft[:, :, 1000], draft[:, :, 7] = 0.5, 0.5
+    tokens = torch.tensor([[1000], [1000], [7], [7], [1000], [1000]])
+    accept = torch.tensor([[0.5], [0.4999], [0.0], [0.9], [0.6], [0.6]])
+    final = torch.tensor([0.0, 0.25, 0.3333, 0.0, 0.3334, 0.9999])
+    tokens_out, accepted = run_verify(target, tokens, accept, final, draft)
+    # row 1 is accepted and draws behind it: 0.25 is the whole part of token 1000
+    assert accepted.tolist() == [0, 1, 0, 0, 0, 0]
+    assert tokens_out.tolist() == [[3000, -1], [1000, 3000], [3000, -1], [3000, -1], [4095, -1], [4095, -1]]
+    check_verify(target, tokens, accept, final, draft)
+
+
+@gpu
+def test_verify_drafts_where_nothing_is_left():
+    """A draft never above the target leaves no difference: the target is drawn from; without anything above 0 the
+    token is -1, and reported.  Numbers not below 1, NaN and infinities choose something that has a part."""
+    V = 5000
+    target, draft = torch.zeros(5, 2, V), torch.zeros(5, 1, V)
+    target[:, :, 10:20] = 0.1
+    draft[:] = target[:, :1]
+    draft[:, :, 4999] = 0.3  # the draft's own token, which the target has nothing of
+    tokens, accept = torch.full((5, 1), 4999), torch.full((5, 1), 0.5)
+    final = torch.tensor([0.0, 0.55, 1.0, 0.2, math.nan])
+    target[3] = 0
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, accepted = run_verify(target, tokens, accept, final, draft, status=status)
+    assert accepted.tolist() == [0] * 5 and out[:, 1].tolist() == [-1] * 5
+    assert out[:, 0].tolist() == [10, 15, 19, -1, 19]
+    assert status.item() == O.BAD_ROW
+    with pytest.raises(ValueError, match="above 0"):
+        O.raise_faults(status)
+    target[:, :, 30], target[:, :, 31] = math.nan, math.nan
+    assert run_verify(target, tokens, accept, final, draft)[0][:3, 0].tolist() == [10, 15, 19]
+
+
+@gpu
+@pytest.mark.parametrize("drafted", [True, False])
+def test_verify_drafts_faults(drafted):
+    """Tokens outside the vocabulary and counts out of range touch nothing out of range, and are reported."""
+    a = list(draws(4, 3, 600, F32, drafted, 3))
+    a[1][1, 0], a[1][2, 1] = 600, -1
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, accepted = run_verify(*a, status=status)
+    want, count = plain_verify(*a)
+    assert torch.equal(out.cpu(), want) and torch.equal(accepted.cpu(), count) and count[1] == 0 and count[2] <= 1
+    assert status.item() == O.BAD_TOKEN
+    with pytest.raises(ValueError, match="outside the vocabulary"):
+        O.raise_faults(status)
+    a = draws(4, 3, 600, F32, drafted, 4)
+    n = torch.tensor([-5, 3, 2 ** 31 - 1, 0], dtype=torch.int32)
+    out, accepted = run_verify(*a, n, status=status)
+    want, count = plain_verify(*a, n.clamp(0, 3))
+    assert torch.equal(out.cpu(), want) and torch.equal(accepted.cpu(), count)
+    assert status.item() == O.BAD_LENGTH
+
+
+@gpu
+def test_verify_drafts_strides():
+    """Probabilities inside wider rows, one target row for all sequences, and none at all."""
+    target, tokens, accept, final, draft = draws(3, 2, 700, BF, True, 5)
+    wide = torch.zeros(3, 4, 900, dtype=BF)
+    wide[:, 1:, 33:733] = target
+    wide2 = torch.zeros(2, 3, 701, dtype=BF)
+    wide2[:, :, 1:] = draft.transpose(0, 1)
+    want = plain_verify(target, tokens, accept, final, draft)
+    got = O.verify_drafts(wide.to(DEV)[:, 1:, 33:733], tokens.to(DEV), accept.to(DEV), final.to(DEV),
+                          draft=wide2.to(DEV)[:, :, 1:].transpose(0, 1))
+    assert torch.equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+    one = target[:1, :1].expand(3, 3, 700)
+    got = O.verify_drafts(target.to(DEV)[:1, :1].expand(3, 3, 700), tokens.to(DEV), accept.to(DEV), final.to(DEV))
+    want = plain_verify(one, tokens, accept, final)
+    assert torch.equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+    none = [t[:0].to(DEV) for t in (target, tokens, accept, final)]
+    assert [t.shape for t in O.verify_drafts(*none)] == [(0, 3), (0,)]
+
+
+# ------------------------------------------------------------ all of them
+@gpu
+def test_offsets_beyond_32_bits():
+    """Rows that lie further apart than 32 bits count: of the norm, of a product and of probabilities."""
+    x = torch.empty(9, 2 ** 28 + 8, dtype=BF, device=DEV)  # 4.8 GB
+    few = rand(9, 256, seed=1)
+    x[:, 64:320] = few.to(DEV)
+    w = rand(256, seed=2)
+    check_norm(O.norm_rows(x[:, 64:320], w.to(DEV)), exact_norm(few, w, None, 1e-6)[1], BF, None, 0)
+    residual = torch.zeros_like(few, device=DEV)
+    kept = x[:, 1024:1280]
+    y = O.norm_rows(few.to(DEV), w.to(DEV), residual, residual_out=kept)
+    assert torch.equal(kept.cpu(), few) and torch.equal(y, O.norm_rows(few.to(DEV), w.to(DEV)))
+    codes, scales, zero, dense, size = make_weights(32, 256, 128, True)
+    check_product(O.product4(x[:, 64:320], device_weights(codes, scales, zero, 256)), few.double(), dense, size, 128, BF)
+    a = draws(3, 2, 500, BF, True, 7)
+    p = x[:, :500].view(3, 3, 500)
+    p.copy_(a[0])
+    got, want = O.verify_drafts(p, *(t.to(DEV) for t in a[1:4]), draft=a[4].to(DEV)), plain_verify(*a)
+    assert torch.equal(got[0].cpu(), want[0]) and torch.equal(got[1].cpu(), want[1])
+
+
+def chain(x, residual, w, W, target, tokens, accept, final, draft):
+    y = O.product4(O.norm_rows(x, w, residual, kind=F8, residual_out=torch.empty_like(residual)), W, gated=True)
+    z = O.norm_rows(y, w[:y.shape[1]])
+    return (y, z) + O.verify_drafts(target, tokens, accept, final, draft=draft)
+
+
+@gpu
+def test_in_graphs_and_on_another_stream():
+    """A captured run of the operators follows its inputs, two graphs replay beside each other and beside eager calls."""
+    codes, scales, zero, _, _ = make_weights(512, 256, 64, True)
+    W = device_weights(codes, scales, zero, 256)
+
+    def inputs(seed):
+        a = draws(6, 3, 9000, F32, True, seed)
+        return [t.to(DEV) for t in (rand(12, 256, seed=seed), rand(12, 256, seed=seed + 50, dtype=F32), rand(256, seed=seed + 90),
+                                    a[0], a[1], a[2], a[3], a[4])]
+    sets = [inputs(0), inputs(1)]
+
+    def go(s):
+        return chain(s[0], s[1], s[2], W, *s[3:])
+    go(sets[0])
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for s in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(go(s))
+    side = [torch.cuda.Stream() for _ in sets]
+    for step in range(4):
+        for i, s in enumerate(sets):
+            for old, new in zip(s, inputs(10 + 2 * step + i)):
+                old.copy_(new)
+        torch.cuda.synchronize()
+        want = [go(s) for s in sets]
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, side):
+            with torch.cuda.stream(st):
+                g.replay()
+        again = go(sets[0])
+        torch.cuda.synchronize()
+        for got, ref in ((outs[0], want[0]), (outs[1], want[1]), (again, want[0])):
+            assert all(torch.equal(u, v) for u, v in zip(got, ref))
+
+
+@gpu
+def test_results_do_not_vary():
+    codes, scales, zero, _, _ = make_weights(300, 4096, 128, True)
+    W = device_weights(codes, scales, zero, 4096)
+    x, w = rand(20, 4096).to(DEV), rand(4096, seed=1).to(DEV)
+    first = O.norm_rows(x, w, kind=I8), O.product4(x, W)
+    for _ in range(3):
+        r = O.norm_rows(x, w, kind=I8)
+        assert torch.equal(r.codes, first[0].codes) and torch.equal(r.scale, first[0].scale)
+        assert torch.equal(O.product4(x, W), first[1])
+
+
+# ------------------------------------------------------------ refusals
+def norm_args(**kw):
+    a = dict(x=FAKE, x_row=64, weight=FAKE, out=FAKE, n_rows=4, dim=64, type=O.BF16, weight_type=O.BF16, out_kind=O.BF16,
+             eps=1e-6)
+    return O.HerschelNormArgs(**{**a, **kw})
+
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(weight=None), dict(out=None), dict(x=FAKE + 1), dict(out=FAKE + 1), dict(n_rows=-1),
+    dict(n_rows=1 << 31), dict(dim=0), dict(dim=32_769), dict(x_row=-1), dict(type=O.F32), dict(type=O.INT8),
+    dict(weight_type=O.F16), dict(weight_type=O.F32, weight=FAKE + 2), dict(out_kind=O.F16), dict(out_kind=O.F32),
+    dict(out_kind=O.FP8), dict(out_kind=O.INT8, scale=FAKE + 2), dict(out_kind=5), dict(group=32),
+    dict(out_kind=O.FP8, scale=FAKE, group=48), dict(out_kind=O.FP8, scale=FAKE, group=128), dict(eps=-1e-9),
+    dict(eps=math.nan), dict(eps=math.inf), dict(residual_out=FAKE, residual_out_row=64),
+    dict(residual=FAKE, residual_row=64, residual_type=O.F16), dict(residual=FAKE, residual_row=-1),
+    dict(residual=FAKE + 2, residual_row=64, residual_type=O.F32),
+    dict(residual=FAKE, residual_row=64, residual_out=FAKE, residual_out_row=63)], ids=named)
+def test_bad_norm_calls_are_refused(bad):
+    assert lib().herschel_norm_rows(ctypes.byref(norm_args(**bad))) == H.EINVAL
+
+
+def weights_struct(**kw):
+    a = dict(codes=FAKE, scales=FAKE, zeros=None, n=64, k=256, group=128, scale_type=O.BF16)
+    return O.HerschelWeights4(**{**a, **kw})
+
+
+def product_args(**kw):
+    a = dict(x=FAKE, x_row=256, out=FAKE, n_rows=4, kind=O.BF16, type=O.BF16)
+    return O.HerschelProductArgs(**{**a, **kw})
+
+
+@pytest.mark.parametrize("bad,weights", [
+    (dict(x=None), {}), (dict(out=None), {}), (dict(x=FAKE + 1), {}), (dict(out=FAKE + 1), {}), (dict(n_rows=-1), {}),
+    (dict(n_rows=1 << 40), {}), (dict(x_row=-1), {}), (dict(kind=O.F16), {}), (dict(kind=O.F32, type=O.F32), {}),
+    (dict(kind=O.INT8), {}), (dict(kind=O.INT8, x_scale=FAKE + 2), {}), (dict(x_group=128), {}),
+    (dict(kind=O.FP8, x_scale=FAKE, x_group=64), {}), (dict(gated=1), dict(n=48)), ({}, dict(codes=None)),
+    ({}, dict(scales=None)), ({}, dict(codes=FAKE + 8)), ({}, dict(zeros=FAKE + 4)), ({}, dict(n=0)), ({}, dict(k=0)),
+    ({}, dict(k=0x7fffff80)), ({}, dict(group=16)), ({}, dict(group=256)), ({}, dict(scale_type=O.F32))], ids=str)
+def test_bad_product_calls_are_refused(bad, weights):
+    assert lib().herschel_product4(ctypes.byref(product_args(**bad)), ctypes.byref(weights_struct(**weights))) == H.EINVAL
+
+
+def verify_args(**kw):
+    a = dict(target=FAKE, target_seq=3000, target_row=1000, draft=FAKE, draft_seq=2000, draft_row=1000, tokens=FAKE,
+             counts=FAKE, accept_u=FAKE, final_u=FAKE, out=FAKE, accepted=FAKE, n_seqs=3, n_drafts=2, vocab=1000, type=O.F32,
+             workspace=FAKE, workspace_bytes=1 << 30)
+    return O.HerschelVerifyArgs(**{**a, **kw})
+
+
+@pytest.mark.parametrize("bad,code", [
+    (dict(target=None), H.EINVAL), (dict(target=FAKE + 2), H.EINVAL), (dict(draft=FAKE + 2), H.EINVAL),
+    (dict(tokens=None), H.EINVAL), (dict(accept_u=None), H.EINVAL), (dict(final_u=None), H.EINVAL), (dict(out=None), H.EINVAL),
+    (dict(accepted=None), H.EINVAL), (dict(n_seqs=-1), H.EINVAL), (dict(n_seqs=65_536), H.EINVAL), (dict(n_drafts=-1), H.EINVAL),
+    (dict(n_drafts=1025), H.EINVAL), (dict(vocab=0), H.EINVAL), (dict(vocab=(1 << 30) + 1), H.EINVAL), (dict(type=O.FP8), H.EINVAL),
+    (dict(target_seq=-1), H.EINVAL), (dict(draft_row=-1), H.EINVAL), (dict(workspace=None), H.EWORKSPACE),
+    (dict(workspace=FAKE + 8), H.EWORKSPACE), (dict(workspace_bytes=8), H.EWORKSPACE)], ids=named)
+def test_bad_verify_calls_are_refused(bad, code):
+    assert lib().herschel_verify_drafts(ctypes.byref(verify_args(**bad))) == code
+
+
+def test_null_and_empty_calls():
+    L, none = lib(), None
+    assert L.herschel_norm_rows(none) == L.herschel_product4(none, none) == L.herschel_verify_drafts(none) == H.EINVAL
+    assert L.herschel_product4(ctypes.byref(product_args()), none) == H.EINVAL
+    assert L.herschel_verify_workspace(1, 10, none) == H.EINVAL
+    # nothing to do, nothing to point at
+    assert L.herschel_norm_rows(ctypes.byref(norm_args(n_rows=0, x=None, weight=None, out=None))) == H.OK
+    assert L.herschel_product4(ctypes.byref(product_args(n_rows=0, x=None, out=None)), ctypes.byref(weights_struct())) == H.OK
+    assert L.herschel_verify_drafts(ctypes.byref(verify_args(n_seqs=0, target=None, workspace=None))) == H.OK
+
+
+def test_struct_layouts_match_the_header(tmp_path):
+    """The binding's structures and the packed forms that calls are made with, against the header's."""
+    import os
+    import subprocess
+    structs = {"herschel_norm_args": (O.HerschelNormArgs, O._NORM), "herschel_weights4": (O.HerschelWeights4, None),
+               "herschel_product_args": (O.HerschelProductArgs, O._PRODUCT), "herschel_verify_args": (O.HerschelVerifyArgs, O._VERIFY)}
+    lines = ['#include <stddef.h>', '#include <stdio.h>', '#include "herschel_ops.h"', "int main(void) {"]
+    for c, (cls, _) in structs.items():
+        lines.append(f'  printf("{c} %zu\\n", sizeof({c}));')
+        lines += [f'  printf("{c}.{f} %zu\\n", offsetof({c}, {f}));' for f, _ in cls._fields_]
+    (tmp_path / "layout.c").write_text("\n".join(lines + ["  return 0;", "}"]) + "\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    subprocess.run(["gcc", "-std=c11", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "layout"),
+                    str(tmp_path / "layout.c")], check=True)
+    got = dict(line.rsplit(" ", 1) for line in subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True,
+                                                             text=True).stdout.splitlines())
+    for c, (cls, packed) in structs.items():
+        assert int(got[c]) == ctypes.sizeof(cls)
+        for f, _ in cls._fields_:
+            assert int(got[f"{c}.{f}"]) == getattr(cls, f).offset, f
+        if packed is None:
+            continue
+        assert packed.size == ctypes.sizeof(cls)
+        numbers = list(range(1, len(cls._fields_) + 1))
+        read = cls.from_buffer_copy(packed.pack(*numbers))
+        assert [getattr(read, f) for f, _ in cls._fields_] == numbers
+
+
+def test_tensor_checks_on_the_cpu():
+    x, w = rand(4, 64), rand(64)
+    with pytest.raises(ValueError, match="GPU"):
+        O.norm_rows(x, w)
+    with pytest.raises(ValueError, match="GPU"):
+        O.product4(x, O.Weights4.quantise(rand(16, 64)))
+    with pytest.raises(ValueError, match="GPU"):
+        O.verify_drafts(*draws(1, 1, 10, F32, False, 0)[:4])
+    codes, scales = torch.zeros(16, 64, dtype=torch.uint8), torch.ones(16, 1, dtype=BF)
+    for bad in (dict(codes=codes.int()), dict(codes=codes[0]), dict(k=130), dict(k=126), dict(scales=scales.float()),
+                dict(scales=scales[:8]), dict(scales=torch.ones(16, 3, dtype=BF)), dict(zeros=torch.zeros(16, 1)),
+                dict(zeros=torch.zeros(8, 1, dtype=torch.uint8)), dict(zeros=torch.full((16, 1), 16, dtype=torch.uint8))):
+        a = {**dict(codes=codes, scales=scales, zeros=None, k=None), **bad}
+        with pytest.raises(ValueError):
+            O.Weights4(a["codes"], a["scales"], a["zeros"], k=a["k"])
+    for bad in (dict(group=16), dict(scale_dtype=F32)):
+        with pytest.raises(ValueError):
+            O.Weights4.quantise(rand(16, 64), **bad)
+    with pytest.raises(ValueError):
+        O.Weights4.quantise(torch.zeros(16, 64, dtype=torch.int32))
+
+
+@gpu
+def test_tensor_checks():
+    x, w, r = rand(4, 64).to(DEV), rand(64).to(DEV), torch.zeros(4, 64, device=DEV)
+    for bad, match in ((dict(x=x.float()), "bfloat16 or float16"), (dict(x=x[0]), "2 dimensions"), (dict(x=x.t()), "contiguous"),
+                       (dict(weight=w.half()), "weight"), (dict(weight=w[:32]), "weight"), (dict(weight=w.cpu()), "weight"),
+                       (dict(eps=-1.0), "eps"), (dict(eps=math.nan), "eps"), (dict(group=32), "group"),
+                       (dict(kind=I8, group=48), "group"), (dict(kind=I8, group=128), "group"), (dict(kind=torch.uint8), "kind"),
+                       (dict(kind=BF), "kind"), (dict(residual=r[:3]), "residual"), (dict(residual=r.half()), "residual"),
+                       (dict(residual=r.cpu()), "residual"), (dict(residual_out=r), "residual"),
+                       (dict(residual=r, residual_out=r.to(BF)), "residual_out"), (dict(out=torch.empty_like(r)), "out"),
+                       (dict(residual=r, residual_out=r[:1].expand(4, 64)), "overlap"), (dict(out=x[:3]), "out"),
+                       (dict(kind=F8, out=O.Rows8(x.to(I8), r[:, :1].contiguous())), "codes"),
+                       (dict(x=torch.zeros(1, 32_769, dtype=BF, device=DEV)), "columns"), (dict(x=x[:, :0]), "columns")):
+        with pytest.raises(ValueError, match=match):
+            O.norm_rows(**{**dict(x=x, weight=w), **bad})
+    W = O.Weights4.quantise(rand(48, 64).to(DEV), 32)
+    r8 = O.norm_rows(x, w, kind=I8)
+    for bad, match in ((dict(x=x.float()), "bfloat16"), (dict(x=x[0]), "2 dimensions"), (dict(x=x[:, :32]), "shape"),
+                       (dict(x=x.cpu()), "GPU"), (dict(dtype=HF), "dtype"), (dict(gated=True), "32"), (dict(out=x), "out"),
+                       (dict(x=O.Rows8(r8.codes, r8.scale[:, 0])), "scale"), (dict(x=O.Rows8(r8.codes, r8.scale[:3])), "scale"),
+                       (dict(x=O.Rows8(r8.codes, torch.ones(4, 4, device=DEV))), "scale"), (dict(x=r8, dtype=F32), "dtype"),
+                       (dict(x=O.Rows8(x, r8.scale)), "8 bits"), (dict(weights=O.Weights4.quantise(rand(48, 64), 32)), "device")):
+        with pytest.raises(ValueError, match=match):
+            O.product4(**{**dict(x=x, weights=W), **bad})
+    t, k, a, f, d = (v.to(DEV) for v in draws(2, 2, 50, F32, True, 0))
+    n = torch.ones(2, dtype=torch.int32, device=DEV)
+    for bad, match in ((dict(target=t.double()), "float32"), (dict(target=t[0]), "drafts"), (dict(target=t.transpose(1, 2)), "contiguous"),
+                       (dict(target=t[:, :2]), "tokens"), (dict(tokens=k.int()), "tokens"), (dict(tokens=k[:1]), "tokens"),
+                       (dict(accept=a.half()), "accept"), (dict(accept=a[:, :1]), "accept"), (dict(final=f[:1]), "final"),
+                       (dict(draft=d.half()), "draft"), (dict(draft=d[:, :1]), "draft"), (dict(draft=d.cpu()), "draft"),
+                       (dict(counts=n.long()), "counts"), (dict(counts=n[:1]), "counts"), (dict(status=n), "status"),
+                       (dict(target=t[:, :, :0]), "vocab")):
+        z = {**dict(target=t, tokens=k, accept=a, final=f, draft=d, counts=None, status=None), **bad}
+        with pytest.raises(ValueError, match=match):
+            O.verify_drafts(z["target"], z["tokens"], z["accept"], z["final"], draft=z["draft"], counts=z["counts"], status=z["status"])
+
+
+@gpu
+def test_gradients_are_refused_and_writes_are_seen():
+    x, w, r = rand(4, 64).to(DEV), rand(64).to(DEV), torch.zeros(4, 64, device=DEV)
+    W = O.Weights4.quantise(rand(48, 64).to(DEV), 32)
+    leaf = x.clone().requires_grad_()
+    a = [t.to(DEV) for t in draws(2, 2, 50, F32, False, 0)[:4]]
+    for call in (lambda: O.norm_rows(leaf, w), lambda: O.norm_rows(x, w.clone().requires_grad_()), lambda: O.product4(leaf, W),
+                 lambda: O.norm_rows(x, w, r.clone().requires_grad_()),
+                 lambda: O.verify_drafts(a[0].clone().requires_grad_(), *a[1:])):
+        with pytest.raises(ValueError, match="no backward"):
+            call()
+        with torch.no_grad():
+            call()
+    out = torch.empty(4, 48, dtype=BF, device=DEV)
+    before = r._version, out._version
+    O.norm_rows(x, w, r)
+    O.product4(x, W, out=out)
+    assert r._version > before[0] and out._version > before[1]
