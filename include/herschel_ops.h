@@ -226,17 +226,18 @@ int herschel_norm_rows(const herschel_norm_args *args);
 
 /* A matrix [n][k] of 4-bit codes c, each worth (c - zero) * scale with the zero
  * and scale of its row's group of `group` columns.  Rows are held in tiles of 16,
- * columns in tiles of 128, both filled up with codes, scales and zeros of 0:
- *   codes[n / 16][k / 128][(k / 8) % 4 * 16 + n % 16][(k / 32) % 4][k % 4], bytes,
- *     column k in the low half of its byte if k % 8 < 4, else in the high half;
- *   scales and zeros[n / 16][groups, those of the filled columns][n % 16]. */
+ * columns in tiles of 128, both filled up with codes, scales and zeros of 0.  A
+ * scale is a 32-bit float of at most 16 significant bits: a word holds its upper
+ * 24 bits, and in its low 8 the zero, 0 ... 15 (8 where the weights have none).  Of
+ * column k in its tile, g = k / group, f = k % group, r = group / 4:
+ *   codes[tile][n / 16][f / r][n % 16][g * r / 8 + f % r / 8][k % 4], bytes, the
+ *     column in the low half of its byte if k % 8 < 4, else in the high half;
+ *   scales[tile][n / 16][n % 16 / 4][g][n % 4], words. */
 typedef struct {
   const void *codes;          /* 16-byte aligned */
-  const void *scales;         /* of scale_type, 16-byte aligned */
-  const uint8_t *zeros;       /* each 0 ... 15, 16-byte aligned; NULL: every zero is 8 */
+  const uint32_t *scales;     /* 16-byte aligned */
   int32_t n, k;               /* >= 1 */
   int32_t group;              /* 32, 64 or 128; the last of a row may be shorter */
-  int32_t scale_type;         /* HERSCHEL_BF16 or HERSCHEL_F16 */
 } herschel_weights4;
 
 typedef struct {
@@ -249,8 +250,13 @@ typedef struct {
   int32_t x_group;            /* 8 bits: 0 or the weights' group */
   int32_t type;               /* HERSCHEL_BF16 or HERSCHEL_F16; that of rows of 16 bits */
   int32_t gated;              /* n a multiple of 32: y = silu(a) b, a the first n / 2 columns of the product, b the others */
+  void *workspace;            /* herschel_product4_workspace() bytes, 16-byte aligned, no two calls at once; or NULL or */
+  size_t workspace_bytes;     /* fewer bytes: a product's columns are then not shared among more workgroups */
   void *hip_stream;
 } herschel_product_args;
+
+/* Bytes of workspace with which a call of these sizes is fastest; 0 for most. */
+int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t gated, int32_t n, int32_t k, size_t *bytes);
 
 /* out[m] = sum over k of x[m][k] * weight[n][k], codes summed within a group
  * before they meet its scale, in 32 bits (int8 rows: whole numbers), rounded

@@ -158,12 +158,6 @@ __device__ __forceinline__ float* row_part(const herschel_prompt_args& a, int pa
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 LdsHalves;
 
-// A wave's copy of 64 chunks of 16 bytes from global memory to consecutive LDS.
-__device__ __forceinline__ void copy_to_lds(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
-}
-
 // Orders N products and their READS LDS reads each: AHEAD products' reads
 // first, then one product and the reads of a later one in turn.  Left alone, the
 // compiler waits for each read just before its product: 60 cycles of 32.

@@ -201,6 +201,12 @@ __device__ __forceinline__ float log_sum(float ref, float sum) {
          0.69314718055994530942f;
 }
 
+// A wave's copy of 64 chunks of 16 bytes from global memory to consecutive LDS.
+__device__ __forceinline__ void copy_to_lds(const void* from, void* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
 // 16 bytes that may lie at any element (2 bytes).
 __device__ __forceinline__ u32x4 load_elements(const uint16_t* p) {
   u32x4 r;

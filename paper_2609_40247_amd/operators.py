@@ -92,13 +92,13 @@ class HerschelNormArgs(ctypes.Structure):
 
 
 class HerschelWeights4(ctypes.Structure):
-    _fields_ = [("codes", _P), ("scales", _P), ("zeros", _P), ("n", _I32), ("k", _I32), ("group", _I32),
-                ("scale_type", _I32)]
+    _fields_ = [("codes", _P), ("scales", _P), ("n", _I32), ("k", _I32), ("group", _I32)]
 
 
 class HerschelProductArgs(ctypes.Structure):
     _fields_ = [("x", _P), ("x_row", _I64), ("x_scale", _P), ("out", _P), ("n_rows", _I64), ("kind", _I32),
-                ("x_group", _I32), ("type", _I32), ("gated", _I32), ("hip_stream", _P)]
+                ("x_group", _I32), ("type", _I32), ("gated", _I32), ("workspace", _P), ("workspace_bytes", ctypes.c_size_t),
+                ("hip_stream", _P)]
 
 
 class HerschelVerifyArgs(ctypes.Structure):
@@ -115,7 +115,7 @@ _READ = struct.Struct("@PqPiq2Pi2P")
 _PROMPT = struct.Struct("@3P6q4Pi2q7ifPN2P")
 _DECODE = struct.Struct("@P3q3PqP5ifPN2P")
 _NORM = struct.Struct("@PqPqPq3Pq6ifP")
-_PRODUCT = struct.Struct("@Pq2Pq4iP")
+_PRODUCT = struct.Struct("@Pq2Pq4iPNP")
 _VERIFY = struct.Struct("@P2qP2q6P4iPN2P")
 
 _ready = {}
@@ -136,6 +136,8 @@ def load(variant: str | None = None) -> ctypes.CDLL:
                                                        ctypes.POINTER(ctypes.c_size_t)]
         lib.herschel_attn_decode_workspace.restype = ctypes.c_int
         lib.herschel_attn_decode_workspace.argtypes = [_I32, _I32, _I32, _P, ctypes.POINTER(ctypes.c_size_t)]
+        lib.herschel_product4_workspace.restype = ctypes.c_int
+        lib.herschel_product4_workspace.argtypes = [_I64, _I32, _I32, _I32, _I32, ctypes.POINTER(ctypes.c_size_t)]
         lib.herschel_verify_workspace.restype = ctypes.c_int
         lib.herschel_verify_workspace.argtypes = [_I32, _I32, ctypes.POINTER(ctypes.c_size_t)]
         if variant:
@@ -680,27 +682,23 @@ class Weights4:
             _need(int(zeros.max()) <= 15, "zeros must be 0 to 15")
         self.n, self.k, self.group, self.groups, self.device = n, k, group, scales.shape[1], codes.device
         tiles_n, tiles_k = -(-n // 16), -(-k // 128)
-        self.codes = codes.new_empty((tiles_n, tiles_k, 4, 16, 4, 4))
+        self.codes = codes.new_empty((tiles_k, tiles_n, 4, 16, 4, 4))
         for at in range(0, tiles_n, 256):  # 4096 rows at a time, so that no copy of a byte a weight is made of them all
             part = codes[at * 16:(at + 256) * 16]
             wide = codes.new_zeros((-(-part.shape[0] // 16) * 16, tiles_k * 128))
             wide[:part.shape[0], 0:k:2] = part & 15
             wide[:part.shape[0], 1:k:2] = part[:, :k // 2] >> 4
-            # rows of a tile, its columns as 4 words' 4 lanes' halves of 4 bytes
-            wide = wide.view(-1, 16, tiles_k, 4, 4, 2, 4)
+            # rows of a tile, its columns as groups of 4 lanes' words, each two halves of 4 bytes
+            wide = wide.view(-1, 16, tiles_k, 128 // group, 4, group // 32, 2, 4)
             packed = wide[..., 0, :] | (wide[..., 1, :] << 4)
-            self.codes[at:at + 256] = packed.permute(0, 2, 4, 1, 3, 5)
-        self.scales, self.zeros = self._tile(scales), None if zeros is None else self._tile(zeros)
-        self.struct = HerschelWeights4(self.codes.data_ptr(), self.scales.data_ptr(),
-                                       None if zeros is None else self.zeros.data_ptr(), n, k, group, TYPES[scales.dtype])
+            self.codes[:, at:at + 256] = packed.permute(2, 0, 4, 1, 3, 5, 6).reshape(tiles_k, -1, 4, 16, 4, 4)
+        # a scale and its zero in a word; bfloat16 and half have no more than the 24 upper bits of a 32-bit float
+        words = (scales.float().view(torch.int32) & -256) | (8 if zeros is None else zeros.to(torch.int32))
+        wide = words.new_zeros((tiles_n * 16, tiles_k * (128 // group)))
+        wide[:n, :self.groups] = words
+        self.scales = wide.view(tiles_n, 4, 4, tiles_k, 128 // group).permute(3, 0, 1, 4, 2).contiguous()
+        self.struct = HerschelWeights4(self.codes.data_ptr(), self.scales.data_ptr(), n, k, group)
         self._at, self._device = ctypes.addressof(self.struct), codes.get_device()
-
-    def _tile(self, t: torch.Tensor) -> torch.Tensor:
-        """[n, groups] as [tiles of 16 rows, groups of the filled up columns, 16]."""
-        tiles, groups = -(-self.n // 16), -(-self.k // 128) * (128 // self.group)
-        wide = t.new_zeros((tiles * 16, groups))
-        wide[:self.n, :self.groups] = t
-        return wide.view(tiles, 16, groups).transpose(1, 2).contiguous()
 
     @classmethod
     def quantise(cls, weights: torch.Tensor, group: int = 128, *, zeros: bool = False, scale_dtype=None):
@@ -735,14 +733,20 @@ class Weights4:
 
     def dense(self) -> torch.Tensor:
         """The weights [n, k] in 32 bits."""
-        tiles_n, tiles_k = self.codes.shape[:2]
-        b = self.codes.permute(0, 3, 1, 4, 2, 5)  # row, tile, word, lane, byte
-        c = torch.stack([b & 15, b >> 4], -2).reshape(tiles_n * 16, tiles_k, 128 // self.group, self.group).float()
-
-        def wide(t):
-            return t.transpose(1, 2).reshape(tiles_n * 16, tiles_k, -1, 1).float()
-        c = (c - (8.0 if self.zeros is None else wide(self.zeros))) * wide(self.scales)
+        tiles_k, tiles_n, per = *self.codes.shape[:2], 128 // self.group
+        b = self.codes.view(tiles_k, tiles_n, 4, 16, per, self.group // 32, 4).permute(1, 3, 0, 4, 2, 5, 6)
+        c = torch.stack([b & 15, b >> 4], -2).reshape(tiles_n * 16, tiles_k * per, self.group).float()
+        words = self.scales.permute(1, 2, 4, 0, 3).reshape(tiles_n * 16, tiles_k * per, 1)
+        c = (c - (words & 255)) * (words & -256).view(torch.float32)
         return c.view(tiles_n * 16, -1)[:self.n, :self.k].contiguous()
+
+
+@functools.lru_cache(maxsize=1024)
+def _product_workspace(lib, *sizes) -> int:
+    """Bytes of workspace for a call of these sizes (0: none)."""
+    size = ctypes.c_size_t(0)
+    lib.herschel_product4_workspace(*sizes, ctypes.byref(size))
+    return int(size.value)
 
 
 def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False, dtype: torch.dtype | None = None,
@@ -788,8 +792,12 @@ def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False,
         to = out.data_ptr()
     else:
         to = _ints(out, "out", dtype, shape, dev)
-    args = _PRODUCT.pack(t.data_ptr(), stride, scales, to, n, kind, x_group, TYPES[dtype], bool(gated), _stream(dev))
-    _call((lib or _lib()).herschel_product4, dev, "product4", args, weights._at)
+    lib = lib or _lib()
+    size = _product_workspace(lib, n, kind, bool(gated), weights.n, weights.k)
+    workspace = t.new_empty(size, dtype=torch.uint8) if size else None
+    args = _PRODUCT.pack(t.data_ptr(), stride, scales, to, n, kind, x_group, TYPES[dtype], bool(gated),
+                         workspace.data_ptr() if size else 0, size, _stream(dev))
+    _call(lib.herschel_product4, dev, "product4", args, weights._at)
     if given is not None:
         _written((given,))
     return out

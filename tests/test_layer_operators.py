@@ -266,6 +266,69 @@ def test_product4_gated(rows, n, k, group, kind):
     check_product(y, r.codes.double() * r.scale.double(), w, size, group, BF, True)
 
 
+# long columns of few weight rows: shared among workgroups, in two to four parts
+SHARED = [(1, 16, 33_000, 128, False, "rows"), (3, 70, 20_011, 64, True, "rows"), (20, 40, 16_400, 32, True, "rows"),
+          (64, 96, 12_800, 128, True, F8), (40, 130, 15_000, 64, False, I8), (16, 48, 25_600, 32, True, I8)]
+
+
+def product_splits(rows, kind, gated, n, k):
+    code = {"rows": O.BF16, F8: O.FP8, I8: O.INT8}[kind]
+    size = ctypes.c_size_t(0)
+    assert lib().herschel_product4_workspace(rows, code, gated, n, k, ctypes.byref(size)) == H.OK
+    return size.value / (rows * -(-n // 16) * 64)
+
+
+def test_product4_workspace_is_for_few_weight_rows_and_long_columns():
+    assert product_splits(16, "rows", 0, 5120, 25_600) == 3
+    assert all(product_splits(rows, kind, 0, n, k) > 1 for rows, n, k, _, _, kind in SHARED)
+    assert product_splits(1, "rows", 0, 4096, 4096) == product_splits(4, "rows", 1, 25_600, 5120) == 0
+    assert product_splits(5000, "rows", 0, 64, 25_600) == 0
+    size = ctypes.byref(ctypes.c_size_t(0))
+    for bad in ((-1, 0, 0, 16, 16), (1, 4, 0, 16, 16), (1, 0, 0, 0, 16), (1, 0, 0, 16, 0)):
+        assert lib().herschel_product4_workspace(*bad, size) == H.EINVAL
+    assert lib().herschel_product4_workspace(1, 0, 0, 16, 16, None) == H.EINVAL
+
+
+@gpu
+@pytest.mark.parametrize("case", SHARED, ids=str)
+@pytest.mark.parametrize("gated", [False, True])
+def test_product4_of_shared_columns(case, gated, monkeypatch):
+    """Parts of the columns in several workgroups, with and without the workspace for it."""
+    rows, n, k, group, zeros, kind = case
+    n = n // 32 * 32 + 32 if gated else n
+    codes, scales, zero, w, size = make_weights(n, k, group, zeros, seed=k)
+    W = device_weights(codes, scales, zero, k)
+    x = rand(rows, k, seed=n, gain=0.1)
+    if kind == "rows":
+        given, wide = x.to(DEV), x.double()
+    else:
+        r = make_rows8(x, kind, group if k % group == 0 else 0)
+        given = O.Rows8(r.codes.to(DEV), r.scale.to(DEV))
+        wide = r.codes.double() * r.scale.double().repeat_interleave(k // r.scale.shape[1], 1)
+    assert product_splits(rows, kind, gated, n, k) > 1
+    check_product(O.product4(given, W, gated=gated), wide, w, size, group, BF, gated)
+    monkeypatch.setattr(O, "_product_workspace", lambda *a: 0)
+    check_product(O.product4(given, W, gated=gated), wide, w, size, group, BF, gated)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["rows", F8, I8], ids=str)
+@pytest.mark.parametrize("rows,n,k,group", [(4, 4160, 520, 64), (30, 8320, 256, 128), (64, 4224, 384, 32), (64, 8448, 128, 128),
+                                            (9, 8400, 130, 128), (130, 4176, 256, 64)])
+def test_product4_of_many_weight_rows(rows, n, k, group, kind):
+    """The wider workgroups: more than 256 of 32 weight rows, and of 64."""
+    codes, scales, zero, w, size = make_weights(n, k, group, True, seed=rows)
+    W = device_weights(codes, scales, zero, k)
+    x = rand(rows, k, seed=3)
+    for gated in (False, True) if n % 32 == 0 else (False,):
+        if kind == "rows":
+            check_product(O.product4(x.to(DEV), W, gated=gated), x.double(), w, size, group, BF, gated)
+        else:
+            r = make_rows8(x, kind, 0)
+            y = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W, gated=gated)
+            check_product(y, r.codes.double() * r.scale.double(), w, size, group, BF, gated)
+
+
 @gpu
 def test_product4_strides_and_outputs():
     """Rows inside wider ones, at odd elements, one row for all; a given output and what lies behind it."""
@@ -336,17 +399,18 @@ def test_weights4_layout_and_quantise():
         codes, scales, zero, w, _ = make_weights(n, k, group, zeros)
         W = O.Weights4(codes, scales, zero, k=k)
         assert torch.equal(W.dense().double(), w)
-        flat = W.codes.view(W.codes.shape[0], W.codes.shape[1], 64, 4, 4)
+        run = W.group // 4
         for i, j in ((0, 0), (n - 1, k - 1), (n // 2, k // 2), (n - 1, k // 3), (n // 3, 5)):
-            byte = int(flat[i // 16, j // 128, (j // 8) % 4 * 16 + i % 16, (j // 32) % 4, j % 4])
+            g, f = j % 128 // W.group, j % W.group
+            byte = int(W.codes[j // 128, i // 16, f // run, i % 16, g * run // 8 + f % run // 8, j % 4])
             assert (byte >> (0 if j % 8 < 4 else 4)) & 15 == (int(codes[i, j // 2]) >> (4 * (j % 2))) & 15
-            g = j // group if k > group else 0
-            assert W.scales[i // 16, g, i % 16] == scales[i, g]
+            word = W.scales[j // 128, i // 16, i % 16 // 4, g, i % 4]
+            assert (word & -256).view(F32) == scales[i, j // W.group] and word & 255 == (zero[i, j // W.group] if zeros else 8)
     for zeros in (False, True):
         x = rand(50, 200, seed=7, dtype=F32) + (1.0 if zeros else 0.0)
         x[3, 64:128] = 0
         W = O.Weights4.quantise(x, 64, zeros=zeros, scale_dtype=HF)
-        s = W.scales.transpose(1, 2).reshape(64, -1)[:50, :4].double().repeat_interleave(64, 1)[:, :200]
+        s = (W.scales & -256).view(F32).permute(1, 2, 4, 0, 3).reshape(64, -1)[:50, :4].double().repeat_interleave(64, 1)[:, :200]
         # half a step; at the ends the scale's rounding on top: 7 or 15 steps of 2^-11, and the zero's half step
         assert ((W.dense().double() - x.double()).abs() <= s * (0.5 + 15 * 2.0 ** -11 + (0.5 if zeros else 0)) + 1e-12).all()
         assert (W.dense()[3, 64:128] == 0).all()
@@ -610,7 +674,7 @@ def test_bad_norm_calls_are_refused(bad):
 
 
 def weights_struct(**kw):
-    a = dict(codes=FAKE, scales=FAKE, zeros=None, n=64, k=256, group=128, scale_type=O.BF16)
+    a = dict(codes=FAKE, scales=FAKE, n=64, k=256, group=128)
     return O.HerschelWeights4(**{**a, **kw})
 
 
@@ -624,8 +688,8 @@ def product_args(**kw):
     (dict(n_rows=1 << 40), {}), (dict(x_row=-1), {}), (dict(kind=O.F16), {}), (dict(kind=O.F32, type=O.F32), {}),
     (dict(kind=O.INT8), {}), (dict(kind=O.INT8, x_scale=FAKE + 2), {}), (dict(x_group=128), {}),
     (dict(kind=O.FP8, x_scale=FAKE, x_group=64), {}), (dict(gated=1), dict(n=48)), ({}, dict(codes=None)),
-    ({}, dict(scales=None)), ({}, dict(codes=FAKE + 8)), ({}, dict(zeros=FAKE + 4)), ({}, dict(n=0)), ({}, dict(k=0)),
-    ({}, dict(k=0x7fffff80)), ({}, dict(group=16)), ({}, dict(group=256)), ({}, dict(scale_type=O.F32))], ids=str)
+    ({}, dict(scales=None)), ({}, dict(codes=FAKE + 8)), ({}, dict(scales=FAKE + 4)), ({}, dict(n=0)), ({}, dict(k=0)),
+    ({}, dict(k=0x7fffff80)), ({}, dict(group=16)), ({}, dict(group=256))], ids=str)
 def test_bad_product_calls_are_refused(bad, weights):
     assert lib().herschel_product4(ctypes.byref(product_args(**bad)), ctypes.byref(weights_struct(**weights))) == H.EINVAL
 
