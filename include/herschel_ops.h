@@ -280,7 +280,7 @@ typedef struct {
   int32_t n_drafts;           /* 0 ... HERSCHEL_MAX_DRAFTS */
   int32_t vocab;              /* >= 1 */
   int32_t type;               /* HERSCHEL_F32, HERSCHEL_BF16 or HERSCHEL_F16 */
-  void *workspace;            /* herschel_verify_workspace() bytes, 16-byte aligned; no two calls at once */
+  void *workspace;            /* herschel_verify_workspace() bytes, 16-byte aligned, or NULL with 0; no two calls at once */
   size_t workspace_bytes;
   uint32_t *status;
   void *hip_stream;
@@ -288,7 +288,7 @@ typedef struct {
 
 #define HERSCHEL_MAX_DRAFTS 1024
 
-/* Bytes of workspace for calls of at most these sizes. */
+/* Bytes of workspace for a call of these sizes; 0 for small vocabularies. */
 int herschel_verify_workspace(int32_t n_seqs, int32_t vocab, size_t *bytes);
 
 /* Draft t of a sequence, token x, is accepted iff those before it are and

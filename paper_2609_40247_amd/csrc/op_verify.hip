@@ -1,11 +1,13 @@
 // Drafted tokens against the target's probabilities: how many are accepted, and
-// the token drawn behind them.  Two launches.
+// the token drawn behind them.
 //
 // Only one row of the vocabulary a sequence is ever read, that of the first draft
-// that is not accepted (and its counterpart of the draft's probabilities): every
-// workgroup finds it by itself from the drafts' own probabilities, a few
-// loads, and sums its share of the row; the second kernel finds the share in
-// which the cumulative sum passes the random number's and goes over it again.
+// that is not accepted (and its counterpart of the draft's probabilities), found
+// from the drafts' own probabilities, a few loads.  Up to ONE_ROW tokens a
+// workgroup a sequence does it all: it sums what each wave's run of the row
+// weighs, finds the run in which the cumulative sum passes the random number's,
+// and in it the lane and the token.  Longer rows are summed in shares by many
+// workgroups first; the second launch finds the share.
 #include "ops.hpp"
 
 namespace hop {
@@ -18,6 +20,8 @@ struct VerifyArgs {
 
 constexpr int VERIFY_THREADS = 256, VERIFY_WAVES = VERIFY_THREADS / WAVE;
 constexpr int SHARE_STEP = VERIFY_THREADS * 8;
+constexpr int MOST_STEPS = 16;  // of a share
+constexpr int ONE_THREADS = 1024, ONE_ROW = ONE_THREADS * 8 * 4;
 
 template <int TYPE>
 __device__ __forceinline__ float probability(const void* p, int64_t at) {
@@ -58,23 +62,32 @@ __device__ __forceinline__ int accepted_drafts(const herschel_verify_args& a, in
 }
 
 // Eight elements from `at` on of a row of probabilities; those from `end` on are 0.
+// The load is in no branch but for a row's last, odd elements, so that several are
+// under way at once.
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x4 u32x4_half __attribute__((aligned(2)));
 template <int TYPE>
 __device__ __forceinline__ void load_row(const void* base, int64_t row, int at, int end, float* x) {
-  if (at + 8 <= end) {
+  if (end >= 8) {
+    const int64_t from = row + min(at, end - 8);
     if constexpr (TYPE == HERSCHEL_F32) {
-      const f32x4 u = *(const f32x4_any*)((const float*)base + row + at), v = *(const f32x4_any*)((const float*)base + row + at + 4);
+      const f32x4 u = *(const f32x4_any*)((const float*)base + from), v = *(const f32x4_any*)((const float*)base + from + 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = u[i], x[i + 4] = v[i];
     } else {
-      const u32x4 w = *(const u32x4_half*)((const uint16_t*)base + row + at);
+      const u32x4 w = *(const u32x4_half*)((const uint16_t*)base + from);
 #pragma unroll
       for (int i = 0; i < 4; ++i) unpack2<TYPE>(w[i], x[2 * i], x[2 * i + 1]);
     }
-  } else {
+  }
+  if (at + 8 > end) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = at + i < end ? probability<TYPE>(base, row + at + i) : 0.0f;
+    for (int i = 0; i < 8; ++i) x[i] = 0;
+    if (at < end) {
+#pragma unroll
+      for (int i = 0; i < 7; ++i)
+        if (at + i < end) x[i] = probability<TYPE>(base, row + at + i);
+    }
   }
 }
 
@@ -97,18 +110,21 @@ __device__ __forceinline__ Row row_of(const herschel_verify_args& a, int64_t b, 
   }
   return r;
 }
-// What eight elements weigh: target - draft, or (alone) the target.
-template <int TYPE>
-__device__ __forceinline__ void weigh(const herschel_verify_args& a, const Row& r, int at, int end, double* both,
-                                      double* alone) {
+struct Eight {
   float p[8], q[8];
-  load_row<TYPE>(a.target, r.target, at, end, p);
-  if (r.differs && a.draft) load_row<TYPE>(a.draft, r.draft, at, end, q);
+};
+template <int TYPE>
+__device__ __forceinline__ void load_eight(const herschel_verify_args& a, const Row& r, int at, int end, Eight& x) {
+  load_row<TYPE>(a.target, r.target, at, end, x.p);
+  if (r.differs && a.draft) load_row<TYPE>(a.draft, r.draft, at, end, x.q);
+}
+// What eight elements weigh: target - draft, or (alone) the target.
+__device__ __forceinline__ void weigh(const herschel_verify_args& a, const Row& r, int at, const Eight& x, double* both, double* alone) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    alone[i] = p[i] > 0 ? (double)p[i] : 0.0;
-    double d = (double)p[i];
-    if (r.differs) d -= a.draft ? (double)q[i] : at + i == r.one ? 1.0 : 0.0;
+    alone[i] = x.p[i] > 0 ? (double)x.p[i] : 0.0;
+    double d = (double)x.p[i];
+    if (r.differs) d -= a.draft ? (double)x.q[i] : at + i == r.one ? 1.0 : 0.0;
     both[i] = d > 0 ? d : 0.0;
   }
 }
@@ -131,8 +147,10 @@ __global__ __launch_bounds__(VERIFY_THREADS) void k_verify_sums(VerifyArgs p) {
   double s = 0, t = 0;
   const int from = blockIdx.x * p.size, end = min(a.vocab, from + p.size);
   for (int at = from + (int)threadIdx.x * 8; at < end; at += SHARE_STEP) {
+    Eight x;
     double both[8], alone[8];
-    weigh<TYPE>(a, r, at, end, both, alone);
+    load_eight<TYPE>(a, r, at, end, x);
+    weigh(a, r, at, x, both, alone);
 #pragma unroll
     for (int i = 0; i < 8; ++i) s += both[i], t += alone[i];
   }
@@ -146,133 +164,179 @@ __global__ __launch_bounds__(VERIFY_THREADS) void k_verify_sums(VerifyArgs p) {
     for (int i = 0; i < VERIFY_WAVES; ++i) s += box[0][i], t += box[1][i];
     out[0] = s;
     out[1] = t;
+    if (blockIdx.x == 0) {
+      int* counted = (int*)((double*)a.workspace + (int64_t)a.n_seqs * p.shares * 2) + b * 2;
+      counted[0] = accepted;
+      counted[1] = n;
+    }
   }
 }
 
-// The first of a workgroup's threads, in order, behind whose v the sum of the
-// values up to it is above `than`, and the sum before it; if there is none, the
-// last with a value above 0; -1 if there is none either.  Returns the whole sum too.
-struct Place {
-  int thread;
-  double before, all;
-};
-__device__ __forceinline__ Place place(double v, double base, double than, double* sums, int* found) {
-  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
+// The first of a wave's lanes, in order, up to which the sum of the lanes' values
+// behind `base` is above `than`; without one, the last with a value above 0, or -1.
+// `before`: the sum before it.
+__device__ __forceinline__ int pick_lane(double v, double base, double than, double& before) {
+  const int lane = threadIdx.x % WAVE;
   double up = v;
 #pragma unroll
   for (int o = 1; o < WAVE; o *= 2) {
     const double below = __shfl_up(up, o);
     if (lane >= o) up += below;
   }
-  __syncthreads();  // what was in sums and found has been read
-  if (lane == WAVE - 1) sums[wave] = up;
-  if (threadIdx.x < 2) found[threadIdx.x] = threadIdx.x == 0 ? VERIFY_THREADS : -1;
-  __syncthreads();
-  double before = base, all = 0;
-  for (int i = 0; i < VERIFY_WAVES; ++i) {
-    if (i < wave) before += sums[i];
-    all += sums[i];
-  }
-  if (before + up > than && v > 0) atomicMin(found, (int)threadIdx.x);
-  if (v > 0) atomicMax(found + 1, (int)threadIdx.x);
-  __syncthreads();
-  Place r;
-  r.thread = found[0] < VERIFY_THREADS ? found[0] : found[1];
-  r.before = before + up - v;
-  r.all = all;
-  return r;
+  const uint64_t some = __ballot(v > 0), above = __ballot(v > 0 && base + up > than);
+  if (!some) return -1;
+  const int at = above ? __builtin_ctzll(above) : 63 - __builtin_clzll(some);
+  before = __shfl(base + up - v, at);
+  return at;
 }
 
 // The token of each sequence, and the outputs.
-template <int TYPE>
-__global__ __launch_bounds__(VERIFY_THREADS) void k_verify_draw(VerifyArgs p) {
+template <int TYPE, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void k_verify_draw(VerifyArgs p) {
+  constexpr int WAVES = THREADS / WAVE, STEP = THREADS * 8;
   const herschel_verify_args& a = p.a;
-  __shared__ double sums[VERIFY_WAVES], start;
-  __shared__ int found[2], token;
+  __shared__ double sums[2][WAVES];
   const int64_t b = blockIdx.x;
-  const int tid = threadIdx.x;
-  int n;
-  const int accepted = accepted_drafts<TYPE>(a, b, n, false);
+  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
+  const double u = (double)a.final_u[b];
+  int n, accepted;
+  if constexpr (ONE) {
+    accepted = accepted_drafts<TYPE>(a, b, n, tid < WAVE);
+  } else {
+    const int* counted = (const int*)((const double*)a.workspace + (int64_t)a.n_seqs * p.shares * 2) + b * 2;
+    accepted = counted[0];
+    n = counted[1];
+  }
   Row r = row_of<TYPE>(a, b, n, accepted);
-  for (int t = tid; t <= a.n_drafts; t += VERIFY_THREADS)
-    if (t != accepted) a.out[b * (a.n_drafts + 1) + t] = t < accepted ? a.tokens[b * a.n_drafts + t] : -1;
+  int64_t* const out = a.out + b * (a.n_drafts + 1);
+  for (int t = tid; t <= a.n_drafts; t += THREADS)
+    if (t != accepted) out[t] = t < accepted ? a.tokens[b * a.n_drafts + t] : -1;
+  if (tid == 0) a.accepted[b] = accepted;
 
-  // the shares' sums, a run of them a thread
-  const double* of = (const double*)a.workspace + b * p.shares * 2;
-  const int run = (p.shares + VERIFY_THREADS - 1) / VERIFY_THREADS, first = tid * run, last = min(p.shares, first + run);
-  double both = 0, alone = 0;
-  for (int i = first; i < last; ++i) both += of[2 * i], alone += of[2 * i + 1];
-  Place at = place(both, 0.0, INFINITY, sums, found);
-  int which = 0;
-  if (!(at.all > 0)) {  // nothing of the target is above the draft: the target alone
-    which = 1;
-    r.differs = false;
-    at = place(alone, 0.0, INFINITY, sums, found);
+  // the share, each wave by itself; a run of shares a lane
+  int from = 0, end = a.vocab;
+  double base = 0, than = 0;
+  bool alone = false;  // nothing of the target is above the draft
+  if constexpr (!ONE) {
+    const double* of = (const double*)a.workspace + b * p.shares * 2;
+    const int run = (p.shares + WAVE - 1) / WAVE, first = lane * run, last = min(p.shares, first + run);
+    double v[2] = {0, 0};
+    for (int i = first; i < last; ++i) v[0] += of[2 * i], v[1] += of[2 * i + 1];
+    const double all[2] = {wave_sum(v[0]), wave_sum(v[1])};
+    alone = !(all[0] > 0);
+    than = u * all[alone];
+    int share = -1;
+    const int at = pick_lane(v[alone], 0.0, than, base);
+    if (at >= 0) {
+      for (int i = at * run; i < min(p.shares, at * run + run); ++i) {  // the same in every lane
+        const double w = of[2 * i + alone];
+        if (!(w > 0)) continue;
+        if (share >= 0) base += of[2 * share + alone];
+        share = i;
+        if (base + w > than) break;
+      }
+    }
+    if (share < 0) {
+      if (tid == 0) {
+        out[accepted] = -1;
+        flag(a.status, HERSCHEL_OP_BAD_ROW);
+      }
+      return;
+    }
+    from = share * p.size;
+    end = min(a.vocab, from + p.size);
+    if (alone) r.differs = false;
   }
-  const double than = (double)a.final_u[b] * at.all;
-  at = place(which ? alone : both, 0.0, than, sums, found);
-  if (tid == 0) {
-    a.accepted[b] = accepted;
-    token = -1;
-    if (at.thread < 0) flag(a.status, HERSCHEL_OP_BAD_ROW);
+
+  // what each wave's run of the share weighs, `steps` times 512 elements
+  const int steps = (end - from + STEP - 1) / STEP, begin = from + wave * steps * (WAVE * 8) + lane * 8;
+  constexpr int AT_ONCE = ONE ? ONE_ROW / STEP : 1;  // one workgroup has no more steps, and keeps their sums
+  Eight x[AT_ONCE];
+  double s[AT_ONCE], s_alone[AT_ONCE], sum = 0, sum_alone = 0;
+  auto lane_sums = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i)
+      if (i0 + i < steps) load_eight<TYPE>(a, r, begin + (i0 + i) * (WAVE * 8), end, x[i]);
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      s[i] = s_alone[i] = 0;
+      if (i0 + i >= steps) continue;
+      double both[8], one[8];
+      weigh(a, r, begin + (i0 + i) * (WAVE * 8), x[i], both, one);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[i] += both[e], s_alone[i] += one[e];
+      sum += s[i];
+      sum_alone += s_alone[i];
+    }
+  };
+  for (int i = 0; i < steps; i += AT_ONCE) lane_sums(i);
+  sum = wave_sum(sum);
+  if constexpr (ONE) sum_alone = wave_sum(sum_alone);
+  if (lane == 0) sums[0][wave] = sum, sums[1][wave] = sum_alone;
+  __syncthreads();
+  const bool counts = lane < WAVES;
+  if constexpr (ONE) {
+    const double all = wave_sum(counts ? sums[0][lane] : 0.0);
+    alone = !(all > 0);
+    than = u * (alone ? wave_sum(counts ? sums[1][lane] : 0.0) : all);
+    if (alone) r.differs = false;
   }
-  if (at.thread < 0) {
-    if (tid == 0) a.out[b * (a.n_drafts + 1) + accepted] = -1;
+  double before = 0;
+  const int at = pick_lane(counts ? sums[ONE && alone][lane] : 0.0, base, than, before);
+  if (at < 0) {
+    if (tid == 0) {
+      out[accepted] = -1;
+      flag(a.status, HERSCHEL_OP_BAD_ROW);
+    }
     return;
   }
-  __syncthreads();
-  if (tid == at.thread) {  // the share of the run
-    double s = at.before;
-    int share = -1;
-    for (int i = first; i < last; ++i) {
-      const double v = of[2 * i + which];
-      if (!(v > 0)) continue;
-      share = i;
-      start = s;
-      s += v;
-      if (s > than) break;
-    }
-    token = share;
-  }
-  __syncthreads();
-  const int share = token, from = share * p.size, end = min(a.vocab, from + p.size);
-  double base = start;
-  // the share's elements, eight a thread
-  int behind = -1;  // the last element above 0 so far
-  __shared__ int pick;
-  for (int at0 = from; at0 < end; at0 += SHARE_STEP) {
-    double w[8], unused[8], s = 0;
-    const int mine = at0 + tid * 8;
-    weigh<TYPE>(a, r, mine, end, w, unused);
+  if (wave != at) return;
+  // its step, the lane in that, and the token
+  int step = -1;
+  double up = before, of_lane = 0;
+  for (int i = 0; i < steps; ++i) {
+    double v = 0;
+    if constexpr (ONE) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s += w[i];
-    const Place e = place(s, base, than, sums, found);
-    if (tid == e.thread) {
-      double up = e.before;
-      int k = -1;
-      bool above = false;
+      for (int k = 0; k < AT_ONCE; ++k)
+        if (k == i) v = alone ? s_alone[k] : s[k];
+    } else {
+      Eight y;
+      double both[8], one[8];
+      load_eight<TYPE>(a, r, begin + i * (WAVE * 8), end, y);
+      weigh(a, r, begin + i * (WAVE * 8), y, both, one);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (above || !(w[i] > 0)) continue;
-        k = mine + i;
-        up += w[i];
-        above = up > than;
-      }
-      pick = k;
+      for (int e = 0; e < 8; ++e) v += both[e];
     }
-    const bool done = found[0] < VERIFY_THREADS;
-    __syncthreads();
-    if (e.thread >= 0) behind = pick;
-    base += e.all;
-    if (done) break;
-    __syncthreads();
+    const double all = wave_sum(v);
+    if (!(all > 0)) continue;
+    step = i;
+    of_lane = v;
+    before = up;
+    up += all;
+    if (up > than) break;
   }
-  if (tid == 0) a.out[b * (a.n_drafts + 1) + accepted] = behind;
+  if (lane != pick_lane(of_lane, before, than, up)) return;
+  Eight mine;
+  double w[8], unused[8];
+  const int first_of = begin + step * (WAVE * 8);
+  load_eight<TYPE>(a, r, first_of, end, mine);
+  weigh(a, r, first_of, mine, w, unused);
+  int token = -1;
+  bool above = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (above || !(w[e] > 0)) continue;
+    token = first_of + e;
+    up += w[e];
+    above = up > than;
+  }
+  out[accepted] = token;
 }
 
 inline int shares_of(int vocab, int n_seqs, int& size) {
   size = SHARE_STEP;
-  while (size < 16 * SHARE_STEP && (int64_t)((vocab + size - 1) / size) * n_seqs > 4096) size *= 2;
+  while (size < MOST_STEPS * SHARE_STEP && (int64_t)((vocab + size - 1) / size) * n_seqs > 4096) size *= 2;
   return (vocab + size - 1) / size;
 }
 
@@ -281,8 +345,8 @@ inline int shares_of(int vocab, int n_seqs, int& size) {
 extern "C" int herschel_verify_workspace(int32_t n_seqs, int32_t vocab, size_t* bytes) {
   using namespace hop;
   if (!bytes || n_seqs < 0 || n_seqs > 65535 || vocab < 1 || vocab > 0x40000000) return HERSCHEL_EINVAL;
-  // shares are no smaller than these
-  *bytes = (size_t)n_seqs * ((vocab + SHARE_STEP - 1) / SHARE_STEP) * 2 * sizeof(double);
+  int size;
+  *bytes = vocab <= ONE_ROW ? 0 : (size_t)n_seqs * (shares_of(vocab, n_seqs, size) * 2 * sizeof(double) + 2 * sizeof(int));
   return HERSCHEL_OK;
 }
 
@@ -300,17 +364,22 @@ extern "C" int herschel_verify_drafts(const herschel_verify_args* args) {
   if (!a.target || !aligned(a.target, to) || !aligned(a.draft, to) || !a.final_u || !a.out || !a.accepted)
     return HERSCHEL_EINVAL;
   if (a.n_drafts && (!a.tokens || !a.accept_u)) return HERSCHEL_EINVAL;
-  if (a.workspace_bytes < need || !a.workspace || !aligned(a.workspace, 16)) return HERSCHEL_EWORKSPACE;
+  if (need && (a.workspace_bytes < need || !a.workspace || !aligned(a.workspace, 16))) return HERSCHEL_EWORKSPACE;
   VerifyArgs p{a};
   p.shares = shares_of(a.vocab, a.n_seqs, p.size);
   const bool f32 = a.type == HERSCHEL_F32, bf = a.type == HERSCHEL_BF16;
+  if (!need)
+    return launch(f32  ? k_verify_draw<HERSCHEL_F32, ONE_THREADS, true>
+                  : bf ? k_verify_draw<HERSCHEL_BF16, ONE_THREADS, true>
+                       : k_verify_draw<HERSCHEL_F16, ONE_THREADS, true>,
+                  dim3((unsigned)a.n_seqs), dim3(ONE_THREADS), 0, a.hip_stream, p);
   const int code = launch(f32  ? k_verify_sums<HERSCHEL_F32>
                           : bf ? k_verify_sums<HERSCHEL_BF16>
                                : k_verify_sums<HERSCHEL_F16>,
                           dim3((unsigned)p.shares, (unsigned)a.n_seqs), dim3(VERIFY_THREADS), 0, a.hip_stream, p);
   if (code != HERSCHEL_OK) return code;
-  return launch(f32  ? k_verify_draw<HERSCHEL_F32>
-                : bf ? k_verify_draw<HERSCHEL_BF16>
-                     : k_verify_draw<HERSCHEL_F16>,
+  return launch(f32  ? k_verify_draw<HERSCHEL_F32, VERIFY_THREADS, false>
+                : bf ? k_verify_draw<HERSCHEL_BF16, VERIFY_THREADS, false>
+                     : k_verify_draw<HERSCHEL_F16, VERIFY_THREADS, false>,
                 dim3((unsigned)a.n_seqs), dim3(VERIFY_THREADS), 0, a.hip_stream, p);
 }

@@ -416,21 +416,26 @@ __global__ __launch_bounds__(S::THREADS) void k_product4(ProductArgs p) {
 // The sums of the workgroups that share a product's columns, four of its elements a thread.
 template <bool GROUPS>
 __global__ __launch_bounds__(256) void k_product4_join(ProductArgs p) {
-  const int wide = p.tiles_n * 4 / (p.a.gated ? 2 : 1);
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, m = id / wide;
-  if (m >= p.a.n_rows) return;
-  const int n = (int)(id % wide) * 4;
+  const int64_t m = blockIdx.y;
+  const int n = (int)(blockIdx.x * 256 + threadIdx.x) * 4;
+  if (n >= p.tiles_n * 16 / (p.a.gated ? 2 : 1)) return;
   const float* from = (const float*)p.a.workspace + m * (p.tiles_n * 16) + n;
   f32x4 y = {0, 0, 0, 0}, b = {0, 0, 0, 0};
-  for (int z = 0; z < p.splits; ++z, from += p.a.n_rows * (p.tiles_n * 16)) {
-    y += *(const f32x4*)from;
-    if (p.a.gated) b += *(const f32x4*)(from + p.half * 16);
+  f32x4 part[4], gate_part[4];
+#pragma unroll
+  for (int z = 0; z < 4; ++z) {  // all asked for before the first is used
+    part[z] = gate_part[z] = f32x4{0, 0, 0, 0};
+    if (z < p.splits) part[z] = *(const f32x4*)from;
+    if (z < p.splits && p.a.gated) gate_part[z] = *(const f32x4*)(from + p.half * 16);
+    from += p.a.n_rows * (p.tiles_n * 16);
   }
+#pragma unroll
+  for (int z = 0; z < 4; ++z) y += part[z], b += gate_part[z];
   store_product(p.a, p.w, p.a.kind, GROUPS, m, n, y, b);
 }
 
 template <class S>
-static int product_launch(ProductArgs& p, int splits = 1) {
+static int product_launch(ProductArgs& p, int splits) {  // at most 4
   const int tiles = p.a.gated ? p.half : p.tiles_n, each = S::WN * (p.a.gated ? S::NT / 2 : S::NT);
   const int64_t blocks = (p.a.n_rows + S::ROWS - 1) / S::ROWS;
   if (blocks > 65535) return HERSCHEL_EINVAL;
@@ -451,40 +456,40 @@ static int product_launch(ProductArgs& p, int splits = 1) {
   const int code = launch(k_product4<S>, dim3((unsigned)((tiles + each - 1) / each), (unsigned)blocks, (unsigned)p.splits),
                           dim3(S::THREADS), lds, p.a.hip_stream, p);
   if (code != HERSCHEL_OK || p.splits == 1) return code;
-  const int64_t quads = p.a.n_rows * (p.tiles_n * 4 / (p.a.gated ? 2 : 1));
-  return launch(S::GROUPS ? k_product4_join<true> : k_product4_join<false>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0,
-                p.a.hip_stream, p);
+  return launch(S::GROUPS ? k_product4_join<true> : k_product4_join<false>,
+                dim3((unsigned)((tiles * 4 + 255) / 256), (unsigned)p.a.n_rows), dim3(256), 0, p.a.hip_stream, p);
 }
 // Which kernel a call takes.  A workgroup's start and end cost as much as several
 // turns, so that one round of workgroups, at most one a CU, is best: with few weight
 // rows narrow ones, with many wide ones; with few weight rows and long columns these
 // are shared among several, joined by a second kernel.  The time of each choice
 // is estimated from measured ones (bf16 rows, groups of 128), in units of 10 ns: 400
-// and so much a turn, 300 for the join.  Measured against the choices beside them: 16
+// and so much a turn, 400 for the join.  Measured against the choices beside them: 16
 // rows by 25600 x 5120 weights 17.3 us with 8 tiles a workgroup, 21.2 with 4, 29.5
-// with 2; by 6144 x 4096 7.9 with 2, 9.5 with 4; by 5120 x 25600 22.8 with 4 in three parts,
+// with 2; by 6144 x 4096 7.9 with 2, 9.5 with 4, 11.6 with 1; by 1280 x 5120 7.2 with 1, 8.4 with 2; by 5120 x 25600 22.8 with 4 in three parts,
 // 26.4 with 2 and no parts; by 4096 x 14336 13.8 with 2 in two parts, 16.3 without.
 struct Choice {
-  int wide;    // 0, 1, 2: two, four, eight tiles of weight rows a workgroup
+  int wide;    // 0 to 3: one, two, four, eight tiles of weight rows a workgroup
   int splits;
 };
 inline size_t parts_bytes(const ProductArgs& p, int splits) { return (size_t)splits * p.a.n_rows * p.tiles_n * 64; }
 inline int rows_at_once(int64_t n_rows) { return n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64; }
 inline Choice choose(const ProductArgs& p, size_t room) {
-  const int rows = rows_at_once(p.a.n_rows);
-  const bool narrow = rows < 64 || !p.a.gated;  // the narrow one for 64 rows has no two tiles a wave
-  static const int TURN[3][3] = {{95, 75, 65}, {175, 105, 85}, {156, 190, 135}}, WAVES_K[2][3] = {{8, 4, 2}, {4, 4, 2}};
-  const int rows_at = rows <= 16 ? 0 : rows <= 32 ? 1 : 2;
+  static const int TURN[3][4] = {{65, 95, 75, 65}, {0, 175, 105, 85}, {0, 156, 190, 135}}, WAVES_K[2][4] = {{8, 8, 4, 2}, {0, 4, 4, 2}};
+  const int rows = rows_at_once(p.a.n_rows), rows_at = rows / 32;
+  // a wave with one tile of weight rows has none that gates
+  const int narrowest = rows == 16 && !p.a.gated ? 0 : rows == 64 && p.a.gated ? 2 : 1;
   const int64_t tiles = p.a.gated ? p.half * 2 : p.tiles_n, blocks_m = (p.a.n_rows + rows - 1) / rows;
-  Choice best{1, 1};
+  Choice best{narrowest, 1};
   int64_t least = INT64_MAX;
-  for (int wide = narrow ? 0 : 1; wide < 3; ++wide) {
-    const int64_t blocks = (tiles + (2 << wide) - 1) / (2 << wide) * blocks_m;
+  for (int wide = narrowest; wide < 4; ++wide) {
+    const int64_t blocks = (tiles + (1 << wide) - 1) / (1 << wide) * blocks_m;
     for (int splits = 1; splits <= 4; ++splits) {
       if (splits > 1 && parts_bytes(p, splits) > room) break;
-      const int each = (p.tiles_k + splits - 1) / splits, k = WAVES_K[rows_at == 2][wide];
+      const int each = (p.tiles_k + splits - 1) / splits, k = WAVES_K[rows == 64][wide];
       const int64_t rounds = (blocks * splits + 255) / 256, turns = (each + k - 1) / k;
-      const int64_t time = rounds * (400 + turns * TURN[rows_at][wide] * (quantised(p.a.kind) && rows_at ? 2 : 3) / 3) + (splits > 1 ? 300 : 0);
+      const int turn = quantised(p.a.kind) && rows > 16 ? TURN[rows_at][wide] * 2 / 3 : TURN[rows_at][wide];
+      const int64_t time = rounds * (400 + turns * turn) + (splits > 1 ? 400 : 0);
       if (time < least) {
         least = time;
         best = Choice{wide, splits};
@@ -496,22 +501,23 @@ inline Choice choose(const ProductArgs& p, size_t room) {
 
 template <int KIND, bool GROUPS, int GROUP>
 static int product_shape(ProductArgs& p) {
-  constexpr int U = GROUP == 32 ? 1 : 2;  // with more groups' scales, two turns' ahead do not fit the registers
+  constexpr int U = GROUP == 32 ? 1 : 2;  // more groups' scales of more turns ahead do not fit the registers
   const int rows = rows_at_once(p.a.n_rows);
   const size_t room = p.a.workspace && aligned(p.a.workspace, 16) ? p.a.workspace_bytes : 0;
   const Choice c = choose(p, room);
   if (rows == 16) {
-    if (c.wide == 0) return product_launch<Shape<KIND, GROUPS, GROUP, 16, 2, 1, 8, U, 4, 131072>>(p, c.splits);
-    if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 16, 2, 2, 4, U, 4, 131072>>(p, c.splits);
+    if (c.wide == 0) return product_launch<Shape<KIND, GROUPS, GROUP, 16, 1, 1, 8, 2 * U, 4, 131072>>(p, c.splits);
+    if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 16, 2, 1, 8, U, 4, 131072>>(p, c.splits);
+    if (c.wide == 2) return product_launch<Shape<KIND, GROUPS, GROUP, 16, 2, 2, 4, U, 4, 131072>>(p, c.splits);
     return product_launch<Shape<KIND, GROUPS, GROUP, 16, 2, 4, 2, U, 4, 131072>>(p, c.splits);
   }
   if (rows == 32) {
-    if (c.wide == 0) return product_launch<Shape<KIND, GROUPS, GROUP, 32, 2, 1, 8, U, 4, 147456>>(p, c.splits);
-    if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 32, 2, 2, 4, U, 4, 131072>>(p, c.splits);
+    if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 32, 2, 1, 8, U, 4, 147456>>(p, c.splits);
+    if (c.wide == 2) return product_launch<Shape<KIND, GROUPS, GROUP, 32, 2, 2, 4, U, 4, 131072>>(p, c.splits);
     return product_launch<Shape<KIND, GROUPS, GROUP, 32, 2, 4, 2, U, 4, 131072>>(p, c.splits);
   }
-  if (c.wide == 0) return product_launch<Shape<KIND, GROUPS, GROUP, 64, 1, 2, 4, U, 4, 147456>>(p, c.splits);
-  if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 64, 2, 2, 4, U, 4, 147456>>(p, c.splits);
+  if (c.wide == 1) return product_launch<Shape<KIND, GROUPS, GROUP, 64, 1, 2, 4, U, 4, 147456>>(p, c.splits);
+  if (c.wide == 2) return product_launch<Shape<KIND, GROUPS, GROUP, 64, 2, 2, 4, U, 4, 147456>>(p, c.splits);
   return product_launch<Shape<KIND, GROUPS, GROUP, 64, 2, 4, 2, U, 4, 147456>>(p, c.splits);
 }
 template <int KIND, bool GROUPS>

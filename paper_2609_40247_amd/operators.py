@@ -805,7 +805,7 @@ def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False,
 
 @functools.lru_cache(maxsize=1024)
 def _verify_workspace(lib, *sizes) -> int:
-    """Bytes of workspace for a call of these sizes."""
+    """Bytes of workspace for a call of these sizes (0: none)."""
     size = ctypes.c_size_t(0)
     lib.herschel_verify_workspace(*sizes, ctypes.byref(size))
     return int(size.value)
@@ -853,9 +853,9 @@ def verify_drafts(target: torch.Tensor, tokens: torch.Tensor, accept: torch.Tens
     out, accepted = tokens.new_empty((B, S + 1)), tokens.new_empty((B,), dtype=torch.int32)
     lib = lib or _lib()
     size = _verify_workspace(lib, B, V)
-    workspace = target.new_empty(size, dtype=torch.uint8)
+    workspace = target.new_empty(size, dtype=torch.uint8) if size else None
     args = _VERIFY.pack(target.data_ptr(), target.stride(0), target.stride(1), dp, ds, dr, drafted, n, u, last,
-                        out.data_ptr(), accepted.data_ptr(), B, S, V, _PROBABILITIES[target.dtype], workspace.data_ptr(),
-                        size, 0 if status is None else _status(status, dev), _stream(dev))
+                        out.data_ptr(), accepted.data_ptr(), B, S, V, _PROBABILITIES[target.dtype],
+                        workspace.data_ptr() if size else 0, size, 0 if status is None else _status(status, dev), _stream(dev))
     _call(lib.herschel_verify_drafts, dev, "verify_drafts", args)
     return out, accepted

@@ -479,7 +479,8 @@ def check_verify(*args):
 @pytest.mark.parametrize("dtype", [F32, BF, HF], ids=str)
 @pytest.mark.parametrize("drafted", [True, False])
 @pytest.mark.parametrize("B,S,V", [(1, 1, 1), (3, 4, 7), (1, 0, 100), (5, 2, 2047), (4, 3, 2049), (2, 70, 300), (7, 5, 32_001),
-                                   (200, 3, 5000), (1, 2, 151_936)])
+                                   (200, 3, 5000), (1, 2, 151_936), (2, 3, 32_768),
+                                   (3, 2, 32_769), (300, 1, 40_000)])
 def test_verify_drafts(B, S, V, drafted, dtype):
     counts = set()
     for seed in range(3):
@@ -492,12 +493,13 @@ def test_verify_drafts(B, S, V, drafted, dtype):
 
 
 @gpu
-def test_verify_drafts_at_the_borders():
+@pytest.mark.parametrize("V", [4096, 70_000])
+def test_verify_drafts_at_the_borders(V):
     """Whole cumulative sums: random numbers at a border go to the next token that has a part; an acceptance test at
     equality is none; a probability of 0 is never accepted, and one above the draft's always."""
-    V = 4096
     target = torch.zeros(6, 2, V)
-    target[:, :, 1000], target[:, :, 3000], target[:, :, 4095] = 0.25, 0.25, 0.5
+    end = V - 1
+    target[:, :, 1000], target[:, :, 3000], target[:, :, end] = 0.25, 0.25, 0.5
     draft = torch.zeros(6, 1, V)
     draft[:, :, 1000], draft[:, :, 7] = 0.5, 0.5
     tokens = torch.tensor([[1000], [1000], [7], [7], [1000], [1000]])
@@ -506,15 +508,15 @@ def test_verify_drafts_at_the_borders():
     tokens_out, accepted = run_verify(target, tokens, accept, final, draft)
     # row 1 is accepted and draws behind it: 0.25 is the whole part of token 1000
     assert accepted.tolist() == [0, 1, 0, 0, 0, 0]
-    assert tokens_out.tolist() == [[3000, -1], [1000, 3000], [3000, -1], [3000, -1], [4095, -1], [4095, -1]]
+    assert tokens_out.tolist() == [[3000, -1], [1000, 3000], [3000, -1], [3000, -1], [end, -1], [end, -1]]
     check_verify(target, tokens, accept, final, draft)
 
 
 @gpu
-def test_verify_drafts_where_nothing_is_left():
+@pytest.mark.parametrize("V", [5000, 50_000])
+def test_verify_drafts_where_nothing_is_left(V):
     """A draft never above the target leaves no difference: the target is drawn from; without anything above 0 the
     token is -1, and reported.  Numbers not below 1, NaN and infinities choose something that has a part."""
-    V = 5000
     target, draft = torch.zeros(5, 2, V), torch.zeros(5, 1, V)
     target[:, :, 10:20] = 0.1
     draft[:] = target[:, :1]
@@ -696,7 +698,7 @@ def test_bad_product_calls_are_refused(bad, weights):
 
 def verify_args(**kw):
     a = dict(target=FAKE, target_seq=3000, target_row=1000, draft=FAKE, draft_seq=2000, draft_row=1000, tokens=FAKE,
-             counts=FAKE, accept_u=FAKE, final_u=FAKE, out=FAKE, accepted=FAKE, n_seqs=3, n_drafts=2, vocab=1000, type=O.F32,
+             counts=FAKE, accept_u=FAKE, final_u=FAKE, out=FAKE, accepted=FAKE, n_seqs=3, n_drafts=2, vocab=100_000, type=O.F32,
              workspace=FAKE, workspace_bytes=1 << 30)
     return O.HerschelVerifyArgs(**{**a, **kw})
 
