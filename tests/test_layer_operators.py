@@ -29,7 +29,7 @@ import torch
 
 from paper_2609_40247_amd import herschel as H
 from paper_2609_40247_amd import operators as O
-from test_operators import BF, DEV, F8, FAKE, HF, I8, U, gpu, lib, named, rand
+from test_operators import (BF, DEV, F8, FAKE, HF, I8, U, exact_attention, exact_rope, gpu, lib, named, rand)
 
 F32 = torch.float32
 TOP = {F8: 448.0, I8: 127.0}
@@ -652,6 +652,103 @@ def test_results_do_not_vary():
         r = O.norm_rows(x, w, kind=I8)
         assert torch.equal(r.codes, first[0].codes) and torch.equal(r.scale, first[0].scale)
         assert torch.equal(O.product4(x, W), first[1])
+
+
+# ------------------------------------------------------------ as a decoder layer
+def plain_layer(L, x, residual, lengths):
+    """A decoder layer over whole sequences in 64 bits, from its own weights; the rows of all sequences."""
+    d, h, g = L.head_dim, L.heads, L.kv_heads
+    W = {k: w.dense().double().cpu() for k, w in L.weights.items()}
+
+    def norm(stream, i):
+        return stream / torch.sqrt((stream ** 2).mean(1, keepdim=True) + L.eps) * L.norms[i].double().cpu()
+    stream = residual.double() + x.double()
+    qkv = (norm(stream, 0) @ W["qkv"].t()).view(-1, h + 2 * g, d)
+    o, at = [], 0
+    for n in lengths:
+        part = qkv[at:at + n]
+        turned = exact_rope(part[:, :h + g], L.table.cpu()[:n], "half", d)[0]
+        o.append(exact_attention(turned[:, :h], turned[:, h:], part[:, h + g:], d ** -0.5, True, 0)[0])
+        at += n
+    stream = stream + torch.cat(o).view(-1, h * d) @ W["out"].t()
+    a, b = (norm(stream, 1) @ W["gate"].t()).chunk(2, 1)
+    return (a * torch.sigmoid(a) * b) @ W["down"].t(), stream
+
+
+def make_layer(rows, total, new_tokens=1, cache="bf16", **kw):
+    from paper_2609_40247_amd import reference as R
+    return R.DecoderLayer(4, 2, 64, len(total), 128, 16, cache, ffn=320, rows=rows, new_tokens=new_tokens, **kw)
+
+
+@gpu
+@pytest.mark.parametrize("rows", ["16", "fp8", "int8"])
+@pytest.mark.parametrize("group,zeros", [(128, False), (32, True)])
+def test_decoder_layer(rows, group, zeros):
+    """Prompts, and steps of a token and two drafts, against the layer in 64 bits.  Between two norms a row goes
+    through at most six roundings to bf16 (2^-8 of itself each, at most), so twelve in all, and with 8-bit rows twice
+    through a code, off by 2^-4 of itself (fp8) or half a 127th of the largest of 256, which is under 4 times their
+    root mean square (int8); nothing in between magnifies what the norms divide by.  The bound is their sum, of norms."""
+    lens, new = [40, 3, 77], 3
+    total = [n + new for n in lens]
+    whole, parts = make_layer(rows, total, group=group, zeros=zeros), make_layer(rows, total, new, group=group, zeros=zeros)
+    x = [rand(n, 256, seed=70 + i) for i, n in enumerate(total)]
+    r = [rand(n, 256, seed=80 + i, dtype=F32) for i, n in enumerate(total)]
+    want, stream = plain_layer(whole, torch.cat(x), torch.cat(r), total)
+    bound = 12 * 2.0 ** -8 + 2 * {"16": 0.0, "fp8": 2.0 ** -4, "int8": 4 * 0.5 / 127}[rows]
+    residual = torch.cat(r).to(DEV)
+    y = whole.prompt(torch.cat(x).to(DEV), residual, total)
+    off = (y.double().cpu() - want).norm() / want.norm()
+    assert off <= bound, off
+    assert (residual.double().cpu() - stream).norm() <= bound * stream.norm()
+    parts.prompt(torch.cat([t[:-new] for t in x]).to(DEV), torch.cat([t[:-new] for t in r]).to(DEV), lens)
+    last = torch.cat([torch.arange(e - new, e) for e in torch.tensor(total).cumsum(0).tolist()])
+    for accepted in ([0, 2, 1], None):  # the same step again after it was taken back, but for the tokens kept
+        y = parts.step(torch.cat([t[-new:] for t in x]).to(DEV), torch.cat([t[-new:] for t in r]).to(DEV))
+        assert (y.double().cpu() - want[last]).norm() <= bound * want[last].norm()
+        assert parts.lengths.tolist() == total
+        if accepted is not None:
+            parts.keep(torch.tensor(accepted, dtype=torch.int32, device=DEV))
+            assert parts.lengths.tolist() == [n + 1 + a for n, a in zip(lens, accepted)]
+            parts.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
+    whole.cache.check(), parts.cache.check()
+
+
+@gpu
+@pytest.mark.parametrize("kw", [dict(ffn=320, rows="int8", drafts=2, vocab=5000), dict(ffn=192, cache="bf16"),
+                                dict(drafts=1, vocab=40_000)], ids=str)
+def test_reference_sol_of_a_layer(kw):
+    """The command with the ops around the attention: the figures are the analyzer's, the trace is the calls'."""
+    import oracle
+    from paper_2609_40247_amd import reference as R
+    r = R.reference_sol(**{**dict(heads=4, kv_heads=2, head_dim=64, prompt=60, batch=3, prompts=2, steps=4, cache="int8", page_size=32), **kw})
+    names = R.OPS + (R.LAYER_OPS if "ffn" in kw else ()) + (("verify_drafts",) if "drafts" in kw else ())
+    assert list(r["ops"]) == list(names)
+    assert {k: o["calls"] for k, o in r["ops"].items()} == {
+        k: (1 if "prompt" in k else 4) * (2 if k.startswith("norm") else 1) for k in names}
+    for o in r["ops"].values():
+        assert o["ns"] > 0 and o["sol"] == max(o["mfu"], o["mbu"]) > 0
+    code, want = oracle.analyze(r["columns"], r["params"], gap_capacity=100)
+    assert code == 0
+    for k in ("op_sol", "opn_sol", "opn_time", "opn_flops", "opn_bytes"):
+        assert (want[k] == r["outputs"][k]).all(), k
+
+
+def test_counts_around_the_attention():
+    from types import SimpleNamespace
+
+    from paper_2609_40247_amd import reference as R
+    w = O.Weights4.quantise(torch.ones(64, 256), 128)
+    layer = SimpleNamespace(heads=4, kv_heads=2, head_dim=64, hidden=256, new_tokens=3, rows=None, weights=dict(qkv=w, gate=w, out=w),
+                            cache=SimpleNamespace(k=torch.zeros(1, dtype=BF), quantised=False))
+    assert R.counts(layer, "attn_decode", [10]) == (4 * 64 * 4 * (10 + 9 + 8), 2 * 3 * 4 * 64 * 2 + 2 * 10 * 2 * 128)
+    assert R.counts(layer, "norm_prompt", [5, 6]) == (6 * 11 * 256, 11 * 256 * 12 + 512)
+    weights = 64 * 128 + 64 * 2 * 4
+    assert R.counts(layer, "product_qkv_step", [9, 9]) == (2 * 6 * 64 * 256, weights + 6 * 512 + 6 * 128)
+    layer.rows = I8
+    assert R.counts(layer, "product_gate_step", [9, 9])[1] == weights + 6 * 260 + 6 * 64
+    assert R.counts(layer, "product_out_step", [9, 9])[1] == weights + 6 * 512 + 6 * 128
+    assert R.counts(layer, "norm_step", [9, 9])[1] == 6 * 256 * 11 + 512 + 24
+    assert R.counts(layer, "verify_drafts", [9, 9], 1000)[1] == 2 * (8000 + 2 * 32 + 16)
 
 
 # ------------------------------------------------------------ refusals
