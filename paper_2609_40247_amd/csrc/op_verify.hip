@@ -118,15 +118,17 @@ __device__ __forceinline__ void load_eight(const herschel_verify_args& a, const 
   load_row<TYPE>(a.target, r.target, at, end, x.p);
   if (r.differs && a.draft) load_row<TYPE>(a.draft, r.draft, at, end, x.q);
 }
-// What eight elements weigh: target - draft, or (alone) the target.
-__device__ __forceinline__ void weigh(const herschel_verify_args& a, const Row& r, int at, const Eight& x, double* both, double* alone) {
+// What eight elements weigh, target - draft where that is above 0 or the target alone, and their sum.
+__device__ __forceinline__ double weigh(const herschel_verify_args& a, const Row& r, int at, const Eight& x, double* w) {
+  double sum = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    alone[i] = x.p[i] > 0 ? (double)x.p[i] : 0.0;
     double d = (double)x.p[i];
     if (r.differs) d -= a.draft ? (double)x.q[i] : at + i == r.one ? 1.0 : 0.0;
-    both[i] = d > 0 ? d : 0.0;
+    w[i] = fmax(d, 0.0);  // 0 for a NaN
+    sum += w[i];
   }
+  return sum;
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -135,37 +137,32 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
-// A share's sums: of target - draft, and of the target.
+// What a share weighs.
 template <int TYPE>
 __global__ __launch_bounds__(VERIFY_THREADS) void k_verify_sums(VerifyArgs p) {
   const herschel_verify_args& a = p.a;
-  __shared__ double box[2][VERIFY_WAVES];
+  __shared__ double box[VERIFY_WAVES];
   const int64_t b = blockIdx.y;
   int n;
   const int accepted = accepted_drafts<TYPE>(a, b, n, blockIdx.x == 0 && threadIdx.x < WAVE);
   const Row r = row_of<TYPE>(a, b, n, accepted);
-  double s = 0, t = 0;
+  double s = 0;
   const int from = blockIdx.x * p.size, end = min(a.vocab, from + p.size);
   for (int at = from + (int)threadIdx.x * 8; at < end; at += SHARE_STEP) {
     Eight x;
-    double both[8], alone[8];
+    double w[8];
     load_eight<TYPE>(a, r, at, end, x);
-    weigh(a, r, at, x, both, alone);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s += both[i], t += alone[i];
+    s += weigh(a, r, at, x, w);
   }
   s = wave_sum(s);
-  t = wave_sum(t);
-  if (threadIdx.x % WAVE == 0) box[0][threadIdx.x / WAVE] = s, box[1][threadIdx.x / WAVE] = t;
+  if (threadIdx.x % WAVE == 0) box[threadIdx.x / WAVE] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    double* out = (double*)a.workspace + (b * p.shares + blockIdx.x) * 2;
-    s = t = 0;
-    for (int i = 0; i < VERIFY_WAVES; ++i) s += box[0][i], t += box[1][i];
-    out[0] = s;
-    out[1] = t;
+    s = 0;
+    for (int i = 0; i < VERIFY_WAVES; ++i) s += box[i];
+    ((double*)a.workspace)[b * p.shares + blockIdx.x] = s;
     if (blockIdx.x == 0) {
-      int* counted = (int*)((double*)a.workspace + (int64_t)a.n_seqs * p.shares * 2) + b * 2;
+      int* counted = (int*)((double*)a.workspace + (int64_t)a.n_seqs * p.shares) + b * 2;
       counted[0] = accepted;
       counted[1] = n;
     }
@@ -190,123 +187,57 @@ __device__ __forceinline__ int pick_lane(double v, double base, double than, dou
   return at;
 }
 
-// The token of each sequence, and the outputs.
-template <int TYPE, int THREADS, bool ONE>
-__global__ __launch_bounds__(THREADS) void k_verify_draw(VerifyArgs p) {
-  constexpr int WAVES = THREADS / WAVE, STEP = THREADS * 8;
-  const herschel_verify_args& a = p.a;
-  __shared__ double sums[2][WAVES];
-  const int64_t b = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid % WAVE, wave = tid / WAVE;
-  const double u = (double)a.final_u[b];
-  int n, accepted;
-  if constexpr (ONE) {
-    accepted = accepted_drafts<TYPE>(a, b, n, tid < WAVE);
-  } else {
-    const int* counted = (const int*)((const double*)a.workspace + (int64_t)a.n_seqs * p.shares * 2) + b * 2;
-    accepted = counted[0];
-    n = counted[1];
-  }
-  Row r = row_of<TYPE>(a, b, n, accepted);
-  int64_t* const out = a.out + b * (a.n_drafts + 1);
-  for (int t = tid; t <= a.n_drafts; t += THREADS)
-    if (t != accepted) out[t] = t < accepted ? a.tokens[b * a.n_drafts + t] : -1;
-  if (tid == 0) a.accepted[b] = accepted;
-
-  // the share, each wave by itself; a run of shares a lane
-  int from = 0, end = a.vocab;
-  double base = 0, than = 0;
-  bool alone = false;  // nothing of the target is above the draft
-  if constexpr (!ONE) {
-    const double* of = (const double*)a.workspace + b * p.shares * 2;
-    const int run = (p.shares + WAVE - 1) / WAVE, first = lane * run, last = min(p.shares, first + run);
-    double v[2] = {0, 0};
-    for (int i = first; i < last; ++i) v[0] += of[2 * i], v[1] += of[2 * i + 1];
-    const double all[2] = {wave_sum(v[0]), wave_sum(v[1])};
-    alone = !(all[0] > 0);
-    than = u * all[alone];
-    int share = -1;
-    const int at = pick_lane(v[alone], 0.0, than, base);
-    if (at >= 0) {
-      for (int i = at * run; i < min(p.shares, at * run + run); ++i) {  // the same in every lane
-        const double w = of[2 * i + alone];
-        if (!(w > 0)) continue;
-        if (share >= 0) base += of[2 * share + alone];
-        share = i;
-        if (base + w > than) break;
-      }
-    }
-    if (share < 0) {
-      if (tid == 0) {
-        out[accepted] = -1;
-        flag(a.status, HERSCHEL_OP_BAD_ROW);
-      }
-      return;
-    }
-    from = share * p.size;
-    end = min(a.vocab, from + p.size);
-    if (alone) r.differs = false;
-  }
-
-  // what each wave's run of the share weighs, `steps` times 512 elements
+// Draws from a row between two of its elements, as whole steps of a workgroup: each
+// wave's run of it is summed, the run found in which the sum behind `base` passes
+// `than` (u times the whole, with WHOLE), in it the step, the lane and the token,
+// which its lane writes.  False if nothing weighs anything.
+template <int TYPE, int WAVES, int KEPT, bool WHOLE>
+__device__ __forceinline__ bool draw_from(const herschel_verify_args& a, const Row& r, int from, int end, double base, double than,
+                                          double u, double* sums, int64_t* out) {
+  constexpr int STEP = WAVES * WAVE * 8;
+  const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
   const int steps = (end - from + STEP - 1) / STEP, begin = from + wave * steps * (WAVE * 8) + lane * 8;
-  constexpr int AT_ONCE = ONE ? ONE_ROW / STEP : 1;  // one workgroup has no more steps, and keeps their sums
-  Eight x[AT_ONCE];
-  double s[AT_ONCE], s_alone[AT_ONCE], sum = 0, sum_alone = 0;
-  auto lane_sums = [&](int i0) {
+  // rows of no more steps than these are read at once, and their sums kept
+  double s[KEPT], w[8], sum = 0;
+  if (steps <= KEPT) {
+    Eight x[KEPT];
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i)
-      if (i0 + i < steps) load_eight<TYPE>(a, r, begin + (i0 + i) * (WAVE * 8), end, x[i]);
+    for (int i = 0; i < KEPT; ++i)
+      if (i < steps) load_eight<TYPE>(a, r, begin + i * (WAVE * 8), end, x[i]);
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      s[i] = s_alone[i] = 0;
-      if (i0 + i >= steps) continue;
-      double both[8], one[8];
-      weigh(a, r, begin + (i0 + i) * (WAVE * 8), x[i], both, one);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s[i] += both[e], s_alone[i] += one[e];
+    for (int i = 0; i < KEPT; ++i) {
+      s[i] = i < steps ? weigh(a, r, begin + i * (WAVE * 8), x[i], w) : 0.0;
       sum += s[i];
-      sum_alone += s_alone[i];
     }
-  };
-  for (int i = 0; i < steps; i += AT_ONCE) lane_sums(i);
+  } else {
+    for (int i = 0; i < steps; ++i) {
+      Eight x;
+      load_eight<TYPE>(a, r, begin + i * (WAVE * 8), end, x);
+      sum += weigh(a, r, begin + i * (WAVE * 8), x, w);
+    }
+  }
   sum = wave_sum(sum);
-  if constexpr (ONE) sum_alone = wave_sum(sum_alone);
-  if (lane == 0) sums[0][wave] = sum, sums[1][wave] = sum_alone;
+  __syncthreads();  // what was in sums has been read
+  if (lane == 0) sums[wave] = sum;
   __syncthreads();
-  const bool counts = lane < WAVES;
-  if constexpr (ONE) {
-    const double all = wave_sum(counts ? sums[0][lane] : 0.0);
-    alone = !(all > 0);
-    than = u * (alone ? wave_sum(counts ? sums[1][lane] : 0.0) : all);
-    if (alone) r.differs = false;
-  }
+  const double of_wave = lane < WAVES ? sums[lane] : 0.0;
+  if constexpr (WHOLE) than = u * wave_sum(of_wave);
   double before = 0;
-  const int at = pick_lane(counts ? sums[ONE && alone][lane] : 0.0, base, than, before);
-  if (at < 0) {
-    if (tid == 0) {
-      out[accepted] = -1;
-      flag(a.status, HERSCHEL_OP_BAD_ROW);
-    }
-    return;
-  }
-  if (wave != at) return;
-  // its step, the lane in that, and the token
+  const int at = pick_lane(of_wave, base, than, before);
+  if (at < 0) return false;
+  if (wave != at) return true;
   int step = -1;
   double up = before, of_lane = 0;
   for (int i = 0; i < steps; ++i) {
     double v = 0;
-    if constexpr (ONE) {
+    if (steps <= KEPT) {
 #pragma unroll
-      for (int k = 0; k < AT_ONCE; ++k)
-        if (k == i) v = alone ? s_alone[k] : s[k];
+      for (int k = 0; k < KEPT; ++k)
+        if (k == i) v = s[k];
     } else {
-      Eight y;
-      double both[8], one[8];
-      load_eight<TYPE>(a, r, begin + i * (WAVE * 8), end, y);
-      weigh(a, r, begin + i * (WAVE * 8), y, both, one);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v += both[e];
+      Eight x;
+      load_eight<TYPE>(a, r, begin + i * (WAVE * 8), end, x);
+      v = weigh(a, r, begin + i * (WAVE * 8), x, w);
     }
     const double all = wave_sum(v);
     if (!(all > 0)) continue;
@@ -316,22 +247,81 @@ __global__ __launch_bounds__(THREADS) void k_verify_draw(VerifyArgs p) {
     up += all;
     if (up > than) break;
   }
-  if (lane != pick_lane(of_lane, before, than, up)) return;
-  Eight mine;
-  double w[8], unused[8];
-  const int first_of = begin + step * (WAVE * 8);
-  load_eight<TYPE>(a, r, first_of, end, mine);
-  weigh(a, r, first_of, mine, w, unused);
+  if (lane != pick_lane(of_lane, before, than, up)) return true;
+  Eight x;
+  const int first = begin + step * (WAVE * 8);
+  load_eight<TYPE>(a, r, first, end, x);
+  weigh(a, r, first, x, w);
   int token = -1;
   bool above = false;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (above || !(w[e] > 0)) continue;
-    token = first_of + e;
+    token = first + e;
     up += w[e];
     above = up > than;
   }
-  out[accepted] = token;
+  *out = token;
+  return true;
+}
+
+// The token of each sequence, and the outputs.
+template <int TYPE, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void k_verify_draw(VerifyArgs p) {
+  constexpr int WAVES = THREADS / WAVE;
+  const herschel_verify_args& a = p.a;
+  __shared__ double sums[WAVES];
+  const int64_t b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid % WAVE;
+  const double u = (double)a.final_u[b];
+  int n, accepted;
+  if constexpr (ONE) {
+    accepted = accepted_drafts<TYPE>(a, b, n, tid < WAVE);
+  } else {
+    const int* counted = (const int*)((const double*)a.workspace + (int64_t)a.n_seqs * p.shares) + b * 2;
+    accepted = counted[0];
+    n = counted[1];
+  }
+  Row r = row_of<TYPE>(a, b, n, accepted);
+  int64_t* const out = a.out + b * (a.n_drafts + 1);
+  for (int t = tid; t <= a.n_drafts; t += THREADS)
+    if (t != accepted) out[t] = t < accepted ? a.tokens[b * a.n_drafts + t] : -1;
+  if (tid == 0) a.accepted[b] = accepted;
+
+  bool drawn = false;
+  if constexpr (ONE) {
+    drawn = draw_from<TYPE, WAVES, 4, true>(a, r, 0, a.vocab, 0.0, 0.0, u, sums, out + accepted);
+  } else {
+    // the share, each wave by itself; a run of shares a lane
+    const double* of = (const double*)a.workspace + b * p.shares;
+    const int run = (p.shares + WAVE - 1) / WAVE, first = lane * run, last = min(p.shares, first + run);
+    double v = 0, base = 0;
+    for (int i = first; i < last; ++i) v += of[i];
+    const double than = u * wave_sum(v);
+    const int at = pick_lane(v, 0.0, than, base);
+    if (at >= 0) {
+      int share = -1;
+      for (int i = at * run; i < min(p.shares, at * run + run); ++i) {  // the same in every lane
+        const double w = of[i];
+        if (!(w > 0)) continue;
+        if (share >= 0) base += of[share];
+        share = i;
+        if (base + w > than) break;
+      }
+      drawn = draw_from<TYPE, WAVES, 2, false>(a, r, share * p.size, min(a.vocab, (share + 1) * p.size), base, than, u, sums,
+                                               out + accepted);
+    }
+  }
+  if (drawn) return;
+  // nothing of the target is above the draft: the target alone
+  if (r.differs) {
+    r.differs = false;
+    drawn = draw_from<TYPE, WAVES, 1, true>(a, r, 0, a.vocab, 0.0, 0.0, u, sums, out + accepted);
+  }
+  if (!drawn && tid == 0) {
+    out[accepted] = -1;
+    flag(a.status, HERSCHEL_OP_BAD_ROW);
+  }
 }
 
 inline int shares_of(int vocab, int n_seqs, int& size) {
@@ -346,7 +336,7 @@ extern "C" int herschel_verify_workspace(int32_t n_seqs, int32_t vocab, size_t* 
   using namespace hop;
   if (!bytes || n_seqs < 0 || n_seqs > 65535 || vocab < 1 || vocab > 0x40000000) return HERSCHEL_EINVAL;
   int size;
-  *bytes = vocab <= ONE_ROW ? 0 : (size_t)n_seqs * (shares_of(vocab, n_seqs, size) * 2 * sizeof(double) + 2 * sizeof(int));
+  *bytes = vocab <= ONE_ROW ? 0 : (size_t)n_seqs * (shares_of(vocab, n_seqs, size) * sizeof(double) + 2 * sizeof(int));
   return HERSCHEL_OK;
 }
 
