@@ -245,7 +245,7 @@ typedef struct {
   int64_t x_row;              /* elements from one row to the next, >= 0 */
   const float *x_scale;       /* 8 bits: [n_rows][ceil(k / group)] with x_group, else [n_rows] */
   void *out;                  /* [n_rows][n], gated [n_rows][n / 2], of type, contiguous */
-  int64_t n_rows;             /* >= 0; 0: nothing is done */
+  int64_t n_rows;             /* 0 ... HERSCHEL_MAX_PRODUCT_ROWS; 0: nothing is done */
   int32_t kind;               /* HERSCHEL_BF16 ... HERSCHEL_INT8 */
   int32_t x_group;            /* 8 bits: 0 or the weights' group */
   int32_t type;               /* HERSCHEL_BF16 or HERSCHEL_F16; that of rows of 16 bits */
@@ -254,6 +254,8 @@ typedef struct {
   size_t workspace_bytes;     /* fewer bytes: a product's columns are then not shared among more workgroups */
   void *hip_stream;
 } herschel_product_args;
+
+#define HERSCHEL_MAX_PRODUCT_ROWS 4194240
 
 /* Bytes of workspace with which a call of these sizes is fastest; 0 for most. */
 int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t gated, int32_t n, int32_t k, size_t *bytes);

@@ -32,7 +32,8 @@ extern "C" int herschel_product4(const herschel_product_args* args, const hersch
   if (w.k > 0x7fffff00 || w.n > 0x7ffffff0) return HERSCHEL_EINVAL;  // filled up they stay in 31 bits
   if (!w.codes || !w.scales || !aligned(w.codes, 16) || !aligned(w.scales, 16))
     return HERSCHEL_EINVAL;
-  if (!type_ok(a.type) || (a.kind != a.type && !quantised(a.kind)) || a.n_rows < 0 || a.x_row < 0) return HERSCHEL_EINVAL;
+  if (!type_ok(a.type) || (a.kind != a.type && !quantised(a.kind)) || a.x_row < 0) return HERSCHEL_EINVAL;
+  if (a.n_rows < 0 || a.n_rows > HERSCHEL_MAX_PRODUCT_ROWS) return HERSCHEL_EINVAL;
   if (a.x_group && (!quantised(a.kind) || a.x_group != w.group)) return HERSCHEL_EINVAL;
   if (a.gated && w.n % 32) return HERSCHEL_EINVAL;
   if (a.n_rows == 0) return HERSCHEL_OK;  // nothing to point at

@@ -437,8 +437,7 @@ __global__ __launch_bounds__(256) void k_product4_join(ProductArgs p) {
 template <class S>
 static int product_launch(ProductArgs& p, int splits) {  // at most 4
   const int tiles = p.a.gated ? p.half : p.tiles_n, each = S::WN * (p.a.gated ? S::NT / 2 : S::NT);
-  const int64_t blocks = (p.a.n_rows + S::ROWS - 1) / S::ROWS;
-  if (blocks > 65535) return HERSCHEL_EINVAL;
+  const int64_t blocks = (p.a.n_rows + S::ROWS - 1) / S::ROWS;  // at most 65535
   p.tiles_split = (p.tiles_k + splits - 1) / splits;
   p.splits = (p.tiles_k + p.tiles_split - 1) / p.tiles_split;
   const int rows = p.a.n_rows < S::ROWS ? (int)p.a.n_rows : S::ROWS, turns_all = (p.tiles_split + S::WK - 1) / S::WK;

@@ -38,7 +38,7 @@ KINDS = {**TYPES, torch.float8_e4m3fn: FP8, torch.int8: INT8}
 LAYOUTS = {"half": 0, "interleaved": 1}
 CODES = {torch.float8_e4m3fn: FP8, torch.int8: INT8}
 BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, BAD_TOKEN, BAD_ROW = 1, 2, 4, 8, 16, 32
-MAX_DECODE_SEQS, MAX_NORM_DIM, MAX_DRAFTS = 4096, 32768, 1024
+MAX_DECODE_SEQS, MAX_NORM_DIM, MAX_PRODUCT_ROWS, MAX_DRAFTS = 4096, 32768, 4_194_240, 1024
 _FAULTS = {BAD_PAGE: "a block table entry outside the cache", BAD_LENGTH: "lengths that do not fit the buffers",
            BAD_POSITION: "a position outside the rotary table", BAD_SLOT: "a slot beyond the cache's end",
            BAD_TOKEN: "a drafted token outside the vocabulary", BAD_ROW: "probabilities of which none is above 0"}
@@ -580,12 +580,14 @@ class Rows8(NamedTuple):
 
 def _row(t: torch.Tensor, name: str, shape: tuple, dtype, device: int) -> int:
     """The row stride of a tensor [rows, columns] of this type on this GPU, columns contiguous."""
-    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or t.stride(1) != 1 and shape[1] > 1:
-        _need(t.dtype == dtype, f"{name} must be {dtype}")
-        _need(t.get_device() == device, f"{name} must be on GPU {device}")
-        _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
-        _need(False, f"{name}'s last dimension must be contiguous")
-    return t.stride(0)
+    if t.dtype is dtype and t.get_device() == device and t.shape == shape:
+        row, step = t.stride()
+        if step == 1 or shape[1] < 2:
+            return row
+    _need(t.dtype == dtype, f"{name} must be {dtype}")
+    _need(t.get_device() == device, f"{name} must be on GPU {device}")
+    _need(tuple(t.shape) == tuple(shape), f"{name} must have shape {tuple(shape)}")
+    raise ValueError(f"{name}'s last dimension must be contiguous")
 
 
 def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | None = None, *, eps: float = 1e-6,
@@ -597,32 +599,37 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
     The norm is that of the sums in 32 bits, before they are rounded.  ``weight`` [columns] has x's type or is
     float32.  ``kind`` float8_e4m3fn or int8 asks for ``Rows8``, with a scale for each row, or for each ``group``
     (32, 64 or 128) of its columns; without it the result has x's type.  ``out`` is written where given."""
-    if not (x.is_cuda and x.dim() == 2 and x.dtype in TYPES and (x.stride(1) == 1 or x.shape[1] < 2)):
+    dev, dtype, shape, code = x.get_device(), x.dtype, x.shape, 0
+    if dev < 0 or dtype not in TYPES or len(shape) != 2 or x.stride(1) != 1 and shape[1] > 1:
         _need(x.dim() == 2, "x must have 2 dimensions")
         _rows(x, "x", 2)
-    dev, dtype, shape = x.get_device(), x.dtype, x.shape
     n, dim = shape
-    if not 1 <= dim <= MAX_NORM_DIM:
-        raise ValueError(f"rows must have 1 to {MAX_NORM_DIM} columns")
-    if not (0 <= eps < math.inf):
-        raise ValueError("eps must be finite and not negative")
-    if weight.dtype is not dtype and weight.dtype is not torch.float32:
+    if not (1 <= dim <= MAX_NORM_DIM and 0 <= eps < math.inf):
+        _need(1 <= dim <= MAX_NORM_DIM, f"rows must have 1 to {MAX_NORM_DIM} columns")
+        _need(False, "eps must be finite and not negative")
+    w_type = weight.dtype
+    if w_type is not dtype and w_type is not torch.float32:
         raise ValueError("weight must have x's type or be float32")
-    w = _ints(weight, "weight", weight.dtype, (dim,), dev)
+    w = _ints(weight, "weight", w_type, (dim,), dev)
     needs, given = x.requires_grad or weight.requires_grad, ()
     rp = rs = op = os = 0
+    r_type = dtype
     if residual is not None:
-        if residual.dtype is not dtype and residual.dtype is not torch.float32:
+        r_type = residual.dtype
+        if r_type is not dtype and r_type is not torch.float32:
             raise ValueError("residual must have x's type or be float32")
-        rp, rs = residual.data_ptr(), _row(residual, "residual", shape, residual.dtype, dev)
+        rp, rs = residual.data_ptr(), _row(residual, "residual", shape, r_type, dev)
+        needs = needs or residual.requires_grad
         if residual_out is None:
-            residual_out = residual
-        op, os = residual_out.data_ptr(), _row(residual_out, "residual_out", shape, residual.dtype, dev)
+            residual_out, op, os = residual, rp, rs
+        else:
+            op, os = residual_out.data_ptr(), _row(residual_out, "residual_out", shape, r_type, dev)
+            needs = needs or residual_out.requires_grad
         if os < dim:
             if n > 1:
                 raise ValueError("residual_out's rows must not overlap")
             os = dim
-        needs, given = needs or residual.requires_grad or residual_out.requires_grad, (residual_out,)
+        given = (residual_out,)
     elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
     scale = 0
@@ -635,7 +642,6 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
         else:
             to, given = _ints(out, "out", dtype, shape, dev), given + (out,)
             needs = needs or out.requires_grad
-        code = TYPES[dtype]
     else:
         if kind not in CODES:
             raise ValueError("kind must be float8_e4m3fn or int8")
@@ -644,14 +650,16 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
         code, groups = CODES[kind], (n, dim // group if group else 1)
         if out is None:
             out = Rows8(x.new_empty(shape, dtype=kind), x.new_empty(groups, dtype=torch.float32))
+            to, scale = out.codes.data_ptr(), out.scale.data_ptr()
         else:
+            to, scale = _ints(out[0], "out's codes", kind, shape, dev), _ints(out[1], "out's scale", torch.float32, groups, dev)
             given += (out[0], out[1])
-        to, scale = _ints(out[0], "out's codes", kind, shape, dev), _ints(out[1], "out's scale", torch.float32, groups, dev)
     if needs:
         _no_gradients("norm_rows")
-    args = _NORM.pack(x.data_ptr(), x.stride(0), rp, rs, op, os, w, to, scale, n, dim, group, TYPES[dtype],
-                      F32 if residual is not None and residual.dtype is torch.float32 else TYPES[dtype],
-                      F32 if weight.dtype is torch.float32 else TYPES[dtype], code, eps, _stream(dev))
+    plain = TYPES[dtype]
+    args = _NORM.pack(x.data_ptr(), x.stride(0), rp, rs, op, os, w, to, scale, n, dim, group, plain,
+                      plain if r_type is dtype else F32, plain if w_type is dtype else F32,
+                      plain if kind is None else code, eps, _stream(dev))
     _call((lib or _lib()).herschel_norm_rows, dev, "norm_rows", args)
     if given:
         _written(given)
@@ -782,6 +790,8 @@ def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False,
             raise ValueError("rows of 8 bits have a scale a row, [rows, 1], or one for each of the weights' groups")
         scales = _ints(scale, "scale", torch.float32, (n, groups), dev)
         x_group = weights.group if groups > 1 else 0
+    if n > MAX_PRODUCT_ROWS:
+        raise ValueError(f"at most {MAX_PRODUCT_ROWS} rows")
     if gated and weights.n % 32:
         raise ValueError("a gated product needs a multiple of 32 weight rows")
     if t.requires_grad or scale is not None and scale.requires_grad or out is not None and out.requires_grad:

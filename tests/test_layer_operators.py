@@ -169,6 +169,17 @@ def test_norm_rows_that_are_not_finite(kind, dim):
 
 
 @gpu
+def test_norm_rows_more_than_a_line_of_workgroups():
+    """More rows than a launch has workgroups across."""
+    x = rand(1, 64, seed=3).to(DEV).expand(2 ** 20 + 3, 64)
+    x = torch.cat([x, rand(2, 64, seed=4).to(DEV)])
+    w = rand(64, seed=5).to(DEV)
+    y = O.norm_rows(x, w)
+    assert torch.equal(y[-2:], O.norm_rows(x[-2:], w)) and (y[:-2] == y[0]).all()
+    assert torch.equal(y[:1], O.norm_rows(x[:1], w))
+
+
+@gpu
 def test_norm_rows_of_none_and_zeros():
     w = torch.ones(40, dtype=BF, device=DEV)
     assert O.norm_rows(torch.empty(0, 40, dtype=BF, device=DEV), w).shape == (0, 40)
@@ -784,7 +795,7 @@ def product_args(**kw):
 
 @pytest.mark.parametrize("bad,weights", [
     (dict(x=None), {}), (dict(out=None), {}), (dict(x=FAKE + 1), {}), (dict(out=FAKE + 1), {}), (dict(n_rows=-1), {}),
-    (dict(n_rows=1 << 40), {}), (dict(x_row=-1), {}), (dict(kind=O.F16), {}), (dict(kind=O.F32, type=O.F32), {}),
+    (dict(n_rows=4_194_241), {}), (dict(x_row=-1), {}), (dict(kind=O.F16), {}), (dict(kind=O.F32, type=O.F32), {}),
     (dict(kind=O.INT8), {}), (dict(kind=O.INT8, x_scale=FAKE + 2), {}), (dict(x_group=128), {}),
     (dict(kind=O.FP8, x_scale=FAKE, x_group=64), {}), (dict(gated=1), dict(n=48)), ({}, dict(codes=None)),
     ({}, dict(scales=None)), ({}, dict(codes=FAKE + 8)), ({}, dict(scales=FAKE + 4)), ({}, dict(n=0)), ({}, dict(k=0)),
