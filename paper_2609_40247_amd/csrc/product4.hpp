@@ -47,14 +47,12 @@ __device__ __forceinline__ typename Sum<KIND>::T mma(typename Operand<KIND>::T a
   else return mfma16<KIND>(a, b, c);
 }
 // The products of a group's operands: N of A, STEPS times 32 columns each, with one
-// B.  8-bit rows have wider instructions: 64 columns of whole numbers in the time of
+// B, added to d.  8-bit rows have wider instructions: 64 columns of whole numbers in the time of
 // 32 (16 cycles a SIMD), 128 of fp8 in that of 64.  A product waits for its
 // own last one: the N take turns.
 template <int KIND, int STEPS, int N>
 __device__ __forceinline__ void mma_group(typename Sum<KIND>::T* d, const typename Operand<KIND>::T (*a)[STEPS],
                                           const typename Operand<KIND>::T* b) {
-#pragma unroll
-  for (int t = 0; t < N; ++t) d[t] = typename Sum<KIND>::T{0, 0, 0, 0};
   if constexpr (KIND == HERSCHEL_FP8 && STEPS == 4) {
     const i32x8 v = {(int)b[0][0], (int)b[0][1], (int)b[1][0], (int)b[1][1],
                      (int)b[2][0], (int)b[2][1], (int)b[3][0], (int)b[3][1]};
@@ -185,6 +183,8 @@ __device__ __forceinline__ void add_columns(f32x4 (*sum)[S::NT], const Columns<S
       float by = 1.0f;
       if constexpr (S::GROUPS) by = lds_at<float>(scale_at + scale_part[i] + g * 4);
       typename Sum<KIND>::T d[NT + 1];
+#pragma unroll
+      for (int t = 0; t <= NT; ++t) d[t] = typename Sum<KIND>::T{0, 0, 0, 0};
       mma_group<KIND, STEPS, NT + 1>(d, codes, b);
       const float of_x = (float)d[NT][0];  // the sum of the lane's row of x, in the codes' unit
 #pragma unroll
@@ -223,11 +223,11 @@ __device__ __forceinline__ void copy_phase(const ProductArgs& p, char* to, int64
   const int K = p.w.k, k0 = tile0 * 128;
   const int shift = p.turns_log + __builtin_ctz(S::WK * S::CHUNKS), size = rows << shift, mask = (1 << shift) - 1;
   if (p.chunked && k0 + S::WK * p.turns * 128 <= K) {
-    const char* x = (const char*)a.x + (m0 * a.x_row + k0) * BYTES;  // 64 chunks are of one row
-    for (int id = copier * WAVE; id < size; id += S::COPY * WAVE) {
-      const int r = id >> shift;
-      const char* from = x + (r * a.x_row) * BYTES + (id & mask) * 16;
-      copy_to_lds(from + ((lane ^ (r & 7)) * 16), to + id * 16);
+    const int64_t step = S::COPY * a.x_row * BYTES;
+    for (int at = 0; at <= mask; at += WAVE) {  // a copy is of one row
+      const char* from = (const char*)a.x + ((m0 + copier) * a.x_row + k0) * BYTES + at * 16;
+      for (int r = copier; r < rows; r += S::COPY, from += step)
+        copy_to_lds(from + ((lane ^ (r & 7)) * 16), to + ((r << shift) + at) * 16);
     }
   } else {
 #pragma unroll 4
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product4(ProductArgs p) {
   if (wave >= S::WAVES) {
     // BUFFERS - 1 phases are under way or in use.  A wave's copies end in their order.
     const int phases = (turns_all + p.turns - 1) >> p.turns_log, copier = wave - S::WAVES;
-    const int copies = (rows * S::WK * p.turns * S::CHUNKS / WAVE + S::COPY - 1 - copier) / S::COPY;  // of a phase
+    const int copies = (rows + S::COPY - 1 - copier) / S::COPY * (S::WK * p.turns * S::CHUNKS / WAVE);  // of a phase
     for (int phase = 0; phase < p.buffers - 1 && phase < phases; ++phase)
       copy_phase<S>(p, (char*)parts + phase * bytes, m0, rows, tile0 + (phase * WK << p.turns_log), copier, lane);
     int to = p.buffers - 1;
