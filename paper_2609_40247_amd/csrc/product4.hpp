@@ -3,9 +3,11 @@
 //
 // y[m][n] = sum_g s[n][g] (sum_{k in g} c[n][k] x[m][k] - z[n][g] sum_{k in g} x[m][k]).
 // The codes enter the matrix cores as what they are, 0 to 15: as bytes they are
-// whole numbers, and read as fp8 they are c 2^-9 exactly (0 to 7 as its
-// subnormals, 8 to 15 as its first eight normals), so fp8 rows meet them as they
-// are and 16-bit rows after a conversion of fp8 pairs, which has an instruction.
+// whole numbers for int8 rows, and read as fp8 they are c 2^-9 exactly (0 to 7 as its
+// subnormals, 8 to 15 as its first eight normals), which an instruction turns into a
+// pair of 16-bit elements.  fp8 rows become half on the way, exactly: the matrix
+// cores' own fp8 products hold their sums to 2^-15 to 2^-19 of the magnitudes' sum
+// only, in 16 bits they are whole to 32.
 // The group's sum of x, which the zero needs, comes from one more product with a
 // constant operand; scale and zero meet the group's sums, not the weights.
 // The bytes of the weights bound large calls of few rows: four rows by a gated
@@ -32,41 +34,30 @@ struct ProductArgs {
 
 typedef u32x4 u32x4_any __attribute__((aligned(1)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// The 16-bit type that rows of a kind, other than int8, and their codes meet in.
+template <int KIND> constexpr int HALF_OF = KIND == HERSCHEL_FP8 ? HERSCHEL_F16 : KIND;
 
 template <int KIND> struct Sum { typedef f32x4 T; };
 template <> struct Sum<HERSCHEL_INT8> { typedef i32x4 T; };
 template <int KIND> struct Operand { typedef u32x4 T; };  // eight elements
-template <> struct Operand<HERSCHEL_FP8> { typedef u32x2 T; };
 template <> struct Operand<HERSCHEL_INT8> { typedef u32x2 T; };
 
 // D += A B of 32 columns: A the weights, 16 rows, B sixteen rows of x.
 template <int KIND>
 __device__ __forceinline__ typename Sum<KIND>::T mma(typename Operand<KIND>::T a, typename Operand<KIND>::T b,
                                                      typename Sum<KIND>::T c) {
-  if constexpr (KIND == HERSCHEL_FP8)
-    return __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
-  else if constexpr (KIND == HERSCHEL_INT8)
+  if constexpr (KIND == HERSCHEL_INT8)
     return __builtin_amdgcn_mfma_i32_16x16x32_i8(__builtin_bit_cast(long, a), __builtin_bit_cast(long, b), c, 0, 0, 0);
-  else return mfma16<KIND>(a, b, c);
+  else return mfma16<HALF_OF<KIND>>(a, b, c);
 }
 // The products of a group's operands: N of A, STEPS times 32 columns each, with one
-// B, added to d.  8-bit rows have wider instructions: 64 columns of whole numbers in the time of
-// 32 (16 cycles a SIMD), 128 of fp8 in that of 64.  A product waits for its
-// own last one: the N take turns.
+// B, added to d.  int8 rows have an instruction for 64 columns in the time of 32 (16
+// cycles a SIMD).  A product waits for its own last one: the N take turns.
 template <int KIND, int STEPS, int N>
 __device__ __forceinline__ void mma_group(typename Sum<KIND>::T* d, const typename Operand<KIND>::T (*a)[STEPS],
                                           const typename Operand<KIND>::T* b) {
-  if constexpr (KIND == HERSCHEL_FP8 && STEPS == 4) {
-    const i32x8 v = {(int)b[0][0], (int)b[0][1], (int)b[1][0], (int)b[1][1],
-                     (int)b[2][0], (int)b[2][1], (int)b[3][0], (int)b[3][1]};
-#pragma unroll
-    for (int t = 0; t < N; ++t) {
-      const i32x8 u = {(int)a[t][0][0], (int)a[t][0][1], (int)a[t][1][0], (int)a[t][1][1],
-                       (int)a[t][2][0], (int)a[t][2][1], (int)a[t][3][0], (int)a[t][3][1]};
-      d[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(u, v, d[t], 0, 0, 0, 0x7f7f7f7f, 0, 0x7f7f7f7f);
-    }
-  } else if constexpr (KIND == HERSCHEL_INT8 && STEPS > 1) {
+  if constexpr (KIND == HERSCHEL_INT8 && STEPS > 1) {
 #pragma unroll
     for (int j = 0; j < STEPS; j += 2) {
       const i32x4 v = {(int)b[j][0], (int)b[j][1], (int)b[j + 1][0], (int)b[j + 1][1]};
@@ -83,23 +74,25 @@ __device__ __forceinline__ void mma_group(typename Sum<KIND>::T* d, const typena
   }
 }
 
+// Eight fp8 as an operand.
+template <int KIND>
+__device__ __forceinline__ u32x4 of_fp8(uint32_t lo, uint32_t hi) {
+  constexpr int TO = HALF_OF<KIND>;
+  return u32x4{decode2<HERSCHEL_FP8, TO, false>(lo), decode2<HERSCHEL_FP8, TO, true>(lo),
+               decode2<HERSCHEL_FP8, TO, false>(hi), decode2<HERSCHEL_FP8, TO, true>(hi)};
+}
 // A word's eight codes as an operand: byte b holds columns b and b + 4.
 template <int KIND>
 __device__ __forceinline__ typename Operand<KIND>::T unpack_codes(uint32_t w) {
   const uint32_t lo = w & 0x0f0f0f0fu, hi = (w >> 4) & 0x0f0f0f0fu;
-  if constexpr (quantised(KIND)) return u32x2{lo, hi};
-  else
-    return u32x4{decode2<HERSCHEL_FP8, KIND, false>(lo), decode2<HERSCHEL_FP8, KIND, true>(lo),
-                 decode2<HERSCHEL_FP8, KIND, false>(hi), decode2<HERSCHEL_FP8, KIND, true>(hi)};
+  if constexpr (KIND == HERSCHEL_INT8) return u32x2{lo, hi};
+  else return of_fp8<KIND>(lo, hi);
 }
 // Ones in the codes' unit, in every place.
 template <int KIND>
 __device__ __forceinline__ typename Operand<KIND>::T ones() {
-  if constexpr (quantised(KIND)) return u32x2{0x01010101u, 0x01010101u};
-  else {
-    const uint32_t one = decode2<HERSCHEL_FP8, KIND, false>(0x0101u);
-    return u32x4{one, one, one, one};
-  }
+  if constexpr (KIND == HERSCHEL_INT8) return u32x2{0x01010101u, 0x01010101u};
+  else return of_fp8<KIND>(0x01010101u, 0x01010101u);
 }
 
 // The sizes of a kernel: up to ROWS rows of x and WN waves' NT tiles of 16 weight
@@ -183,7 +176,15 @@ __device__ __forceinline__ void add_columns(f32x4 (*sum)[S::NT], const Columns<S
       const uint32_t from = at + part[i];
       Op b[STEPS];
 #pragma unroll
-      for (int j = 0; j < STEPS; ++j) b[j] = lds_at<Op>(from ^ ((g * S::GROUP + j * 8) * (16 / S::EACH)));
+      for (int j = 0; j < STEPS; ++j) {
+        const uint32_t here = from ^ ((g * S::GROUP + j * 8) * (16 / S::EACH));
+        if constexpr (KIND == HERSCHEL_FP8) {
+          const u32x2 w = lds_at<u32x2>(here);
+          b[j] = of_fp8<KIND>(w[0], w[1]);
+        } else {
+          b[j] = lds_at<Op>(here);
+        }
+      }
       float by = 1.0f;
       if constexpr (S::GROUPS) by = lds_at<float>(scale_at + scale_part[i] + g * 4);
       typename Sum<KIND>::T d[NT + 1];
@@ -466,8 +467,8 @@ static int product_launch(ProductArgs& p, int splits) {  // at most 4
 // turns, so that one round of workgroups, at most one a CU, is best: with few weight
 // rows narrow ones, with many wide ones; with few weight rows and long columns these
 // are shared among several, joined by a second kernel.  The time of each choice
-// is estimated from measured ones (bf16 rows, groups of 128), in units of 10 ns: 400
-// and so much a turn, 400 for the join.  Measured against the choices beside them: 16
+// is estimated from measured ones (bf16 rows, groups of 128; two thirds for many int8 rows), in units of 10 ns: 400
+// and so much a turn, 600 for the join and its launch.  Measured against the choices beside them: 16
 // rows by 25600 x 5120 weights 17.3 us with 8 tiles a workgroup, 21.2 with 4, 29.5
 // with 2; by 6144 x 4096 7.9 with 2, 9.5 with 4, 11.6 with 1; by 1280 x 5120 7.2 with 1, 8.4 with 2; by 5120 x 25600 22.8 with 4 in three parts,
 // 26.4 with 2 and no parts; by 4096 x 14336 13.8 with 2 in two parts, 16.3 without.
@@ -491,8 +492,8 @@ inline Choice choose(const ProductArgs& p, size_t room) {
       if (splits > 1 && parts_bytes(p, splits) > room) break;
       const int each = (p.tiles_k + splits - 1) / splits, k = WAVES_K[rows == 64][wide];
       const int64_t rounds = (blocks * splits + 255) / 256, turns = (each + k - 1) / k;
-      const int turn = quantised(p.a.kind) && rows > 16 ? TURN[rows_at][wide] * 2 / 3 : TURN[rows_at][wide];
-      const int64_t time = rounds * (400 + turns * turn) + (splits > 1 ? 400 : 0);
+      const int turn = p.a.kind == HERSCHEL_INT8 && rows > 16 ? TURN[rows_at][wide] * 2 / 3 : TURN[rows_at][wide];
+      const int64_t time = rounds * (400 + turns * turn) + (splits > 1 ? 600 : 0);
       if (time < least) {
         least = time;
         best = Choice{wide, splits};

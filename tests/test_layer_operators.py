@@ -404,6 +404,33 @@ def test_product4_far_magnitudes():
         check_product(y, x.double(), w * s_gain, size * s_gain, 128, BF)
 
 
+@gpu
+@pytest.mark.parametrize("kind", ["rows", F8, I8], ids=str)
+def test_product4_sums_are_of_32_bits(kind):
+    """A few elements far larger than the rest, which meet weights of 0: their products are in the sums all the same,
+    less the zero's part, and what is lost there is lost from the result.  One group of whole products: the sums of its
+    codes are off by at most one rounding of 2^-24 of their magnitudes for each instruction's 32 or 64 columns and each
+    of the three steps behind, under 2^-20 in all with the zero's."""
+    n, k, rows = 160, 128, 16
+    codes, scales, zero, _, _ = make_weights(n, k, 128, True, HF, seed=5)
+    x = rand(rows, k, seed=6, dtype=HF)
+    large = [3, 40, 77, 126]
+    x[:, large] *= 64
+    c = torch.stack([codes & 15, codes >> 4], -1).view(n, -1)
+    c[:, large] = zero
+    codes = c[:, ::2] | (c[:, 1::2] << 4)
+    z, s = zero.double(), scales.double()
+    W = device_weights(codes, scales, zero, k)
+    if kind == "rows":
+        y, wide = O.product4(x.to(DEV), W), x.double()
+    else:
+        r = make_rows8(x, kind, 0)
+        y, wide = O.product4(O.Rows8(r.codes.to(DEV), r.scale.to(DEV)), W, dtype=HF), r.codes.double() * r.scale.double()
+    e = wide @ ((c.double() - z) * s).t()
+    size = wide.abs() @ ((c.double() + z) * s.abs()).t()
+    assert ((y.double().cpu() - e).abs() <= U[HF] * e.abs() + 2.0 ** -20 * size + TINY[HF]).all()
+
+
 def test_weights4_layout_and_quantise():
     """Every code where the layout says, the dense weights, and the quantiser's error: half a scale, on the CPU."""
     for n, k, group, zeros in ((40, 256, 128, True), (33, 301, 32, True), (5, 7, 128, False), (4100, 129, 64, True)):
