@@ -296,8 +296,8 @@ __device__ __forceinline__ void store_product(const herschel_product_args& a, co
 }
 
 // A workgroup takes the tiles that its shape says (gated: half of a wave's of the
-// rows that gate, half of those that they gate).  x comes through LDS in phases, two
-// in turn, which waves of their own bring: loads are waited for in their order, and
+// rows that gate, half of those that they gate).  x comes through LDS in phases, up
+// to six in turn, which waves of their own bring: loads are waited for in their order, and
 // x's between those of weights asked for long before would have these waited for too.
 // The weights go straight to registers, in no branch, so that the count of
 // what may still be under way is known.  The waves' sums meet in LDS.

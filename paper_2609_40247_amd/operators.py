@@ -679,6 +679,7 @@ class Weights4:
         n, half = codes.shape
         k = 2 * half if k is None else k
         _need(k >= 1 and (k + 1) // 2 == half, "codes must have k / 2 bytes a row, rounded up")
+        _need(n <= 2 ** 30 and k <= 2 ** 30, "at most 2^30 rows and columns")
         _need(scales.dtype in TYPES, "scales must be bfloat16 or float16")
         _need(scales.dim() == 2 and scales.shape[0] == n and scales.device == codes.device,
               "scales must be [n, groups], on the codes' device")
@@ -722,14 +723,15 @@ class Weights4:
         scales = torch.empty((n, groups), dtype=scale_dtype, device=weights.device)
         zero = torch.empty((n, groups), dtype=torch.uint8, device=weights.device) if zeros else None
         for at in range(0, n, 4096):
-            w = weights[at:at + 4096].float()
+            w = weights.detach()[at:at + 4096].float()
             w = torch.nn.functional.pad(w, (0, groups * group - k)).view(-1, groups, group)
             if zeros:
                 low, high = w.amin(-1).clamp_max(0), w.amax(-1).clamp_min(0)
                 s = (high / 15 - low / 15).to(scale_dtype)
             else:
                 s = (w.abs().amax(-1) / 7).to(scale_dtype)
-            inv = torch.where(s > 0, 1 / s.float(), 0.0)
+            _need(bool(torch.isfinite(s).all()), "weights must be finite, and their scales in the type's range")
+            inv = torch.where(s >= 2.0 ** -126, 1 / s.float(), 0.0)  # a group of next to nothing is 0
             z = (-low * inv).round().clamp(0, 15) if zeros else torch.full_like(inv, 8.0)
             c = (w * inv[..., None] + z[..., None]).round().clamp(0 if zeros else 1, 15).to(torch.uint8).view(-1, groups * group)
             c = torch.nn.functional.pad(c[:, :k], (0, k % 2))

@@ -452,6 +452,8 @@ def test_weights4_layout_and_quantise():
         # half a step; at the ends the scale's rounding on top: 7 or 15 steps of 2^-11, and the zero's half step
         assert ((W.dense().double() - x.double()).abs() <= s * (0.5 + 15 * 2.0 ** -11 + (0.5 if zeros else 0)) + 1e-12).all()
         assert (W.dense()[3, 64:128] == 0).all()
+        tiny = torch.full((16, 64), 1e-39)
+        assert (O.Weights4.quantise(tiny.requires_grad_(), zeros=zeros).dense() == 0).all()
 
 
 # ------------------------------------------------------------ verification of drafted tokens
@@ -826,7 +828,7 @@ def product_args(**kw):
     (dict(kind=O.INT8), {}), (dict(kind=O.INT8, x_scale=FAKE + 2), {}), (dict(x_group=128), {}),
     (dict(kind=O.FP8, x_scale=FAKE, x_group=64), {}), (dict(gated=1), dict(n=48)), ({}, dict(codes=None)),
     ({}, dict(scales=None)), ({}, dict(codes=FAKE + 8)), ({}, dict(scales=FAKE + 4)), ({}, dict(n=0)), ({}, dict(k=0)),
-    ({}, dict(k=0x7fffff80)), ({}, dict(group=16)), ({}, dict(group=256))], ids=str)
+    ({}, dict(k=(1 << 30) + 1)), ({}, dict(n=(1 << 30) + 1)), ({}, dict(group=16)), ({}, dict(group=256))], ids=str)
 def test_bad_product_calls_are_refused(bad, weights):
     assert lib().herschel_product4(ctypes.byref(product_args(**bad)), ctypes.byref(weights_struct(**weights))) == H.EINVAL
 
@@ -908,6 +910,11 @@ def test_tensor_checks_on_the_cpu():
             O.Weights4.quantise(rand(16, 64), **bad)
     with pytest.raises(ValueError):
         O.Weights4.quantise(torch.zeros(16, 64, dtype=torch.int32))
+    for value, zeros in ((math.nan, False), (math.inf, False), (-math.inf, True), (1e6, False)):
+        w = torch.zeros(40, 64)
+        w[33, 5] = value
+        with pytest.raises(ValueError, match="finite"):
+            O.Weights4.quantise(w, zeros=zeros, scale_dtype=HF)
 
 
 @gpu
