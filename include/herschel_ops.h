@@ -221,7 +221,9 @@ typedef struct {
  * type, y = h / sqrt(mean(h^2) + eps) * weight, from the h that is not rounded.
  * Squares of rows whose sum would leave 32 bits are summed scaled by a power of
  * two.  out = y rounded, or codes with the scale of the row or of each group of
- * columns, by the rule of a cache row. */
+ * columns, by the rule of a cache row.  residual_out may be residual or x, and a
+ * 16-bit out x, with the same rows; else what is written shares no memory with
+ * anything. */
 int herschel_norm_rows(const herschel_norm_args *args);
 
 /* A matrix [n][k] of 4-bit codes c, each worth (c - zero) * scale with the zero
@@ -262,7 +264,8 @@ int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t gated, int
 
 /* out[m] = sum over k of x[m][k] * weight[n][k], codes summed within a group
  * before they meet its scale, in 32 bits (int8 rows: whole numbers), rounded
- * once.  A row that holds an infinity or a NaN comes out as NaN. */
+ * once.  A row that holds an infinity or a NaN comes out as NaN.  out shares no
+ * memory with x or x_scale. */
 int herschel_product4(const herschel_product_args *args, const herschel_weights4 *weights);
 
 typedef struct {
@@ -280,7 +283,7 @@ typedef struct {
   int32_t *accepted;          /* [n_seqs] */
   int32_t n_seqs;             /* 0 ... 65535; 0: nothing is done */
   int32_t n_drafts;           /* 0 ... HERSCHEL_MAX_DRAFTS */
-  int32_t vocab;              /* >= 1 */
+  int32_t vocab;              /* 1 ... 2^30 */
   int32_t type;               /* HERSCHEL_F32, HERSCHEL_BF16 or HERSCHEL_F16 */
   void *workspace;            /* herschel_verify_workspace() bytes, 16-byte aligned, or NULL with 0; no two calls at once */
   size_t workspace_bytes;

@@ -598,7 +598,8 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
     ``residual`` has x's type or is float32; the sums go to ``residual_out``, without it back into ``residual``.
     The norm is that of the sums in 32 bits, before they are rounded.  ``weight`` [columns] has x's type or is
     float32.  ``kind`` float8_e4m3fn or int8 asks for ``Rows8``, with a scale for each row, or for each ``group``
-    (32, 64 or 128) of its columns; without it the result has x's type.  ``out`` is written where given."""
+    (32, 64 or 128) of its columns; without it the result has x's type.  ``out`` is written where given.  x can be
+    ``residual_out`` or a 16-bit ``out`` as well; else what is written shares no memory with the other tensors."""
     dev, dtype, shape, code = x.get_device(), x.dtype, x.shape, 0
     if dev < 0 or dtype not in TYPES or len(shape) != 2 or x.stride(1) != 1 and shape[1] > 1:
         _need(x.dim() == 2, "x must have 2 dimensions")
@@ -685,6 +686,8 @@ class Weights4:
               "scales must be [n, groups], on the codes' device")
         group = next((g for g in (128, 64, 32) if -(-k // g) == scales.shape[1]), 0)
         _need(group > 0, "scales must be one for each 32, 64 or 128 columns")
+        if scales.requires_grad:
+            _no_gradients("Weights4")
         if zeros is not None:
             _need(zeros.dtype == torch.uint8 and zeros.shape == scales.shape and zeros.device == codes.device,
                   "zeros must be uint8, like scales")
@@ -712,7 +715,8 @@ class Weights4:
     @classmethod
     def quantise(cls, weights: torch.Tensor, group: int = 128, *, zeros: bool = False, scale_dtype=None):
         """To the nearest codes: -7 to 7 times a group's scale, or with ``zeros`` 16 steps from its smallest weight
-        (or 0) to its largest (or 0).  ``scale_dtype``: that of 16-bit weights, else bfloat16."""
+        (or 0) to its largest (or 0), of the weights as they are: gradients end here.  ``scale_dtype``: that of 16-bit
+        weights, else bfloat16."""
         _need(weights.dim() == 2 and weights.numel() > 0 and weights.is_floating_point(), "weights must be [n, k] of numbers")
         _need(group in (32, 64, 128), "group must be 32, 64 or 128")
         scale_dtype = scale_dtype or (weights.dtype if weights.dtype in TYPES else torch.bfloat16)
@@ -765,7 +769,7 @@ def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False,
     [n, k]: [rows, n].  Gated, the first half of the weights' rows gates the second: silu(a) * b, [rows, n / 2].
 
     ``dtype`` is the result's: the type of 16-bit rows, else bfloat16 or float16 (bfloat16 if not given).  A row
-    that holds an infinity or a NaN comes out as NaN."""
+    that holds an infinity or a NaN comes out as NaN.  ``out`` shares no memory with x."""
     if isinstance(x, Rows8):
         t, scale = x
         if t.dtype not in CODES:

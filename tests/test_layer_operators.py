@@ -364,6 +364,13 @@ def test_product4_strides_and_outputs():
     O.product4(big[:, :260].to(DEV), device_weights(codes, scales, zero, 260), out=buffer[:21 * 40].view(21, 40))
     check_product(buffer[:21 * 40].view(21, 40), big[:, :260].double(), w, size, 64, BF)
     assert (buffer[21 * 40:] == 3).all()
+    both = torch.zeros(21 * (260 + 40), dtype=BF, device=DEV)  # rows and output side by side, and one over the other
+    both[:21 * 260] = big[:, :260].reshape(-1).to(DEV)
+    rows = both[:21 * 260].view(21, 260)
+    y = O.product4(rows, device_weights(codes, scales, zero, 260), out=both[21 * 260:].view(21, 40))
+    check_product(y, big[:, :260].double(), w, size, 64, BF)
+    with pytest.raises(ValueError):
+        O.product4(rows, device_weights(codes, scales, zero, 260), out=both[21 * 260 - 1:-1].view(21, 40))
     odd = torch.full((21 * 64 + 1,), 3.0, dtype=BF, device=DEV)[1:].view(21, 64)  # an output at an odd element
     codes, scales, zero, w, size = make_weights(64, 260, 64, True)
     check_product(O.product4(big[:, :260].to(DEV), device_weights(codes, scales, zero, 260), out=odd), big[:, :260].double(),
@@ -812,18 +819,23 @@ def test_bad_norm_calls_are_refused(bad):
     assert lib().herschel_norm_rows(ctypes.byref(norm_args(**bad))) == H.EINVAL
 
 
+APART = FAKE + (1 << 20)  # an output that is not the rows
+
+
 def weights_struct(**kw):
     a = dict(codes=FAKE, scales=FAKE, n=64, k=256, group=128)
     return O.HerschelWeights4(**{**a, **kw})
 
 
 def product_args(**kw):
-    a = dict(x=FAKE, x_row=256, out=FAKE, n_rows=4, kind=O.BF16, type=O.BF16)
+    a = dict(x=FAKE, x_row=256, out=APART, n_rows=4, kind=O.BF16, type=O.BF16)
     return O.HerschelProductArgs(**{**a, **kw})
 
 
 @pytest.mark.parametrize("bad,weights", [
-    (dict(x=None), {}), (dict(out=None), {}), (dict(x=FAKE + 1), {}), (dict(out=FAKE + 1), {}), (dict(n_rows=-1), {}),
+    (dict(x=None), {}), (dict(out=None), {}), (dict(x=FAKE + 1), {}), (dict(out=APART + 1), {}), (dict(n_rows=-1), {}),
+    (dict(out=FAKE), {}), (dict(out=FAKE + 2046), {}), (dict(out=FAKE - 510), {}), (dict(out=FAKE - 1022, gated=0, n_rows=8), {}),
+    (dict(kind=O.INT8, x_scale=APART + 508), {}), (dict(kind=O.INT8, x_scale=APART - 60, x_group=128, n_rows=8), {}),
     (dict(n_rows=4_194_241), {}), (dict(x_row=-1), {}), (dict(kind=O.F16), {}), (dict(kind=O.F32, type=O.F32), {}),
     (dict(kind=O.INT8), {}), (dict(kind=O.INT8, x_scale=FAKE + 2), {}), (dict(x_group=128), {}),
     (dict(kind=O.FP8, x_scale=FAKE, x_group=64), {}), (dict(gated=1), dict(n=48)), ({}, dict(codes=None)),
@@ -905,6 +917,11 @@ def test_tensor_checks_on_the_cpu():
         a = {**dict(codes=codes, scales=scales, zeros=None, k=None), **bad}
         with pytest.raises(ValueError):
             O.Weights4(a["codes"], a["scales"], a["zeros"], k=a["k"])
+    leaf = scales.clone().requires_grad_()
+    with pytest.raises(ValueError, match="no backward"):
+        O.Weights4(codes, leaf)
+    with torch.no_grad():
+        O.Weights4(codes, leaf)
     for bad in (dict(group=16), dict(scale_dtype=F32)):
         with pytest.raises(ValueError):
             O.Weights4.quantise(rand(16, 64), **bad)
