@@ -99,6 +99,7 @@ __device__ __forceinline__ typename Operand<KIND>::T ones() {
 // rows a workgroup, whose WK waves share the columns, 128 each in turn; a wave's
 // weights are asked for U times 128 columns ahead, and COPY waves bring x.
 // GROUPS: rows of 8 bits with a scale for each of the weights' groups.
+constexpr int PHASE_ALIGN = 128;
 template <int KIND_, bool GROUPS_, int GROUP_, int ROWS_, int NT_, int WN_, int WK_, int U_, int COPY_, int LDS_>
 struct Shape {
   static constexpr int KIND = KIND_, GROUP = GROUP_, ROWS = ROWS_, NT = NT_, WN = WN_, WK = WK_, U = U_, COPY = COPY_, LDS = LDS_;
@@ -109,12 +110,11 @@ struct Shape {
   static constexpr int EACH = quantised(KIND) ? 16 : 8;   // elements of a chunk of 16 bytes
   static constexpr int CHUNKS = 128 / EACH;               // of 128 columns of a row
   static constexpr int LEAST = WK * CHUNKS < WAVE ? WAVE / (WK * CHUNKS) : 1;  // turns of a phase: a copy is of one row
-  // LDS bytes of a phase, `turns` times 128 columns for each of WK waves
+  // LDS bytes of a phase, `turns` times 128 columns for each of WK waves, from one multiple of PHASE_ALIGN to another
   static __host__ __device__ constexpr int phase_bytes(int rows, int turns) {
-    return rows * WK * turns * (CHUNKS * 16 + (GROUPS ? PER * 4 : 0));
+    return (rows * WK * turns * (CHUNKS * 16 + (GROUPS ? PER * 4 : 0)) + PHASE_ALIGN - 1) & -PHASE_ALIGN;
   }
   static_assert((WK & (WK - 1)) == 0, "a row's chunks of a phase are counted by shifts");
-  static_assert(2 * ROWS * WK * LEAST * (CHUNKS * 16 + (GROUPS ? PER * 4 : 0)) <= LDS, "two phases must fit");
 };
 
 // What a wave reads of the weights for 128 columns.
@@ -143,7 +143,8 @@ __device__ __forceinline__ T lds_at(uint32_t address) {
 // order but for the lowest three bits of their number, which the row's turn, so
 // that sixteen rows' reads of one chunk meet every bank equally often.  The bits of the
 // rest of a column are apart from all these, and a phase and 128 columns of it
-// begin at multiples of 128 bytes.
+// begin at multiples of 128 bytes (the scales behind a phase's rows fill it up to one:
+// those of an odd number of rows in groups of 64 end in the middle).
 template <class S>
 __device__ __forceinline__ uint32_t lane_part(int row, int row_bytes, int lane) {
   return row * row_bytes + ((lane / 16 * S::RUN * (16 / S::EACH)) ^ ((row & 7) * 16));
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(S::THREADS) void k_product4(ProductArgs p) {
   constexpr int KIND = S::KIND, MT = S::MT, NT = S::NT, U = S::U, WK = S::WK;
   const herschel_product_args& a = p.a;
   const herschel_weights4& w = p.w;
-  extern __shared__ f32x4 parts[];
+  extern __shared__ __attribute__((aligned(PHASE_ALIGN))) f32x4 parts[];
   const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), wk = wave % WK, wn = wave / WK;
   const int64_t m0 = (int64_t)blockIdx.y * S::ROWS;
   const int rows = (int)min((int64_t)S::ROWS, a.n_rows - m0);
@@ -441,6 +442,7 @@ __global__ __launch_bounds__(256) void k_product4_join(ProductArgs p) {
 
 template <class S>
 static int product_launch(ProductArgs& p, int splits) {  // at most 4
+  static_assert(2 * S::phase_bytes(S::ROWS, S::LEAST) <= S::LDS, "two phases must fit");
   const int tiles = p.a.gated ? p.half : p.tiles_n, each = S::WN * (p.a.gated ? S::NT / 2 : S::NT);
   const int64_t blocks = (p.a.n_rows + S::ROWS - 1) / S::ROWS;  // at most 65535
   p.tiles_split = (p.tiles_k + splits - 1) / splits;
