@@ -16,8 +16,7 @@ extern "C" int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t
   p.tiles_n = (n + 15) / 16;
   p.tiles_k = (k + 127) / 128;
   p.half = n / 32;
-  // more rows than these fill the card without parts
-  const int splits = n_rows == 0 || n_rows > 4096 ? 1 : choose(p, SIZE_MAX).splits;
+  const int splits = n_rows == 0 ? 1 : choose(p, SIZE_MAX).splits;
   *bytes = splits > 1 ? parts_bytes(p, splits) : 0;
   return HERSCHEL_OK;
 }

@@ -480,7 +480,9 @@ struct Choice {
 };
 inline size_t parts_bytes(const ProductArgs& p, int splits) { return (size_t)splits * p.a.n_rows * p.tiles_n * 64; }
 inline int rows_at_once(int64_t n_rows) { return n_rows <= 16 ? 16 : n_rows <= 32 ? 32 : 64; }
+constexpr int64_t MOST_SHARED = 4096;  // rows whose columns are shared: more fill the card without, and are too many to join
 inline Choice choose(const ProductArgs& p, size_t room) {
+  if (p.a.n_rows > MOST_SHARED) room = 0;
   static const int TURN[3][4] = {{65, 95, 75, 65}, {0, 175, 105, 85}, {0, 156, 190, 135}}, WAVES_K[2][4] = {{8, 8, 4, 2}, {0, 4, 4, 2}};
   const int rows = rows_at_once(p.a.n_rows), rows_at = rows / 32;
   // a wave with one tile of weight rows has none that gates

@@ -77,3 +77,40 @@ def test_product4_of_rows_with_group_scales_in_wide_workgroups_and_parts(rows, n
     codes, scales, zero, w, size = make_weights(n, k, group, True, HF, seed=n)
     r, wide = group_rows(rows, k, kind, group, k)
     check_product(O.product4(r, device_weights(codes, scales, zero, k), dtype=HF), wide, w, size, group, HF)
+
+
+# ------------------------------------------------------------ workspaces
+def test_product4_shares_columns_only_where_the_workspace_says(fake):  # noqa: F811
+    """A workspace with room for more is used as the size that is asked for says: not at all beyond 4096 rows, whose
+    parts one launch could not join."""
+    sizes = child(fake, PRODUCT + """
+size = ctypes.c_size_t(0)
+for rows in (1, 64, 1000, 4096, 4097, 65_535, 65_536, 70_000, 4_194_240):
+    for n, k, gated in ((16, 25_600, 0), (64, 25_600, 1), (640, 128_000, 0), (16, 100, 0)):
+        assert lib.herschel_product4_workspace(ctypes.c_int64(rows), BF16, gated, n, k, ctypes.byref(size)) == 0
+        code, launched = product(rows, n, k, 128, gated=gated, workspace=1 << 50)
+        out.append((code, rows, size.value // (rows * -(-n // 16) * 64), [[int(v) for v in line[1:4]] for line in launched]))
+""")
+    assert {parts > 0 for code, rows, parts, _ in sizes if rows <= 4096} == {True, False}
+    for code, rows, parts, launched in sizes:
+        assert code == 0 and (parts == 0 or rows <= 4096)
+        assert len(launched) == (2 if parts else 1) and launched[0][2] == max(1, parts)
+        assert all(y <= 65_535 for _, y, _ in launched)
+
+
+@gpu
+def test_product4_of_many_rows_leaves_a_workspace_alone():
+    rows, n, k, group = 70_000, 16, 25_600, 128
+    codes, scales, zero, w, size = make_weights(n, k, group, True)
+    W = device_weights(codes, scales, zero, k)
+    x = rand(k + 8 * (rows - 1), seed=3)
+    given = x.to(DEV).as_strided((rows, k), (8, 1))  # each row 8 elements behind the one before
+    want = O.product4(given, W)
+    some = [0, 1, 4095, 4096, 65_535, 65_536, rows - 1]
+    check_product(want[some], torch.stack([x[8 * i:8 * i + k] for i in some]).double(), w, size, group, BF)
+    workspace = torch.full((4 * rows * 16,), 7.0, device=DEV)
+    out = torch.empty_like(want)
+    args = O._PRODUCT.pack(given.data_ptr(), 8, 0, out.data_ptr(), rows, O.BF16, 0, O.BF16, 0, workspace.data_ptr(),
+                           workspace.numel() * 4, torch.cuda.current_stream().cuda_stream)
+    assert O.load().herschel_product4(args, W._at) == 0
+    assert torch.equal(out, want) and (workspace == 7).all()
