@@ -223,7 +223,8 @@ typedef struct {
  * two.  out = y rounded, or codes with the scale of the row or of each group of
  * columns, by the rule of a cache row.  residual_out may be residual or x, and a
  * 16-bit out x, with the same rows; else what is written shares no memory with
- * anything. */
+ * anything (rows of one tensor may lie between those of another), or the call is
+ * refused. */
 int herschel_norm_rows(const herschel_norm_args *args);
 
 /* A matrix [n][k] of 4-bit codes c, each worth (c - zero) * scale with the zero

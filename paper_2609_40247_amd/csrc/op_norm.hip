@@ -312,6 +312,25 @@ extern "C" int herschel_norm_rows(const herschel_norm_args* args) {
   if (!a.x || !a.weight || !a.out || !aligned(a.x, 2) || !aligned(a.weight, a.weight_type == HERSCHEL_F32 ? 4 : 2))
     return HERSCHEL_EINVAL;
   if (quantised(a.out_kind) ? !a.scale || !aligned(a.scale, 4) : !aligned(a.out, 2)) return HERSCHEL_EINVAL;
+  // What is written is read by no other row's workgroup: it is the rows it stands for, element by element, or memory
+  // of its own.
+  const int64_t rows = a.n_rows, dim = a.dim, res = a.residual_type == HERSCHEL_F32 ? 4 : 2, out = quantised(a.out_kind) ? 1 : 2;
+  const int64_t groups = a.group ? dim / a.group : 1;
+  const RowsMemory x{a.x, rows, a.x_row * 2, dim * 2}, residual{a.residual, rows, a.residual_row * res, dim * res},
+      weight{a.weight, 1, 0, dim * (a.weight_type == HERSCHEL_F32 ? 4 : 2)},
+      written[3] = {{a.residual_out, rows, a.residual_out_row * res, dim * res}, {a.out, rows, dim * out, dim * out},
+                    {quantised(a.out_kind) ? a.scale : nullptr, rows, groups * 4, groups * 4}};
+  auto same = [&](const RowsMemory& u, const RowsMemory& v) {
+    return u.at == v.at && u.width == v.width && (u.step == v.step || rows == 1);
+  };
+  for (int i = 0; i < 3; ++i) {
+    const RowsMemory& w = written[i];
+    if (!(i < 2 && same(w, x)) && share_memory(w, x)) return HERSCHEL_EINVAL;
+    if (!(i < 1 && same(w, residual)) && share_memory(w, residual)) return HERSCHEL_EINVAL;
+    if (share_memory(w, weight)) return HERSCHEL_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (share_memory(w, written[j])) return HERSCHEL_EINVAL;
+  }
   NormArgs p{a};
   return a.type == HERSCHEL_BF16 ? norm_kind<HERSCHEL_BF16>(p) : norm_kind<HERSCHEL_F16>(p);
 }

@@ -228,6 +228,40 @@ inline int launch(void (*kernel)(Args), dim3 grid, dim3 block, size_t lds, void*
   return HERSCHEL_EDEVICE;
 }
 
+// Memory of a tensor of rows: `width` bytes each, `step` apart, >= 0.
+struct RowsMemory {
+  const void* at;
+  int64_t rows, step, width;
+};
+// Whether two tensors share a byte; rows of one may lie between those of the other.
+inline bool share_memory(RowsMemory a, RowsMemory b) {
+  int64_t begin[2], end[2];
+  RowsMemory* const of[2] = {&a, &b};
+  for (int i = 0; i < 2; ++i) {
+    RowsMemory& m = *of[i];
+    if (!m.at || m.rows < 1 || m.width < 1) return false;
+    begin[i] = (int64_t)(uintptr_t)m.at;
+    end[i] = begin[i] + (m.rows - 1) * m.step + m.width;
+    if (m.rows == 1 || m.step <= m.width) m = {m.at, 1, 1, end[i] - begin[i]};  // without gaps: one row
+  }
+  if (begin[0] >= end[1] || begin[1] >= end[0]) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  // Row j of b meets the bytes from..to iff begin + j step lies above from - width and below to.
+  auto meets = [](int64_t from, int64_t to, int64_t first, const RowsMemory& m, int64_t least, int64_t last) {
+    const int64_t above = from - m.width - first;
+    const int64_t j = above < 0 ? -((-above - 1) / m.step) : above / m.step + 1;  // the lowest j with j step > above
+    const int64_t k = j < least ? least : j;
+    return k <= last && first + k * m.step < to;
+  };
+  if (a.rows > 1 && b.rows > 1 && a.step == b.step)  // by the difference of the rows' numbers
+    return meets(begin[0], begin[0] + a.width, begin[1], b, 1 - a.rows, b.rows - 1);
+  const int few = a.rows <= b.rows ? 0 : 1;
+  const RowsMemory &f = *of[few], &m = *of[1 - few];
+  for (int64_t i = 0; i < f.rows; ++i)
+    if (meets(begin[few] + i * f.step, begin[few] + i * f.step + f.width, begin[1 - few], m, 0, m.rows - 1)) return true;
+  return false;
+}
+
 inline bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 inline bool type_ok(int t) { return t == HERSCHEL_BF16 || t == HERSCHEL_F16; }
 inline bool strides_ok(const herschel_strides& s) { return s.row >= 0 && s.head >= 0; }

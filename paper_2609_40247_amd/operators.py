@@ -599,7 +599,7 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
     The norm is that of the sums in 32 bits, before they are rounded.  ``weight`` [columns] has x's type or is
     float32.  ``kind`` float8_e4m3fn or int8 asks for ``Rows8``, with a scale for each row, or for each ``group``
     (32, 64 or 128) of its columns; without it the result has x's type.  ``out`` is written where given.  x can be
-    ``residual_out`` or a 16-bit ``out`` as well; else what is written shares no memory with the other tensors."""
+    ``residual_out`` or a 16-bit ``out`` as well; calls in which what is written shares other memory are refused."""
     dev, dtype, shape, code = x.get_device(), x.dtype, x.shape, 0
     if dev < 0 or dtype not in TYPES or len(shape) != 2 or x.stride(1) != 1 and shape[1] > 1:
         _need(x.dim() == 2, "x must have 2 dimensions")

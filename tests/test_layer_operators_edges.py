@@ -3,6 +3,9 @@ goes another way than its neighbours.  Tolerances are those of
 ``test_layer_operators``, derived there."""
 from __future__ import annotations
 
+import json
+import random
+
 import pytest
 import torch
 
@@ -24,6 +27,20 @@ def product(rows, n, k, group, kind=BF16, x_group=0, gated=0, workspace=0, x=1 <
                     0 if kind > 1 else kind, gated, 1 << 54 if workspace else 0, workspace, 0)
     code = lib.herschel_product4(a, w)
     return code, [line.split()[1:8] for line in log() if line.startswith("launch ")]  # name, grid, threads, "lds", bytes
+'''
+
+
+NORM = '''
+import struct
+device()
+BF16, F16, FP8, INT8, F32 = 0, 1, 2, 3, 4
+
+def norm(n, dim, x, x_row, out, residual=0, residual_row=0, kept=0, kept_row=0, weight=1 << 40, scale=0, group=0, residual_type=BF16,
+         weight_type=BF16, kind=BF16):
+    a = struct.pack("@PqPqPq3Pq6ifP", x, x_row, residual, residual_row, kept, kept_row, weight, out, scale, n, dim, group, BF16,
+                    residual_type, weight_type, kind, 1e-6, 0)
+    code = lib.herschel_norm_rows(a)
+    return code, sum(line.startswith("launch ") for line in log())
 '''
 
 
@@ -114,3 +131,108 @@ def test_product4_of_many_rows_leaves_a_workspace_alone():
                            workspace.numel() * 4, torch.cuda.current_stream().cuda_stream)
     assert O.load().herschel_product4(args, W._at) == 0
     assert torch.equal(out, want) and (workspace == 7).all()
+
+
+# ------------------------------------------------------------ what is written over what is read
+def norm_memory(rng):
+    """A small norm call with its tensors close together, and whether it is to be refused: from the bytes of each."""
+    n, dim = rng.choice([1, 2, 3, 7]), rng.choice([1, 2, 5, 32])
+    kind = rng.choice([0, 0, 0, 2, 3])
+    group = 32 if kind and dim == 32 and rng.random() < 0.5 else 0
+    residual_type = rng.choice([0, 0, 4]) if rng.random() < 0.7 else None
+    e = 4 if residual_type == 4 else 2
+    base = 1 << 20
+    room = rng.choice([200, 1000, 8000])
+
+    def at(align):
+        return base + rng.randrange(room) // align * align
+    steps = [dim, dim + 1, dim + 8, 2 * dim, 3 * dim, 100]
+    c = dict(n=n, dim=dim, x=at(2), x_row=rng.choice([0, 1] + steps), out=at(1 if kind else 2), weight=at(4), kind=kind, group=group,
+             weight_type=rng.choice([0, 4]), scale=at(4) if kind else 0)
+    if residual_type is not None:
+        c.update(residual=at(e), residual_row=rng.choice([0, 1] + steps), residual_type=residual_type)
+        if rng.random() < 0.8:
+            c.update(kept=at(e), kept_row=rng.choice(steps))
+    # the same rows, now and then
+    if rng.random() < 0.3:
+        c.update(out=c["x"], x_row=rng.choice([dim, c["x_row"]]))
+    if "kept" in c and rng.random() < 0.4:
+        c.update(residual=c["kept"], residual_row=rng.choice([c["kept_row"], c["residual_row"]]))
+    elif "kept" in c and e == 2 and rng.random() < 0.4:
+        c.update(x=c["kept"], x_row=rng.choice([c["kept_row"], c["x_row"]]))
+
+    def rows(start, step, width, size):
+        return [range(start + r * step * size, start + (r * step + width) * size) for r in range(n)]
+    read = dict(x=rows(c["x"], c["x_row"], dim, 2), weight=[range(c["weight"], c["weight"] + dim * (4 if c["weight_type"] else 2))])
+    written = dict(out=rows(c["out"], dim, dim, 1 if kind else 2))
+    if kind:
+        groups = dim // group if group else 1
+        written["scale"] = rows(c["scale"], groups, groups, 4)
+    if "residual" in c:
+        read["residual"] = rows(c["residual"], c["residual_row"], dim, e)
+    if "kept" in c:
+        written["kept"] = rows(c["kept"], c["kept_row"], dim, e)
+    sets = {k: {b for r in v for b in r} for k, v in {**read, **written}.items()}
+    bad = False
+    for w in written:
+        for o in [*read, *written]:
+            same = (w, o) in (("kept", "residual"), ("kept", "x"), ("out", "x")) and written[w] == read[o]
+            bad |= w != o and not same and bool(sets[w] & sets[o])
+    return c, bad
+
+
+def test_norm_rows_over_other_rows_are_refused(fake, tmp_path):  # noqa: F811
+    """What is written may be the rows that it stands for; any other byte that it shares with what is read, or written
+    as well, would be read before or after it changes.  Rows between another tensor's rows are none."""
+    rng = random.Random(1)
+    cases = [norm_memory(rng) for _ in range(6000)]
+    (tmp_path / "cases.json").write_text(json.dumps([c for c, _ in cases]))
+    codes = child(fake, NORM + f"out += [norm(**c) for c in json.load(open({str(tmp_path / 'cases.json')!r}))]\n")
+    bad = [b for _, b in cases]
+    assert 500 < sum(bad) < 5500 and codes == [[-1, 0] if b else [0, 1] for b in bad]
+
+
+def test_norm_rows_beside_other_rows(fake):  # noqa: F811
+    """Tensors that are columns of one buffer, of many rows: shifted by an element they are refused."""
+    codes = child(fake, NORM + """
+n, dim, X = 2_000_000, 64, 1 << 30
+for shift in (0, 128, 130, 126, -128, -126, 256, 258):
+    for step in (192, 191, 193, 384, 100):  # of the residual's rows; those of x lie 192 elements apart
+        out.append((shift, step, norm(n, dim, X, 192, 1 << 50, X + shift, step, X + shift, step)[0]))
+out.append((0, 0, norm(n, dim, X, dim, X)[0]))
+out.append((2, 0, norm(n, dim, X, dim, X + 2)[0]))
+out.append((2, 0, norm(n, dim, X, dim, X + n * dim * 2 - 2)[0]))
+out.append((0, 0, norm(n, dim, X, dim, X + n * dim * 2)[0]))
+""")
+    for shift, step, code in codes:
+        # x's rows take 128 of every 384 bytes; those of the residual fit between them if they keep their place in it
+        between = step in (192, 384) and 128 <= shift % 384 <= 256
+        fine = shift == 0 if step == 0 else between or (step, shift) == (192, 0)
+        assert (code == 0) == fine, (shift, step)
+
+
+@gpu
+def test_norm_rows_in_shared_buffers():
+    """Rows, sums and residual as columns of one buffer, and a residual stream that is the rows; shifted ones are refused."""
+    n, dim = 37, 264
+    big, w = rand(n, 3 * dim, seed=1, dtype=HF).to(DEV), rand(dim, seed=2, dtype=HF).to(DEV)
+    x, r, kept = big[:, :dim], big[:, dim:2 * dim], big[:, 2 * dim:]
+    sums = torch.empty(n, dim, dtype=HF, device=DEV)
+    want = O.norm_rows(x.clone(), w, r.clone(), residual_out=sums)
+    before = big.clone()
+    assert torch.equal(O.norm_rows(x, w, r, residual_out=kept), want)
+    assert torch.equal(kept, sums) and torch.equal(big[:, :2 * dim], before[:, :2 * dim])
+    assert torch.equal(O.norm_rows(x, w, r, residual_out=x), want) and torch.equal(x, sums)
+    twice = O.norm_rows(r.clone(), w, r.clone())
+    assert torch.equal(O.norm_rows(r, w, r), twice)  # a stream that is the rows
+    before = big.clone()
+    line = big.view(-1)
+    for bad in (dict(residual=r, residual_out=big[:, 1:dim + 1]), dict(residual=r, residual_out=big[:, dim + 1:2 * dim + 1]),
+                dict(out=line[:n * dim].view(n, dim)), dict(residual=x, out=line[2 * dim + 1:][:n * dim].view(n, dim)),
+                dict(kind=I8, out=O.Rows8(line.view(I8)[:n * dim].view(n, dim), torch.empty(n, 1, device=DEV))),
+                dict(x=line[:n * dim].view(n, dim), out=line[1:n * dim + 1].view(n, dim)),
+                dict(x=line[:n * dim].view(n, dim), residual=r.clone(), out=line[:n * dim].view(n, dim), residual_out=line[:n * dim].view(n, dim)),
+                dict(weight=line[:dim], x=r, out=line[:n * dim].view(n, dim))):
+        with pytest.raises(ValueError):
+            O.norm_rows(**{**dict(x=x, weight=w), **bad})
+    assert torch.equal(big, before)
