@@ -266,7 +266,8 @@ int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t gated, int
 /* out[m] = sum over k of x[m][k] * weight[n][k], codes summed within a group
  * before they meet its scale, in 32 bits (int8 rows: whole numbers), rounded
  * once.  A row that holds an infinity or a NaN comes out as NaN.  out shares no
- * memory with x or x_scale. */
+ * memory with x, x_scale or the weights (it may lie between rows of x), or the call
+ * is refused. */
 int herschel_product4(const herschel_product_args *args, const herschel_weights4 *weights);
 
 typedef struct {

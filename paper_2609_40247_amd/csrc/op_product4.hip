@@ -38,14 +38,14 @@ extern "C" int herschel_product4(const herschel_product_args* args, const hersch
   if (a.n_rows == 0) return HERSCHEL_OK;  // nothing to point at
   if (!a.x || !a.out || !aligned(a.out, 2) || !aligned(a.x, quantised(a.kind) ? 1 : 2)) return HERSCHEL_EINVAL;
   if (quantised(a.kind) && (!a.x_scale || !aligned(a.x_scale, 4))) return HERSCHEL_EINVAL;
-  // a row of x is read by many workgroups, some after others have written
-  auto over_out = [&](const void* p, int64_t bytes) {
-    const int64_t out = (int64_t)(uintptr_t)a.out, from = (int64_t)(uintptr_t)p;
-    return from < out + a.n_rows * (a.gated ? w.n / 2 : w.n) * 2 && out < from + bytes;
-  };
-  const int64_t groups = a.x_group ? (w.k + w.group - 1) / w.group : 1;
-  if (over_out(a.x, ((a.n_rows - 1) * a.x_row + w.k) * (quantised(a.kind) ? 1 : 2))) return HERSCHEL_EINVAL;
-  if (quantised(a.kind) && over_out(a.x_scale, a.n_rows * groups * 4)) return HERSCHEL_EINVAL;
+  // a row of x and a tile of the weights are read by many workgroups, some after others have written
+  const int64_t e = quantised(a.kind) ? 1 : 2, groups = a.x_group ? (w.k + w.group - 1) / w.group : 1;
+  const int64_t tiles = (int64_t)((w.k + 127) / 128) * ((w.n + 15) / 16), row = (int64_t)(a.gated ? w.n / 2 : w.n) * 2;
+  const RowsMemory out{a.out, a.n_rows, row, row};
+  if (share_memory(out, {a.x, a.n_rows, a.x_row * e, w.k * e})) return HERSCHEL_EINVAL;
+  if (quantised(a.kind) && share_memory(out, {a.x_scale, a.n_rows, groups * 4, groups * 4})) return HERSCHEL_EINVAL;
+  if (share_memory(out, {w.codes, tiles, 1024, 1024}) || share_memory(out, {w.scales, tiles, 8192 / w.group, 8192 / w.group}))
+    return HERSCHEL_EINVAL;
   ProductArgs p{};
   p.a = a;
   p.w = w;

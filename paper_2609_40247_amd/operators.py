@@ -769,7 +769,7 @@ def product4(x: torch.Tensor | Rows8, weights: Weights4, *, gated: bool = False,
     [n, k]: [rows, n].  Gated, the first half of the weights' rows gates the second: silu(a) * b, [rows, n / 2].
 
     ``dtype`` is the result's: the type of 16-bit rows, else bfloat16 or float16 (bfloat16 if not given).  A row
-    that holds an infinity or a NaN comes out as NaN.  ``out`` shares no memory with x."""
+    that holds an infinity or a NaN comes out as NaN.  ``out`` shares no memory with x or the weights."""
     if isinstance(x, Rows8):
         t, scale = x
         if t.dtype not in CODES:

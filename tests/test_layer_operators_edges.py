@@ -236,3 +236,40 @@ def test_norm_rows_in_shared_buffers():
         with pytest.raises(ValueError):
             O.norm_rows(**{**dict(x=x, weight=w), **bad})
     assert torch.equal(big, before)
+
+
+def test_product4_over_what_it_reads_is_refused(fake):  # noqa: F811
+    """An output over rows, their scales or the weights; between rows that lie far apart there is room for one."""
+    codes = child(fake, PRODUCT + """
+X, rows, n, k = 1 << 40, 5, 48, 256  # an output of 480 bytes, rows of 512 (8 bits: 256), 6 KB of codes, 48 x 2 words of scales
+for kind, e in ((BF16, 2), (INT8, 1)):
+    for x_row in (k, 1024):
+        for at in range(-600, 6000, 2):
+            out.append((kind, at, [(r * x_row * e, r * x_row * e + k * e) for r in range(rows)],
+                        product(rows, n, k, 128, kind, x_row=x_row, x=X, out=X + at)[0]))
+S = 1 << 51
+for at in range(-600, 200, 2):
+    out.append((INT8, at, [(0, rows * 2 * 4)], product(rows, n, k, 128, INT8, x_group=128, x_scale=S, out=S + at)[0]))
+for at in range(-600, 6800, 2):
+    out.append((BF16, at, [(0, 6144)], product(rows, n, k, 128, codes=S, out=S + at)[0]))
+    out.append((BF16, at, [(0, 48 * 2 * 4)], product(rows, n, k, 128, scales=S, out=S + at)[0]))
+""")
+    refused = 0
+    for kind, at, read, code in codes:
+        over = any(a < at + 480 and at < b for a, b in read)
+        assert code == (-1 if over else 0), (kind, at, read)
+        refused += over
+    assert 1000 < refused < len(codes) - 1000
+
+
+@gpu
+def test_product4_between_rows():
+    """An output that lies between rows of x, which it leaves alone."""
+    codes, scales, zero, w, size = make_weights(48, 256, 64, True)
+    W = device_weights(codes, scales, zero, 256)
+    big = rand(5, 1024, seed=8).to(DEV)
+    before = big.clone()
+    out = big[2, 300:300 + 5 * 48].view(5, 48)
+    check_product(O.product4(big[:, :256], W, out=out), before[:, :256].cpu().double(), w, size, 64, BF)
+    before[2, 300:540] = big[2, 300:540]
+    assert torch.equal(big, before)
