@@ -567,15 +567,19 @@ class DecodeAttention:
 # ------------------------------------------------------------ around the attention
 class Rows8(NamedTuple):
     """Rows of 8-bit codes [rows, columns], float8_e4m3fn or int8, each worth itself times its scale, float32
-    [rows, 1] or [rows, groups of columns]."""
+    [rows, 1] or [rows, groups of columns].  The group is the one, of 128, 64 or 32 columns, of which a row has as many
+    as there are scales; the last may have fewer."""
     codes: torch.Tensor
     scale: torch.Tensor
 
     def values(self) -> torch.Tensor:
         """The rows in 32 bits."""
-        rows, columns = self.codes.shape
-        groups = self.scale.shape[1]
-        return (self.codes.float().view(rows, groups, columns // groups) * self.scale[..., None]).view(rows, columns)
+        columns, groups = self.codes.shape[1], self.scale.shape[1]
+        group = columns if groups == 1 else next((g for g in (128, 64, 32) if -(-columns // g) == groups), 0)
+        if not group:  # equal parts of another size
+            _need(groups > 0 and columns % groups == 0, "scale must be one a row, or one for each 32, 64 or 128 columns")
+            group = columns // groups
+        return self.codes.float() * self.scale.repeat_interleave(group, 1)[:, :columns]
 
 
 def _row(t: torch.Tensor, name: str, shape: tuple, dtype, device: int) -> int:

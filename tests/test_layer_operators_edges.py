@@ -80,6 +80,7 @@ def test_product4_of_rows_with_group_scales(rows, group, kind):
         codes, scales, zero, w, size = make_weights(96, k, group, True, seed=k)
         W = device_weights(codes, scales, zero, k)
         r, wide = group_rows(rows, k, kind, group, rows)
+        assert torch.equal(r.values().cpu(), wide.float())
         for gated in (False, True):
             check_product(O.product4(r, W, gated=gated), wide, w, size, group, BF, gated)
 
@@ -273,3 +274,20 @@ def test_product4_between_rows():
     check_product(O.product4(big[:, :256], W, out=out), before[:, :256].cpu().double(), w, size, 64, BF)
     before[2, 300:540] = big[2, 300:540]
     assert torch.equal(big, before)
+
+
+# ------------------------------------------------------------ 8-bit rows as numbers
+@pytest.mark.parametrize("columns,group", [(200, 64), (1500, 128), (1500, 64), (1500, 32), (96, 32), (64, 64), (130, 128), (40, 32),
+                                           (512, 64), (7, 0), (200, 0), (512, 256)])
+def test_rows8_values_of_a_shorter_last_group(columns, group):
+    """The groups are those that a product takes the scales for: of 32, 64 or 128 columns, the last with what is left."""
+    r = O.Rows8(rand(3, columns, seed=1, gain=40.0).to(I8), 2.0 ** (torch.arange(3 * -(-columns // (group or columns))) % 11 - 5.0).view(3, -1))
+    want = torch.empty(3, columns)
+    for j in range(columns):
+        want[:, j] = r.codes[:, j].float() * r.scale[:, j // (group or columns)]
+    assert torch.equal(r.values(), want)
+
+
+def test_rows8_values_of_scales_that_fit_no_group():
+    with pytest.raises(ValueError, match="scale"):
+        O.Rows8(torch.zeros(3, 200, dtype=I8), torch.ones(3, 3)).values()
