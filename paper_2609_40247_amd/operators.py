@@ -659,6 +659,7 @@ def norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor | No
         else:
             to, scale = _ints(out[0], "out's codes", kind, shape, dev), _ints(out[1], "out's scale", torch.float32, groups, dev)
             given += (out[0], out[1])
+            needs = needs or out[1].requires_grad
     if needs:
         _no_gradients("norm_rows")
     plain = TYPES[dtype]

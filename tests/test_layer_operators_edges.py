@@ -291,3 +291,15 @@ def test_rows8_values_of_a_shorter_last_group(columns, group):
 def test_rows8_values_of_scales_that_fit_no_group():
     with pytest.raises(ValueError, match="scale"):
         O.Rows8(torch.zeros(3, 200, dtype=I8), torch.ones(3, 3)).values()
+
+
+@gpu
+def test_norm_rows_refuses_scales_that_require_gradients():
+    """An output of 8-bit rows whose scales are a leaf would be cut off from the rows without a word, as any other."""
+    x, w = rand(4, 64).to(DEV), rand(64).to(DEV)
+    out = O.Rows8(torch.zeros(4, 64, dtype=I8, device=DEV), torch.zeros(4, 1, device=DEV, requires_grad=True))
+    with pytest.raises(ValueError, match="no backward"):
+        O.norm_rows(x, w, kind=I8, out=out)
+    with torch.no_grad():
+        O.norm_rows(x, w, kind=I8, out=out)
+    assert torch.equal(out.scale.detach(), O.norm_rows(x, w, kind=I8).scale)
