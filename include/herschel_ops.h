@@ -239,9 +239,11 @@ int herschel_norm_rows(const herschel_norm_args *args);
 typedef struct {
   const void *codes;          /* 16-byte aligned */
   const uint32_t *scales;     /* 16-byte aligned */
-  int32_t n, k;               /* 1 ... 2^30 */
+  int32_t n, k;               /* 1 ... HERSCHEL_MAX_WEIGHT_ROWS, 1 ... 2^30 */
   int32_t group;              /* 32, 64 or 128; the last of a row may be shorter */
 } herschel_weights4;
+
+#define HERSCHEL_MAX_WEIGHT_ROWS 715827840
 
 typedef struct {
   const void *x;              /* [n_rows][k] of kind */

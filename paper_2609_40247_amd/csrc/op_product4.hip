@@ -7,7 +7,8 @@ int product_bf16(ProductArgs& p) { return product_group<HERSCHEL_BF16, false>(p)
 
 extern "C" int herschel_product4_workspace(int64_t n_rows, int32_t kind, int32_t gated, int32_t n, int32_t k, size_t* bytes) {
   using namespace hop;
-  if (!bytes || n_rows < 0 || kind < HERSCHEL_BF16 || kind > HERSCHEL_INT8 || n < 1 || n > (1 << 30) || k < 1 || k > (1 << 30))
+  if (!bytes || n_rows < 0 || kind < HERSCHEL_BF16 || kind > HERSCHEL_INT8 || n < 1 || n > HERSCHEL_MAX_WEIGHT_ROWS || k < 1 ||
+      k > (1 << 30))
     return HERSCHEL_EINVAL;
   ProductArgs p{};
   p.a.n_rows = n_rows;
@@ -28,7 +29,9 @@ extern "C" int herschel_product4(const herschel_product_args* args, const hersch
   const herschel_weights4& w = *weights;
   if (w.n < 1 || w.k < 1 || (w.group != 32 && w.group != 64 && w.group != 128))
     return HERSCHEL_EINVAL;
-  if (w.k > (1 << 30) || w.n > (1 << 30)) return HERSCHEL_EINVAL;  // with what a phase reads beyond they stay in 31 bits
+  // k with what a phase reads beyond stays in 31 bits; the threads of the largest n's workgroups, each 768 for 8 tiles of
+  // 16 rows, in the 32 that a launch counts them in
+  if (w.k > (1 << 30) || w.n > HERSCHEL_MAX_WEIGHT_ROWS) return HERSCHEL_EINVAL;
   if (!w.codes || !w.scales || !aligned(w.codes, 16) || !aligned(w.scales, 16))
     return HERSCHEL_EINVAL;
   if (!type_ok(a.type) || (a.kind != a.type && !quantised(a.kind)) || a.x_row < 0) return HERSCHEL_EINVAL;

@@ -38,7 +38,7 @@ KINDS = {**TYPES, torch.float8_e4m3fn: FP8, torch.int8: INT8}
 LAYOUTS = {"half": 0, "interleaved": 1}
 CODES = {torch.float8_e4m3fn: FP8, torch.int8: INT8}
 BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, BAD_TOKEN, BAD_ROW = 1, 2, 4, 8, 16, 32
-MAX_DECODE_SEQS, MAX_NORM_DIM, MAX_PRODUCT_ROWS, MAX_DRAFTS = 4096, 32768, 4_194_240, 1024
+MAX_DECODE_SEQS, MAX_NORM_DIM, MAX_PRODUCT_ROWS, MAX_WEIGHT_ROWS, MAX_DRAFTS = 4096, 32768, 4_194_240, 715_827_840, 1024
 _FAULTS = {BAD_PAGE: "a block table entry outside the cache", BAD_LENGTH: "lengths that do not fit the buffers",
            BAD_POSITION: "a position outside the rotary table", BAD_SLOT: "a slot beyond the cache's end",
            BAD_TOKEN: "a drafted token outside the vocabulary", BAD_ROW: "probabilities of which none is above 0"}
@@ -685,7 +685,7 @@ class Weights4:
         n, half = codes.shape
         k = 2 * half if k is None else k
         _need(k >= 1 and (k + 1) // 2 == half, "codes must have k / 2 bytes a row, rounded up")
-        _need(n <= 2 ** 30 and k <= 2 ** 30, "at most 2^30 rows and columns")
+        _need(n <= MAX_WEIGHT_ROWS and k <= 2 ** 30, f"at most {MAX_WEIGHT_ROWS} rows and 2^30 columns")
         _need(scales.dtype in TYPES, "scales must be bfloat16 or float16")
         _need(scales.dim() == 2 and scales.shape[0] == n and scales.device == codes.device,
               "scales must be [n, groups], on the codes' device")

@@ -303,3 +303,30 @@ def test_norm_rows_refuses_scales_that_require_gradients():
     with torch.no_grad():
         O.norm_rows(x, w, kind=I8, out=out)
     assert torch.equal(out.scale.detach(), O.norm_rows(x, w, kind=I8).scale)
+
+
+# ------------------------------------------------------------ the largest
+def test_product4_launches_of_the_most_weight_rows(fake):  # noqa: F811
+    """A launch's threads are counted in 32 bits along each line of workgroups: matrices are taken up to the last one
+    whose launch they hold."""
+    most = 715_827_840
+    assert O.MAX_WEIGHT_ROWS == most
+    calls = child(fake, PRODUCT + f"""
+size = ctypes.c_size_t(0)
+for n in ({most}, {most} - 31, {most} // 64 * 32, 1 << 29, 1 << 28, 1 << 27, 10 ** 8, 1 << 24):
+    for rows in (1, 16, 17, 64, 65, 4_194_240):
+        for k in (1, 1024, 50_000, 1 << 30):
+            for kind, gated in ((BF16, 0), (INT8, 0), (FP8, 1)):
+                if not gated or n % 32 == 0:
+                    out.append(product(rows, n, k, 128, kind, gated=gated, out=1 << 61, x=1 << 40, codes=1 << 60, scales=1 << 60, x_row=0))
+                    assert lib.herschel_product4_workspace(ctypes.c_int64(rows), kind, gated, n, k, ctypes.byref(size)) == 0
+out.append((product(1, {most} + 1, 1, 128)[0], None))
+out.append((lib.herschel_product4_workspace(ctypes.c_int64(1), 0, 0, {most} + 1, 1, ctypes.byref(size)), None))
+""")
+    assert [code for code, launched in calls if launched is None] == [-1, -1]
+    for code, launched in calls[:-2]:
+        assert code == 0 and len(launched) == 1
+        x, y, z, threads = (int(v) for v in launched[0][1:5])
+        assert x * threads < 1 << 32 and max(y, z) <= 65_535
+    with pytest.raises(ValueError, match="at most"):
+        O.Weights4(torch.zeros(1, 1, dtype=torch.uint8).expand(most + 1, 1), torch.zeros(1, 1, dtype=BF).expand(most + 1, 1))
