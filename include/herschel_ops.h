@@ -308,7 +308,8 @@ int herschel_verify_workspace(int32_t n_seqs, int32_t vocab, size_t *bytes);
  * above final_u times the sum of all (with a final_u not below 1, the last whose
  * part is above 0).  Products, differences and sums are in 64 bits; what is not
  * above 0, a NaN among it, counts as 0.  A count out of range is taken as the
- * nearest valid one (HERSCHEL_OP_BAD_LENGTH). */
+ * nearest valid one (HERSCHEL_OP_BAD_LENGTH).  What is written shares no memory with
+ * anything (it may lie between rows of probabilities), or the call is refused. */
 int herschel_verify_drafts(const herschel_verify_args *args);
 
 #ifdef __cplusplus

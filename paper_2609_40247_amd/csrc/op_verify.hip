@@ -359,6 +359,25 @@ extern "C" int herschel_verify_drafts(const herschel_verify_args* args) {
     return HERSCHEL_EINVAL;
   if (a.n_drafts && (!a.tokens || !a.accept_u)) return HERSCHEL_EINVAL;
   if (need && (a.workspace_bytes < need || !a.workspace || !aligned(a.workspace, 16))) return HERSCHEL_EWORKSPACE;
+  // a sequence's workgroup reads its tokens, and others theirs, while some have written
+  const int64_t seqs = a.n_seqs, drafts = a.n_drafts;
+  const RowsMemory written[3] = {{a.out, 1, 0, seqs * (drafts + 1) * 8}, {a.accepted, 1, 0, seqs * 4}, {a.workspace, 1, 0, (int64_t)need}};
+  const RowsMemory read[4] = {{drafts ? a.tokens : nullptr, 1, 0, seqs * drafts * 8}, {a.counts, 1, 0, seqs * 4},
+                              {drafts ? a.accept_u : nullptr, 1, 0, seqs * drafts * 4}, {a.final_u, 1, 0, seqs * 4}};
+  auto probabilities = [&](const RowsMemory& w, const void* from, int64_t seq, int64_t row, int64_t rows) {
+    if (!from || !share_memory(w, {from, 1, 0, ((seqs - 1) * seq + (rows - 1) * row + a.vocab) * (int64_t)to})) return false;
+    for (int64_t t = 0; t < rows; ++t)
+      if (share_memory(w, {(const char*)from + t * row * (int64_t)to, seqs, seq * (int64_t)to, a.vocab * (int64_t)to})) return true;
+    return false;
+  };
+  for (int i = 0; i < 3; ++i) {
+    for (const RowsMemory& r : read)
+      if (share_memory(written[i], r)) return HERSCHEL_EINVAL;
+    if (probabilities(written[i], a.target, a.target_seq, a.target_row, drafts + 1)) return HERSCHEL_EINVAL;
+    if (probabilities(written[i], a.draft, a.draft_seq, a.draft_row, drafts)) return HERSCHEL_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (share_memory(written[i], written[j])) return HERSCHEL_EINVAL;
+  }
   VerifyArgs p{a};
   p.shares = shares_of(a.vocab, a.n_seqs, p.size);
   const bool f32 = a.type == HERSCHEL_F32, bf = a.type == HERSCHEL_BF16;

@@ -276,6 +276,47 @@ def test_product4_between_rows():
     assert torch.equal(big, before)
 
 
+def test_verify_drafts_over_what_it_reads_is_refused(fake):  # noqa: F811
+    """Tokens, counts and workspaces over the inputs, or over one another; between rows of probabilities there is room."""
+    codes = child(fake, """
+import struct
+device()
+B, S = 3, 2
+A = {k: 1 << 40 + i for i, k in enumerate(("target", "draft", "tokens", "counts", "accept_u", "final_u", "out", "accepted", "workspace"))}
+
+def verify(vocab, drafted=True, **at):
+    a = {**A, **at}
+    row = 40_000
+    args = struct.pack("@P2qP2q6P4iPN2P", a["target"], (S + 1) * row, row, a["draft"] if drafted else 0, S * row, row, a["tokens"],
+                       a["counts"], a["accept_u"], a["final_u"], a["out"], a["accepted"], B, S, vocab, 4, a["workspace"], 1 << 30, 0, 0)
+    code = lib.herschel_verify_drafts(args)
+    return code, sum(line.startswith("launch ") for line in log())
+
+need = ctypes.c_size_t(0)
+assert lib.herschel_verify_workspace(B, 39_000, ctypes.byref(need)) == 0
+spans = {v: dict(target=[(r * 160_000, v * 4) for r in range(B * (S + 1))], draft=[(r * 160_000, v * 4) for r in range(B * S)],
+                 tokens=[(0, B * S * 8)], counts=[(0, B * 4)], accept_u=[(0, B * S * 4)], final_u=[(0, B * 4)],
+                 out=[(0, B * (S + 1) * 8)], accepted=[(0, B * 4)], workspace=[(0, need.value if v > 32_768 else 0)]) for v in (39_000, 1000)}
+for v, of in spans.items():
+    for w in ("out", "accepted", "workspace"):
+        size = of[w][0][1]
+        for other in A:
+            if w == other or not size or not of[other][0][1]:
+                continue
+            for begin, n in of[other]:
+                for shift, bad in ((-size, False), (16 - size, True), (0, True), ((n + 15) // 16 * 16 - 16, True), ((n + 15) // 16 * 16, False)):
+                    out.append((v, w, other, begin + shift, bad, verify(v, **{w: A[other] + begin + shift})))
+out.append((1000, "", "", 0, False, verify(1000)))
+out.append((1000, "out", "draft", 0, False, verify(1000, drafted=False, out=A["draft"])))
+""")
+    assert len(codes) > 200
+    for *case, bad, (code, launched) in codes:
+        if case[1] == "workspace" and case[3] % 16:
+            assert code == -4 and not launched, case  # that it is not aligned is found first
+        else:
+            assert (code, launched) == ((-1, 0) if bad else (0, 2 if case[0] > 32_768 else 1)), case
+
+
 # ------------------------------------------------------------ 8-bit rows as numbers
 @pytest.mark.parametrize("columns,group", [(200, 64), (1500, 128), (1500, 64), (1500, 32), (96, 32), (64, 64), (130, 128), (40, 32),
                                            (512, 64), (7, 0), (200, 0), (512, 256)])
