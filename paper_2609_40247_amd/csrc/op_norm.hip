@@ -4,7 +4,7 @@
 // 8-bit codes with a scale a row or a group of columns.  A row is read once and
 // stays in the registers of its workgroup: the traffic is the floor, each
 // input read and each output written once, and bounds it: 8192 rows of 5120 in
-// bf16 with the residual, 336 MB, 60.8 us, 5.5 TB/s.  One row of 4096 takes 2.4 us, a
+// bf16 with the residual, 336 MB, 60.7 us, 5.5 TB/s.  One row of 4096 takes 2.6 us, a
 // launch's latency.
 #include "ops.hpp"
 
@@ -256,12 +256,12 @@ static int norm_launch(NormArgs& p) {
                    rows16(a.residual_out, a.residual_out_row, res) && aligned(a.weight, 16) &&
                    aligned(a.out, quantised(OUT) ? 8 : 16);
   // What is written goes past the caches, which hold what is still to be read, where there is much of it (8192 rows of
-  // 5120 66.3 to 60.8 us, 2048 of 4096 11.9 to 11.3); a step's few rows stay in them for the product that reads
-  // them next.
+  // 5120 66.4 to 61.0 us, 2048 of 4096 12.2 to 12.1); a step's few rows stay in them for the product that reads
+  // them next.  Measured on the norm alone: what the product of a prompt's rows pays for it has not been.
   const bool stream = a.n_rows * a.dim >= (1 << 22);
   // A workgroup to a row, a thread to eight of its elements, to sixteen where there are rows enough to fill the card
-  // (2048 rows of 4096 in bf16 with a residual 11.8 us against 13.3 with eight, 8192 of 5120 to fp8 63.8 against 72.6;
-  // one row of 4096 2.4 against 3.0 with sixteen), to 32 for the longest.
+  // (8192 rows of 5120 in bf16 with a residual 61.0 us against 62.9 with eight, to fp8 58.4 against 69.5; 2048 of 4096
+  // 12.1 against 11.8; one row of 4096 2.6 against 3.2 with sixteen), to 32 for the longest.
   const int eights = (a.dim + 7) / 8, share = a.n_rows < 2048 ? 1 : 2;
   int V = 1, T = (eights + WAVE - 1) / WAVE * WAVE;
   while (V < 4 && (T > 1024 || (T > 256 && V < share))) {

@@ -11,7 +11,7 @@
 // at 32000 tokens of one sequence (8.3 us against 3.8 and 4.3) and takes 3 us less of the
 // host; at 64000 it takes 14.8 against 3.8 and 4.4: its sums are 64-bit work of one CU.
 // Large calls are bound by the sums' traffic: 64 sequences of 151936 tokens, 78 MB,
-// 13.0 us, 6.0 TB/s, and 6.0 for the draw.
+// 12.3 us, 6.3 TB/s, and 5.7 for the draw.
 #include "ops.hpp"
 
 namespace hop {

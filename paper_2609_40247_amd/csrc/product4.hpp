@@ -12,9 +12,11 @@
 // constant operand; scale and zero meet the group's sums, not the weights.
 // The bytes of the weights bound large calls of few rows: four rows by a gated
 // 25600 x 5120 matrix, 72 MB, 16.2 us, 4.4 TB/s with the start of the kernel (65 MB that
-// are only read take 15 to 16); small ones their first loads' latency (one row by 6144 x
-// 4096 6.4 us), 64 rows vector instructions (int8 by 5120 x 25600 27.6 us and 4.1 for
-// the join), prompts the copies of x (2048 rows by 6144 x 4096 160 us, 640 TFLOP/s).
+// are only read take 15 to 16; with other weights each time, 600 MB in turn, so that no
+// cache holds them, 20.1); small ones their first loads' latency (one row by 6144 x 4096
+// 6.5 us), 64 rows vector instructions (int8 by 5120 x 25600 27.9 us with the join, with
+// weights in turn 31.0: 26.6 and 4.2), prompts the copies of x (2048 rows by 6144 x 4096
+// 152 us, 680 TFLOP/s).
 #pragma once
 
 #include "ops.hpp"
@@ -474,6 +476,8 @@ static int product_launch(ProductArgs& p, int splits) {  // at most 4
 // rows by 25600 x 5120 weights 17.3 us with 8 tiles a workgroup, 21.2 with 4, 29.5
 // with 2; by 6144 x 4096 7.9 with 2, 9.5 with 4, 11.6 with 1; by 1280 x 5120 7.2 with 1, 8.4 with 2; by 5120 x 25600 22.8 with 4 in three parts,
 // 26.4 with 2 and no parts; by 4096 x 14336 13.8 with 2 in two parts, 16.3 without.
+// fp8 rows and groups of 32 and 64 go by the same times: the choices beside theirs have
+// not been measured.
 struct Choice {
   int wide;    // 0 to 3: one, two, four, eight tiles of weight rows a workgroup
   int splits;
